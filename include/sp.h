@@ -274,7 +274,8 @@ sp_status sp_copy_out(const sp_matrix* h, void* buf_host, size_t buf_cap, uint64
 /* (Library plumbing; no counterpart in the paper.)  Synchronise `stream`; report and clear
  * the current device's status word.
  * Returns SP_ERR_TIMEOUT if a kernel's bounded wait expired since the last
- * check, SP_ERR_CUDA if the stream reported an error, else SP_OK. */
+ * check, SP_ERR_INVALID_ARG if a kernel left out an index of the device tables that it was given
+ * (sp_serve.h; the first of the two), SP_ERR_CUDA if the stream reported an error, else SP_OK. */
 sp_status sp_check(void* stream);
 
 /* (Library plumbing; no counterpart in the paper.)  The identifier of the graph capture that

@@ -360,7 +360,7 @@ sp_status sp_check(void* stream) {
   if (v != 0) {
     const int zero = 0;
     cudaMemcpy(p, &zero, sizeof(int), cudaMemcpyHostToDevice);
-    return SP_ERR_TIMEOUT;
+    return v == kStatusBadIndex ? SP_ERR_INVALID_ARG : SP_ERR_TIMEOUT;
   }
   return SP_OK;
 }

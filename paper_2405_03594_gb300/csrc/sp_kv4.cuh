@@ -1,0 +1,73 @@
+// sp_kv4.cuh -- the layout of a cache held in 4 bits (include/sp_serve.h), and the launch helper of
+// the serving kernels.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "../../include/sp_serve.h"
+#include "sp_internal.cuh"
+
+namespace sp {
+
+constexpr int kMaxGroup = 64;       // query heads per key head
+constexpr int kUnitKeys = 32;       // keys of one step of attend_kernel
+constexpr int kRowTile = 32;        // query rows (token, head of the group) of its widest form
+
+struct Kv4 {
+  uint8_t* data;
+  int64_t pages;
+  int32_t shift;  // page_size = 1 << shift
+  int32_t heads;
+};
+
+inline bool kv4_supported(const sp_kv4* c) {
+  return (c->page_size == 16 || c->page_size == 32 || c->page_size == 64 || c->page_size == 128) &&
+         (c->head_dim == 64 || c->head_dim == 128);
+}
+inline bool kv4_positive(const sp_kv4* c) { return c->pages > 0 && c->kv_heads > 0; }
+inline int page_shift(int page_size) { return __builtin_ctz((unsigned)page_size); }
+inline Kv4 kv4_view(const sp_kv4* c) {
+  return {static_cast<uint8_t*>(c->data), c->pages, page_shift(c->page_size), c->kv_heads};
+}
+
+// Offsets inside a block of P = 1 << shift tokens.
+template <int D>
+__host__ __device__ constexpr int64_t kv4_block_bytes(int shift) { return (int64_t)(D + 8) << shift; }
+template <int D>
+__host__ __device__ constexpr int kv4_value_codes(int shift) { return (D / 2) << shift; }
+template <int D>
+__host__ __device__ constexpr int kv4_key_params(int shift) { return D << shift; }
+template <int D>
+__host__ __device__ constexpr int kv4_value_params(int shift) { return (D + 4) << shift; }
+
+inline bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// SMs of the current device, looked up once per device; 0 if that failed.
+int current_sms();
+
+// A launch under programmatic dependent launch, as the stack's kernels: every kernel starts with
+// griddepcontrol.wait.
+template <typename... Params, typename... Args>
+sp_status launch_pdl(void (*kern)(Params...), dim3 grid, int block, size_t smem, int cluster, cudaStream_t stream,
+                     Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  if (cudaLaunchKernelEx(&cfg, kern, args...) != cudaSuccess) {
+    cudaGetLastError();
+    return SP_ERR_CUDA;
+  }
+  return SP_OK;
+}
+
+}  // namespace sp

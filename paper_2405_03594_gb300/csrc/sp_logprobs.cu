@@ -1,0 +1,363 @@
+// sp_logprobs.cu -- log probabilities of given tokens, the entropy of each row and its most likely
+// entries (include/sp_serve.h).
+//
+// One pass over the row keeps, per thread and around its running maximum m,
+//     s = sum e^(x - m),   z = sum (x - m) e^(x - m),
+// which join as sums do once rescaled to the larger maximum; then
+//     log p(i) = (x_i - m) - log s,   H = log s - z / s.
+// The pass is bound by reading the row.  A row goes to one CTA, or, where rows are few, to a cluster
+// of up to eight that exchange their sums through shared memory.
+//
+// The most likely entries need no second pass over the row: of the threads' own maxima, some k are at
+// least tau (a binary search by block-wide counts), so the k best entries are all at least tau, and
+// only a thread whose maximum is at least tau can hold one.  Those few threads look at their
+// entries again (L2 has them) and the handful that reach tau are ranked by counting.
+#include <cfloat>
+
+#include "sp_kv4.cuh"
+
+namespace sp {
+namespace {
+
+constexpr int kLpThreads = 512;
+constexpr int kLpWarps = kLpThreads / 32;
+constexpr int kMaxTop = 64;
+constexpr int kMaxCluster = 8;
+constexpr int kCandidates = 1024;
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// Keys in the order of the numbers, NaN above all; none is 0.
+__device__ __forceinline__ uint32_t key_of(float x) {
+  const uint32_t u = __float_as_uint(x);
+  if ((u & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
+  return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float of_key(uint32_t k) {
+  if (k == 0xffffffffu) return __uint_as_float(0x7fffffffu);
+  return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k);
+}
+
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+struct Stat {
+  float m, s, z;
+};
+__device__ __forceinline__ Stat join(const Stat& a, const Stat& b) {
+  Stat r;
+  r.m = fmaxf(a.m, b.m);
+  const float da = a.m == -INFINITY ? 0.f : a.m - r.m, db = b.m == -INFINITY ? 0.f : b.m - r.m;
+  const float fa = ex2(da * kLog2e), fb = ex2(db * kLog2e);
+  // a side that has seen nothing but -inf has s = z = 0; one so far below that its factor is 0 may
+  // be an infinite distance below, and adds nothing (a NaN stays in s)
+  r.s = a.s * fa + b.s * fb;
+  r.z = (fa > 0.f ? fmaf(a.s, da, a.z) * fa : 0.f) + (fb > 0.f ? fmaf(b.s, db, b.z) * fb : 0.f);
+  return r;
+}
+
+template <typename T>
+struct Vec;
+template <>
+struct Vec<uint16_t> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ float one(uint16_t u) { return __uint_as_float((uint32_t)u << 16); }
+  static __device__ __forceinline__ void get(const uint4& u, float (&x)[8]) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+};
+template <>
+struct Vec<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ float one(float u) { return u; }
+  static __device__ __forceinline__ void get(const uint4& u, float (&x)[4]) {
+    x[0] = __uint_as_float(u.x), x[1] = __uint_as_float(u.y), x[2] = __uint_as_float(u.z), x[3] = __uint_as_float(u.w);
+  }
+};
+
+template <int N>
+__device__ __forceinline__ void take(Stat& st, float& top, const float (&x)[N]) {
+  float vm = x[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) vm = max_nan(vm, x[i]);
+  top = max_nan(top, vm);
+  if (vm > st.m) {  // (never for a NaN, which makes s NaN below)
+    const float d = st.m == -INFINITY ? 0.f : st.m - vm, f = ex2(d * kLog2e);
+    st.z = f > 0.f ? fmaf(st.s, d, st.z) * f : 0.f;
+    st.s *= f;
+    st.m = vm;
+  }
+  const float m = st.m == -INFINITY ? 0.f : st.m;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float d = x[i] - m, e = ex2(d * kLog2e);
+    st.s += e;
+    st.z = e > 0.f ? fmaf(e, d, st.z) : st.z;
+  }
+}
+
+struct LogprobParams {
+  const void* logits;
+  int64_t stride, vocab;
+  const int64_t* ids;
+  int32_t top, cluster;
+  float *logp, *entropy, *top_logp;
+  int64_t* top_ids;
+  int32_t* status;
+};
+
+__device__ __forceinline__ uint64_t ld_cluster_u64(uint32_t caddr) {
+  uint64_t v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(caddr) : "memory");
+  return v;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kLpThreads) logprobs_kernel(const __grid_constant__ LogprobParams p) {
+  using V = Vec<T>;
+  constexpr int N = V::N;
+  __shared__ uint64_t s_cand[kCandidates];
+  __shared__ uint64_t s_top[kMaxTop];
+  __shared__ Stat s_stat[kLpWarps];
+  __shared__ Stat s_row;
+  __shared__ float s_lse[2];
+  __shared__ int s_count;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = p.cluster > 1 ? (int)cluster_rank() : 0;
+  const int64_t row = blockIdx.x / p.cluster;
+  pdl_wait();
+  const T* x = static_cast<const T*>(p.logits) + row * p.stride;
+  // entries before the first 16-byte boundary, whole vectors, entries behind the last
+  const int64_t head = min((int64_t)(((16 - (reinterpret_cast<uintptr_t>(x) & 15u)) & 15u) / sizeof(T)), p.vocab);
+  const int64_t vecs = (p.vocab - head) / N, tail = head + vecs * N;
+  const int64_t v0 = vecs * rank / p.cluster, v1 = vecs * (rank + 1) / p.cluster;
+  const uint4* xv = reinterpret_cast<const uint4*>(x + head);
+  // the loose entries, at most N - 1 on either side, go to rank 0's first threads
+  const int loose = rank == 0 ? (int)(head + (p.vocab - tail)) : 0;
+  auto loose_at = [&](int i) { return i < head ? (int64_t)i : tail + (i - head); };
+
+  Stat st = {-INFINITY, 0.f, 0.f};
+  float top = -INFINITY;
+  bool any = false;
+  constexpr int kBatch = 4;
+  for (int64_t i = v0 + tid; i < v1; i += kBatch * kLpThreads) {
+    uint4 u[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j)
+      if (i + j * kLpThreads < v1) u[j] = __ldg(xv + i + j * kLpThreads);
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      if (i + j * kLpThreads < v1) {
+        float f[N];
+        V::get(u[j], f);
+        take<N>(st, top, f);
+        any = true;
+      }
+    }
+  }
+  if (tid < loose) {
+    const float f[1] = {V::one(x[loose_at(tid)])};
+    take<1>(st, top, f);
+    any = true;
+  }
+  Stat w = st;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    const Stat o = {__shfl_xor_sync(0xffffffffu, w.m, d), __shfl_xor_sync(0xffffffffu, w.s, d),
+                    __shfl_xor_sync(0xffffffffu, w.z, d)};
+    w = join(w, o);
+  }
+  if (lane == 0) s_stat[warp] = w;
+  if (tid == 0) s_count = 0;
+  if (tid < kMaxTop) s_top[tid] = 0;
+  __syncthreads();
+  if (warp == 0) {
+    w = lane < kLpWarps ? s_stat[lane] : Stat{-INFINITY, 0.f, 0.f};
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+      const Stat o = {__shfl_xor_sync(0xffffffffu, w.m, d), __shfl_xor_sync(0xffffffffu, w.s, d),
+                      __shfl_xor_sync(0xffffffffu, w.z, d)};
+      w = join(w, o);
+    }
+    if (lane == 0) s_row = w;
+  }
+
+  if (p.top > 0) {
+    // tau: a key that at least `top` threads reach (0 if there are not so many)
+    const uint32_t own = any ? key_of(top) : 0u;
+    uint32_t lo = 0, hi = 0xffffffffu;  // count(lo) >= top, or lo = 0
+    while (lo < hi) {
+      const uint32_t mid = lo + (hi - lo) / 2 + 1;
+      const int n = __syncthreads_count(own >= mid);
+      if (n >= p.top) {
+        lo = mid;
+        if (n <= p.top + 8) break;
+      } else {
+        hi = mid - 1;
+      }
+    }
+    const uint32_t tau = lo;
+    auto offer = [&](float f, int64_t at) {
+      const uint32_t k = key_of(f);
+      if (k >= tau) {
+        const int c = atomicAdd(&s_count, 1);
+        if (c < kCandidates) s_cand[c] = ((uint64_t)k << 32) | (uint32_t)~(uint32_t)at;
+      }
+    };
+    if (any && own >= tau) {
+#pragma unroll 4
+      for (int64_t i = v0 + tid; i < v1; i += kLpThreads) {
+        float f[N];
+        V::get(__ldg(xv + i), f);
+#pragma unroll
+        for (int j = 0; j < N; ++j) offer(f[j], head + i * N + j);
+      }
+      if (tid < loose) offer(V::one(x[loose_at(tid)]), loose_at(tid));
+    }
+    __syncthreads();
+    int n = s_count;
+    if (n > kCandidates) {
+      // as many equal entries: the best ones one after the other, each below the one before
+      uint64_t below = ~0ull;
+      for (int r = 0; r < p.top; ++r) {
+        uint64_t best = 0;
+        auto look = [&](float f, int64_t at) {
+          const uint64_t k = ((uint64_t)key_of(f) << 32) | (uint32_t)~(uint32_t)at;
+          if (k < below && k > best) best = k;
+        };
+        if (any && own >= tau) {
+          for (int64_t i = v0 + tid; i < v1; i += kLpThreads) {
+            float f[N];
+            V::get(__ldg(xv + i), f);
+#pragma unroll
+            for (int j = 0; j < N; ++j) look(f[j], head + i * N + j);
+          }
+          if (tid < loose) look(V::one(x[loose_at(tid)]), loose_at(tid));
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, d));
+        if (lane == 0) s_cand[warp] = best;
+        __syncthreads();
+        best = s_cand[lane & (kLpWarps - 1)];
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, d));
+        if (tid == 0) s_top[r] = best;
+        below = best;
+        __syncthreads();
+      }
+    } else {
+      for (int c = tid; c < n; c += kLpThreads) {
+        const uint64_t k = s_cand[c];
+        int above = 0;
+        for (int j = 0; j < n; ++j) above += s_cand[j] > k ? 1 : 0;
+        if (above < p.top) s_top[above] = k;
+      }
+    }
+  }
+  __syncthreads();
+
+  if (p.cluster > 1) {
+    cluster_sync_all();
+    if (rank == 0) {
+      if (tid < p.cluster) {
+        const uint32_t a = cluster_map(smem_u32(&s_row), (uint32_t)tid);
+        s_stat[tid] = Stat{ld_cluster_f32(a), ld_cluster_f32(a + 4), ld_cluster_f32(a + 8)};
+      }
+      const int n = p.cluster * p.top;
+      for (int i = tid; i < n; i += kLpThreads)
+        s_cand[i] = ld_cluster_u64(cluster_map(smem_u32(&s_top[i % p.top]), (uint32_t)(i / p.top)));
+      __syncthreads();
+      if (tid == 0) {
+        Stat a = s_stat[0];
+        for (int i = 1; i < p.cluster; ++i) a = join(a, s_stat[i]);
+        s_row = a;
+      }
+      for (int c = tid; c < n; c += kLpThreads) {
+        const uint64_t k = s_cand[c];
+        int above = 0;
+        for (int j = 0; j < n; ++j) above += s_cand[j] > k ? 1 : 0;
+        if (k != 0 && above < p.top) s_top[above] = k;
+      }
+      __syncthreads();
+    }
+    // (the other CTAs' shared memory has been read once all are here)
+    cluster_sync_all();
+    if (rank != 0) return;
+  }
+  if (tid == 0) {
+    const Stat a = s_row;
+    const float ls = logf(a.s);
+    const bool empty = a.m == -INFINITY && a.s == 0.f;
+    s_lse[0] = a.m;
+    s_lse[1] = ls;
+    p.entropy[row] = empty ? 0.f : ls - a.z / a.s;
+    const int64_t id = p.ids[row];
+    float r = 0.f;
+    if (id >= p.vocab) {
+      set_status(p.status, kStatusBadIndex);
+      r = __uint_as_float(0x7fffffffu);
+    } else if (id >= 0) {
+      r = empty ? -INFINITY : (V::one(x[id]) - a.m) - ls;
+    }
+    p.logp[row] = r;
+  }
+  if (p.top > 0) {
+    __syncthreads();
+    if (tid < p.top) {
+      const uint64_t k = s_top[tid];
+      const float f = of_key((uint32_t)(k >> 32)), m = s_lse[0];
+      p.top_logp[row * p.top + tid] = m == -INFINITY && f == -INFINITY && s_lse[1] == -INFINITY ? -INFINITY : (f - m) - s_lse[1];
+      p.top_ids[row * p.top + tid] = (int64_t)(uint32_t)~(uint32_t)k;
+    }
+  }
+}
+
+}  // namespace
+}  // namespace sp
+
+using namespace sp;
+
+extern "C" sp_status sp_token_logprobs(const void* logits, sp_logits_dtype dtype, int64_t stride, int64_t tokens,
+                                       int64_t vocab, const int64_t* ids, int32_t top, float* logp_out,
+                                       float* entropy_out, float* top_logp_out, int64_t* top_ids_out, void* stream) {
+  if (dtype != SP_LOGITS_BF16 && dtype != SP_LOGITS_F32) return SP_ERR_INVALID_ARG;
+  if (tokens < 0 || vocab < 1 || stride < vocab || top < 0 || top > kMaxTop || top > vocab) return SP_ERR_INVALID_ARG;
+  if (vocab >= (int64_t)1 << 31) return SP_ERR_UNSUPPORTED;
+  if (tokens == 0) return SP_OK;
+  if (!logits || !ids || !logp_out || !entropy_out || (top > 0 && (!top_logp_out || !top_ids_out)))
+    return SP_ERR_INVALID_ARG;
+  const int64_t es = dtype == SP_LOGITS_BF16 ? 2 : 4;
+  if (reinterpret_cast<uintptr_t>(logits) % es) return SP_ERR_ALIGNMENT;
+  const int sms = current_sms();
+  if (sms == 0) return SP_ERR_CUDA;
+  // as many CTAs per row as the SMs have room for two of, each with a vector for half its threads
+  int cluster = 1;
+  while (cluster < kMaxCluster && tokens * cluster * 2 <= 2 * sms &&
+         vocab * es / 16 >= (int64_t)cluster * 2 * (kLpThreads / 2))
+    cluster *= 2;
+  if (tokens * cluster > ((int64_t)1 << 31) - 1) return SP_ERR_UNSUPPORTED;
+  LogprobParams p = {};
+  p.logits = logits;
+  p.stride = stride;
+  p.vocab = vocab;
+  p.ids = ids;
+  p.top = top;
+  p.cluster = cluster;
+  p.logp = logp_out;
+  p.entropy = entropy_out;
+  p.top_logp = top_logp_out;
+  p.top_ids = top_ids_out;
+  p.status = device_status_ptr();
+  auto kern = dtype == SP_LOGITS_BF16 ? logprobs_kernel<uint16_t> : logprobs_kernel<float>;
+  return launch_pdl(kern, dim3((unsigned)(tokens * cluster)), kLpThreads, 0, cluster, (cudaStream_t)stream, p);
+}

@@ -25,13 +25,14 @@ STATUS = {
     5: "SP_ERR_OUT_OF_MEMORY", 6: "SP_ERR_TIMEOUT", 7: "SP_ERR_BAD_HANDLE", 8: "SP_ERR_WORKSPACE",
 }
 SP_ERR_UNSUPPORTED = 2
-# every function declared in include/sp.h and include/sp_stack.h
+# every function declared in include/sp.h, include/sp_stack.h and include/sp_serve.h
 EXPORTS = ["sp_compress", "sp_decompress", "sp_workspace_size", "sp_linear", "sp_linear_ex", "sp_launch_count",
            "sp_kernel_family",
            "sp_linear_noalloc", "sp_test_expired_wait", "sp_masked_update", "sp_linear_w8a8", "sp_w8a8_workspace_size",
            "sp_clone", "sp_free", "sp_info", "sp_copy_out", "sp_check", "sp_capture_id", "sp_status_string",
            "sp_copy_columns", "sp_residual_add", "sp_mul_halves", "sp_mul_pairs", "sp_chain_workspace_size",
-           "sp_chain_run", "sp_linear_epi"]
+           "sp_chain_run", "sp_linear_epi", "sp_kv4_bytes", "sp_kv_plan", "sp_qk_norm_rope", "sp_kv4_read",
+           "sp_kv4_attend", "sp_kv4_attend_workspace_size", "sp_token_logprobs"]
 
 
 KERNELS = {0: "", 1: "linear_cc_kernel", 2: "linear_ccw_kernel", 3: "linear_tc_kernel", 4: "linear_mma_kernel",
@@ -57,6 +58,39 @@ EPILOGUES = {"store": 0, "residual": 1, "pair_product": 2}  # sp_chain_epilogue
 class SpChainOp(ctypes.Structure):
     _fields_ = [("w", ctypes.c_void_p), ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("y", ctypes.c_void_p),
                 ("ldy", ctypes.c_int64), ("r", ctypes.c_void_p), ("epilogue", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class SpKv4(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page_size", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class SpKvPlanArgs(ctypes.Structure):
+    _fields_ = [("cached", ctypes.c_void_p), ("new_tokens", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("free_pages", ctypes.c_void_p), ("free_count", ctypes.c_void_p), ("next_count", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("cu_q", ctypes.c_void_p), ("work", ctypes.c_void_p),
+                ("slots", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("status", ctypes.c_void_p),
+                ("max_tokens", ctypes.c_int64), ("pages", ctypes.c_int64), ("requests", ctypes.c_int32),
+                ("width", ctypes.c_int32), ("page_size", ctypes.c_int32), ("group", ctypes.c_int32)]
+
+
+class SpRopeArgs(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("q_out", ctypes.c_void_p),
+                ("k_out", ctypes.c_void_p), ("cache", ctypes.POINTER(SpKv4)), ("slots", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("cos_sin", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("tokens", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("rot", ctypes.c_int32), ("pairs", ctypes.c_int32)]
+
+
+class SpAttendArgs(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("out_stride", ctypes.c_int64), ("cache", ctypes.POINTER(SpKv4)), ("table", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("cu_q", ctypes.c_void_p), ("work", ctypes.c_void_p),
+                ("tokens", ctypes.c_int64), ("requests", ctypes.c_int32), ("width", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("max_new", ctypes.c_int32), ("scale", ctypes.c_float),
                 ("reserved", ctypes.c_int32)]
 
 
@@ -94,6 +128,13 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.sp_linear_epi.argtypes = [P, P, I64, P, ctypes.c_int32, P, P, SZ, P]
     lib.sp_chain_workspace_size.argtypes = [I64, ctypes.POINTER(SZ)]
     lib.sp_chain_run.argtypes = [ctypes.POINTER(SpChainOp), ctypes.c_int32, I64, P, SZ, P]
+    lib.sp_kv4_bytes.argtypes = [ctypes.POINTER(SpKv4), ctypes.POINTER(SZ)]
+    lib.sp_kv_plan.argtypes = [ctypes.POINTER(SpKvPlanArgs), P]
+    lib.sp_qk_norm_rope.argtypes = [ctypes.POINTER(SpRopeArgs), P]
+    lib.sp_kv4_read.argtypes = [ctypes.POINTER(SpKv4), P, I64, P, P, P]
+    lib.sp_kv4_attend.argtypes = [ctypes.POINTER(SpAttendArgs), P, SZ, P]
+    lib.sp_kv4_attend_workspace_size.argtypes = [ctypes.c_int32, ctypes.POINTER(SZ)]
+    lib.sp_token_logprobs.argtypes = [P, ctypes.c_int, I64, I64, I64, P, ctypes.c_int32, P, P, P, P, P]
     lib.sp_status_string.argtypes = [ctypes.c_int]
     lib.sp_status_string.restype = ctypes.c_char_p
     for name in EXPORTS:
