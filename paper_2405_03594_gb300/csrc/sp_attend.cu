@@ -2,25 +2,30 @@
 // short runs of tokens of many requests.
 //
 // Mathematics.  With codes n, scale s and minimum m per key, and c = scale * log2(e):
-//     log2 score   = c s_k (q . n) + c m_k sum(q)
-//     out          = (sum_k (p_k s_k) (n - 8) + sum_k p_k (m_k + 8 s_k)) / sum_k p_k
-// so the products run on the codes themselves, which bf16 holds exactly, and no value is rounded:
-// the queries are bf16 already, and p_k s_k enters as the sum of two bf16 numbers.  The codes of
-// the keys enter as 128 + n (a code's bits under the exponent of 128), and 128 s_k moves into m_k;
-// over a long context that offset would swamp the fp32 sums of the values, which take n - 8.
+//     log2 score   x_k = c s_k (q . n) + c m_k sum(q)
+//     out          = (sum_k (e_k s_k) n + sum_k e_k m_k) / sum_k e_k,    e_k = 2^(x_k - M)
+// so both products run on the codes.  A code's four bits, wherever they lie in the low byte of a
+// 16-bit half, are an fp16 subnormal, n 2^-24 or n 2^-20, which the tensor cores multiply exactly:
+// one AND per two codes is all the expansion there is.  The queries enter as fp16 too, exactly: a
+// row is scaled by the power of two that brings its largest entry under fp16's (bf16 has fewer
+// bits).  The weights e_k s_k of the values are rounded to fp16; M is a running maximum of
+// x_k + log2(s_k), so that they stay below 2^8 and their large ones keep 11 bits whatever the scales
+// are.  M moves only when a weight would pass 2^8, so most steps rescale nothing.
 //
 // Layout.  A warp takes units of 32 keys.  Both products have the codes as the wide operand of
 // m16n8k16 (keys, then channels, along M) and up to 8 NT query rows -- the heads that share the key
 // head, times the new tokens -- along N.  The channels of a key, and the keys of a channel, may be
-// taken in any order in a sum, so each lane's operand is the 16 consecutive bytes of a key (keys) or
-// 8 of four keys (values) that it loads from global memory in one go: no shared memory, no shuffle.
-// The scores' transposition between the products is movmatrix.
+// taken in any order in a sum, so a lane's operand is 16 consecutive bytes of a key, or 8 of four
+// keys.  The scores' transposition between the products is movmatrix.  Each warp copies its own units
+// into a ring in shared memory (bulk copies: a unit's keys, values and parameters are contiguous).
 //
 // Split.  The units of all requests, key heads and row tiles form one list, cut into equal ranges,
-// one per CTA, whatever the lengths of the requests are; the warps of a CTA share each segment (the
-// units of one request, head and row tile) and join their maxima and sums in shared memory.  A
-// segment that several CTAs share is joined from the workspace, in their order, by the last of them.
+// first among CTAs (one per SM), then among their warps, whatever the lengths of the requests are.  A
+// warp finishes the segments (units of one request, head and row tile) that it holds whole; of the
+// others it leaves sums and maxima in shared memory, which the CTA joins at its end, and where a
+// segment spans CTAs the last of them joins their parts from the workspace, in order.
 #include <algorithm>
+#include <climits>
 
 #include "sp_kv4.cuh"
 #include "sp_lookup.h"
@@ -28,11 +33,14 @@
 namespace sp {
 namespace {
 
-constexpr int kWarps = 4;
-constexpr int kThreads = 32 * kWarps;
-constexpr int kCtasPerSm = 3;
-constexpr int kMinUnits = 2 * kWarps;  // units of a CTA, before more CTAs share the work
 constexpr int kMaxDevices = 64;
+constexpr int kMinUnits = 8;  // units of a CTA, before more CTAs share the work
+
+// Warps of a CTA, stages of a warp's ring and place of its query operands, for NT tiles of eight query
+// rows: what the registers and shared memory of an SM hold.
+constexpr int warps_of(int d, int nt) { return nt == 1 ? 16 : nt == 2 ? (d == 64 ? 12 : 8) : d == 64 ? 8 : 6; }
+constexpr int stages_of(int d, int nt) { return d == 64 ? 4 : nt == 1 ? 2 : nt == 2 ? 4 : 3; }
+constexpr bool queries_shared(int d, int nt) { return nt == 4; }
 
 struct AttendParams {
   const uint16_t* q;
@@ -43,20 +51,27 @@ struct AttendParams {
   int32_t requests, width, group;
   int32_t max_new;
   int64_t tokens;
+  int32_t group_inverse;  // 2^16 / group, rounded up
   float scale_log2;
   float* part;  // [2 grid][8 NT] of (D sums, maximum, sum of weights, unused)
   int* cnt;     // [grid]
   int32_t* status;
+  uint64_t timeout_ns;
 };
 
-__device__ __forceinline__ float exp2_approx(float x) {
+__device__ __forceinline__ float ex2(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
-                                         uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+__device__ __forceinline__ float lg2(float x) {
+  float r;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -65,32 +80,45 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
   return r;
 }
-// bf16 pair (128 + n_i, 128 + n_{i+4}) of the nibbles i and i + 4 of w
-__device__ __forceinline__ uint32_t codes128(uint32_t w, int i) { return ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u; }
-// bf16 pair (n - 8) of the same nibbles
-__device__ __forceinline__ uint32_t codes8(uint32_t w, int i) {
-  const uint32_t x = codes128(w, i);
-  uint32_t r;
-  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(0x43084308u));  // 136
-  return r;
-}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// fp16 pairs of the nibbles i and i + 4 of w: n 2^-24 for i = 0 (and 2, of w >> 8), n 2^-20 for i = 1 (3)
+__device__ __forceinline__ uint32_t nib_lo(uint32_t w) { return w & 0x000f000fu; }
+__device__ __forceinline__ uint32_t nib_hi(uint32_t w) { return w & 0x00f000f0u; }
+constexpr float kLo = 16777216.f, kHi = 1048576.f;
 
-// The codes and parameters of one unit, as a lane holds them.
-template <int D>
-struct UnitK {
-  uint32_t w[2][2][D / 32];  // [16 keys][key g, g + 8][words: channels D/4 t ...]
-  uint32_t par[2][2];
-};
-template <int D>
-struct UnitV {
-  uint32_t w[2][4][D / 64];  // [16 keys][keys 2t, 2t + 1, 2t + 8, 2t + 9][words: channels D/8 g ...]
-  uint32_t par[2][2];        // of keys g, g + 8
-};
+// Two fp32 numbers in one register pair, and arithmetic on both at once.
+__device__ __forceinline__ uint64_t two(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void apart(uint64_t x, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x));
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
 
 template <int W>
 __device__ __forceinline__ void load_words(uint32_t (&d)[W], const uint8_t* p) {
@@ -105,390 +133,699 @@ __device__ __forceinline__ void load_words(uint32_t (&d)[W], const uint8_t* p) {
   }
 }
 
-// A segment: units [u0, u1) of `units` of one request, key head and row tile.
-struct Segment {
-  int b, h, rt;
-  int units, u0, u1;
-  int rows;       // query rows of the tile
-  int row0;       // first of them among the request's
-  int fresh, len;
+// The list of units in equal ranges: part i of n takes [begin(i), begin(i + 1)).
+struct Ranges {
+  int each, more;  // the first `more` parts take one unit more
+  __device__ __forceinline__ Ranges(int units, int n) : each(units / n), more(units % n) {}
+  __device__ __forceinline__ int begin(int i) const { return i * each + min(i, more); }
+  __device__ __forceinline__ int owner(int u) const {
+    const int cut = more * (each + 1);
+    return u < cut ? u / (each + 1) : more + (u - cut) / each;
+  }
 };
 
+// A segment: the units of one request, key head and row tile.
+struct Segment {
+  int vis0;         // its first unit's place in the list
+  int seen;         // its units that any of its rows sees
+  int h;            // key head
+  int q0, head0;    // row of q and head, among the group's, of its first query row
+  int rows;         // query rows
+  int sees;         // keys that its first row sees
+};
+
+// What a stage of a ring holds.
+struct Meta {
+  int u, ok, opens;  // the unit, its halves that have a page, whether a segment begins
+  Segment s;         // that segment
+};
+
+// What a warp leaves in shared memory of a segment that it does not hold whole.
+struct PartInfo {
+  int vis0, seen, rows;  // rows == 0: nothing
+  int h, q0, head0;
+};
+
+// One row of n parts, by a warp: its maximum and sum of weights (in every lane), and C of its sums.
+template <int C>
+struct Row {
+  float m, sum, acc[C];
+};
+template <int C, class Stat, class Sums>
+__device__ __forceinline__ Row<C> join(int n, Stat stat_at, Sums sums_at) {
+  const int lane = threadIdx.x & 31;
+  Row<C> r;
+  // the first 32 parts' numbers stay in registers
+  const float2 own = lane < n ? stat_at(lane) : make_float2(-INFINITY, 0.f);
+  r.m = own.x;
+  for (int k = lane + 32; k < n; k += 32) r.m = fmaxf(r.m, stat_at(k).x);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) r.m = fmaxf(r.m, __shfl_xor_sync(0xffffffffu, r.m, d));
+  const float safe = r.m == -INFINITY ? 0.f : r.m;
+  r.sum = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) r.acc[c] = 0.f;
+  for (int k0 = 0; k0 < n; k0 += 32) {
+    float f = 0.f;
+    if (k0 + lane < n) {
+      const float2 st = k0 == 0 ? own : stat_at(k0 + lane);
+      f = ex2(st.x - safe);
+      r.sum = fmaf(st.y, f, r.sum);
+    }
+    const int kn = min(32, n - k0);
+    for (int k = 0; k < kn; k += 4) {
+      Row<C> a[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (k + i < kn) a[i] = sums_at(k0 + k + i);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float fk = __shfl_sync(0xffffffffu, f, (k + i) & 31);
+        if (k + i < kn) {
+#pragma unroll
+          for (int c = 0; c < C; ++c) r.acc[c] = fmaf(a[i].acc[c], fk, r.acc[c]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) r.sum += __shfl_xor_sync(0xffffffffu, r.sum, d);
+  return r;
+}
+
 template <int D, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? kCtasPerSm : 2)
-    attend_kernel(const __grid_constant__ AttendParams p) {
+__global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const __grid_constant__ AttendParams p) {
   constexpr int KW = D / 32, VW = D / 64;  // words of a lane: keys, values
   constexpr int MT = D / 16;               // channel tiles
   constexpr int R = 8 * NT;                // query rows
-  extern __shared__ __align__(16) float smem[];  // [kWarps][R][D] sums, then [kWarps][R] (maximum, weights, offset)
-  __shared__ int s_last;
-  float* s_o = smem;
-  float4* s_stat = reinterpret_cast<float4*>(smem + kWarps * R * D);
+  constexpr int W = warps_of(D, NT), S = stages_of(D, NT);
+  constexpr bool kQShared = queries_shared(D, NT);
+  constexpr int kCodes = kUnitKeys * D / 2;
+  constexpr int kStage = 2 * kCodes + 2 * kUnitKeys * 4;
+  constexpr int kRow = D + 4;              // floats of a row of a part: sums, maximum, weights
+  constexpr int kPartBytes = R * kRow * 4;
+  constexpr int kQBytes = kQShared ? 32 * NT * KW * 16 : 0;  // query operands of a warp
+  static_assert(S * kStage + kQBytes >= kPartBytes, "a warp's last part takes the place of its ring");
+  constexpr int kFirst = S * kStage + kQBytes, kWarpBytes = kFirst + kPartBytes;
+  extern __shared__ __align__(128) uint8_t smem[];  // [W] of (ring, query operands, first part)
+  __shared__ uint64_t s_bar[W][S];
+  __shared__ Meta s_meta[W][S];
+  __shared__ PartInfo s_info[W][2];
+  __shared__ int s_last[2], s_order[2 * W], s_row0[2 * W], s_parts, s_rows;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const int kg = g ^ ((g >> 1) & 1);  // key of operand row g: neighbours in different halves of the banks
+  uint8_t* ring = smem + warp * kWarpBytes;
+  uint4* q_shared = reinterpret_cast<uint4*>(ring + S * kStage) + lane;
+  uint64_t* bar = s_bar[warp];
+  if (lane == 0) {
+    for (int i = 0; i < S; ++i) mbar_init(&bar[i], 1);
+    fence_barrier_init();
+    s_info[warp][0].rows = s_info[warp][1].rows = 0;
+  }
+  __syncwarp();
   pdl_wait();
 
-  const int64_t total = (int64_t)p.work[p.requests] * p.cache.heads;
-  const int64_t ctas = max((int64_t)1, min((int64_t)gridDim.x, total / kMinUnits));
+  const int heads = p.cache.heads;
+  const int64_t all = (int64_t)p.work[p.requests] * heads;
+  const int total = (int)min(all, (int64_t)INT_MAX);
+  if (total != all && tid == 0) set_status(p.status, kStatusBadIndex);
+  const int ctas = max(1, min((int)gridDim.x, total / kMinUnits));
   if (blockIdx.x >= ctas) return;
-  const int64_t w0 = range_begin(blockIdx.x, total, ctas), w1 = range_begin(blockIdx.x + 1, total, ctas);
+  const Ranges by_cta(total, ctas);
+  const int c0 = by_cta.begin(blockIdx.x), c1 = by_cta.begin(blockIdx.x + 1);
+  const Ranges by_warp(c1 - c0, W);
+  const int w0 = c0 + by_warp.begin(warp), w1 = c0 + by_warp.begin(warp + 1);
   const int shift = p.cache.shift;
   const int64_t block = kv4_block_bytes<D>(shift);
+  // the token of query row x, counted from the head 0 of a token (x < 2^7, so the quotient is exact)
+  auto token_of = [&](int x) { return x * p.group_inverse >> 16; };
+  // row r of a segment in q or out
+  auto q_row = [&](int q0, int h, int head0, int r, auto* base, int64_t stride) {
+    const int token = token_of(head0 + r);
+    return base + (int64_t)(q0 + token) * stride + (int64_t)(h * p.group + head0 + r - token * p.group) * D;
+  };
 
-  int b = 0;
-  if (w0 < w1) {  // the request of the first unit
-    int lo = 0, hi = p.requests;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if ((int64_t)p.work[mid] * p.cache.heads <= w0) lo = mid;
-      else hi = mid;
-    }
-    b = lo;
-  }
-  for (int64_t w = w0; w < w1;) {
-    while (b + 1 < p.requests && (int64_t)p.work[b + 1] * p.cache.heads <= w) ++b;
-    Segment s;
-    s.b = b;
-    s.len = p.lens[b];
-    const int q0 = p.cu_q[b];
-    s.fresh = p.cu_q[b + 1] - q0;
-    const int64_t base = (int64_t)p.work[b] * p.cache.heads, next = (int64_t)p.work[b + 1] * p.cache.heads;
-    s.units = (int)(((int64_t)s.len + kUnitKeys - 1) / kUnitKeys);
-    // shares that do not belong to these lengths are passed over by every CTA alike
-    const int64_t tiles = ((int64_t)s.fresh * p.group + kRowTile - 1) / kRowTile;
-    if (w < base || next <= w || s.units <= 0 || tiles <= 0 || tiles * s.units * p.cache.heads != next - base) {
-      if (tid == 0) set_status(p.status, kStatusBadIndex);
-      if (next <= w) break;
-      w = next;
-      continue;
-    }
-    const int64_t idx = (w - base) / s.units;  // (row tile, key head)
-    s.u0 = (int)((w - base) - idx * s.units);
-    s.u1 = (int)min((int64_t)s.units, s.u0 + (w1 - w));
-    s.h = (int)(idx % p.cache.heads);
-    s.rt = (int)(idx / p.cache.heads);
-    s.row0 = s.rt * kRowTile;
-    s.rows = min(s.fresh * p.group - s.row0, kRowTile);
-    if (s.fresh > p.max_new || q0 < 0 || q0 + (int64_t)s.fresh > p.tokens) {
-      if (tid == 0) set_status(p.status, kStatusBadIndex);
-      s.rows = 0;
-    }
-    const int rows = min(s.rows, R);
-    const int64_t seg0 = w - s.u0;  // the segment's first unit in the list, with other CTAs' shares
-    w += s.u1 - s.u0;
-
-    // queries: operand registers, and sums over the channels
-    uint32_t qf[NT][KW][4];
-    float qsum[NT][2];
-    int limit[NT][2];  // keys seen by query rows 2t, 2t + 1
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int r = nt * 8 + g;
-      float sum = 0.f;
-      const int row = s.row0 + r;
-      const uint16_t* src = p.q + (q0 + row / p.group) * p.q_stride + (int64_t)(s.h * p.group + row % p.group) * D + t * (D / 4);
-#pragma unroll
-      for (int i = 0; i < KW; ++i) {
-        uint4 u = make_uint4(0, 0, 0, 0);
-        if (r < rows) u = *(reinterpret_cast<const uint4*>(src) + i);
-        const uint32_t x[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) sum += __uint_as_float(x[j] << 16) + __uint_as_float(x[j] & 0xffff0000u);
-        qf[nt][i][0] = __byte_perm(u.x, u.z, 0x5410);  // channels 0, 4
-        qf[nt][i][1] = __byte_perm(u.x, u.z, 0x7632);  // 1, 5
-        qf[nt][i][2] = __byte_perm(u.y, u.w, 0x5410);  // 2, 6
-        qf[nt][i][3] = __byte_perm(u.y, u.w, 0x7632);  // 3, 7
-      }
-      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        qsum[nt][c] = __shfl_sync(0xffffffffu, sum, 4 * (2 * t + c)) * p.scale_log2;
-        const int rr = nt * 8 + 2 * t + c;
-        limit[nt][c] = rr < rows ? s.len - s.fresh + (s.row0 + rr) / p.group + 1 : 0;
-      }
-    }
-    const int most = rows > 0 ? s.len - s.fresh + (s.row0 + rows - 1) / p.group + 1 : 0;  // keys that any row sees
-
-    float o[NT][MT][4];
-    float mx[NT][2], l[NT][2], off[NT][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-      for (int i = 0; i < MT; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
-#pragma unroll
-      for (int c = 0; c < 2; ++c) mx[nt][c] = -INFINITY, l[nt][c] = 0.f, off[nt][c] = 0.f;
-    }
-
-    const int u_end = min(s.u1, (most + kUnitKeys - 1) / kUnitKeys);
-    const int32_t* table = p.table + (int64_t)s.b * p.width;
-    // block of the 16 keys from k0 on; null behind the last key (or for a page that does not exist)
-    auto block_of = [&](int k0) -> const uint8_t* {
-      if (k0 >= most) return nullptr;
-      const int page = (k0 >> shift) < p.width ? table[k0 >> shift] : -1;
-      if (page < 0 || page >= p.cache.pages) {
-        set_status(p.status, kStatusBadIndex);
-        return nullptr;
-      }
-      return p.cache.data + ((int64_t)page * p.cache.heads + s.h) * block;
+  if (w0 < w1) {
+    // ---------------------------------------------------------------- the copies
+    // 32 requests from wb on, one per lane: where their units end, lengths, rows of q
+    int wb = 0, w_end, w_len, w_q0, w_q1, w_base;
+    auto window = [&] {
+      const int b = wb + lane;
+      w_base = p.work[wb];
+      w_end = b < p.requests ? p.work[b + 1] : INT_MAX;
+      w_len = b < p.requests ? p.lens[b] : 0;
+      w_q0 = b < p.requests ? p.cu_q[b] : 0;
+      w_q1 = b < p.requests ? p.cu_q[b + 1] : 0;
     };
-    auto load_k = [&](UnitK<D>& k, int u) {
+    if (p.requests > 32) {
+      // a window that holds the first unit's request: 32 shares at a time
+      int lo = 0, n = p.requests;
+      const int first = w0 / heads;
+      while (n > 32) {
+        const int step = (n + 31) / 32;
+        const int at = lo + min(n, (lane + 1) * step);
+        const unsigned past = __ballot_sync(0xffffffffu, p.work[at] > first);
+        const int k = past ? __ffs(past) - 1 : 31;
+        n = min(step, n - min(n, k * step));
+        lo += k * step;
+      }
+      wb = min(lo, p.requests - 1);
+    }
+    window();
+    Segment ps = {};
+    int pw = w0, p_end = w0, pu = 0;         // the next unit; where its segment ends; its place there
+    int p_b = 0, p_len = 0;                  // its request, that one's tokens
+    int pg_from = 0, page[2] = {-1, -1};       // pages of 32 units, one per lane, from pg_from on
+    bool opens = false;
+    int pstage = 0, pending = 0;
+    // the segment that holds unit pw; a share that does not belong to the lengths is passed over
+    auto find = [&] {
+      unsigned past;
+      while (!(past = __ballot_sync(0xffffffffu, (int64_t)w_end * heads > pw))) {
+        wb += 32;
+        window();
+      }
+      const int k = __ffs(past) - 1;
+      const int end = __shfl_sync(0xffffffffu, w_end, k);
+      const int before = __shfl_sync(0xffffffffu, w_end, max(k - 1, 0));
+      const int begin = (k == 0 ? w_base : before) * heads;
+      p_len = __shfl_sync(0xffffffffu, w_len, k);
+      const int q0 = __shfl_sync(0xffffffffu, w_q0, k), fresh = __shfl_sync(0xffffffffu, w_q1, k) - q0;
+      p_b = wb + k;
+      const int units = (p_len + kUnitKeys - 1) / kUnitKeys + kSetupUnits;
+      const int tiles = (int)(((int64_t)fresh * p.group + kRowTile - 1) / kRowTile);
+      opens = true;
+      if (p_b >= p.requests || pw < begin || tiles <= 0 || p_len < fresh || fresh > p.max_new || q0 < 0 ||
+          q0 + (int64_t)fresh > p.tokens || (int64_t)tiles * units != (int64_t)end - begin / heads) {
+        if (lane == 0) set_status(p.status, kStatusBadIndex);
+        p_end = p_b >= p.requests ? w1 : (int)min((int64_t)w1, (int64_t)end * heads);
+        pu = ps.seen = 0;
+        return;
+      }
+      const int idx = (pw - begin) / units;  // (row tile, key head)
+      const int at = begin + idx * units;
+      const int tile = idx / heads, row0 = tile * kRowTile, token = row0 / p.group;
+      ps.h = idx - tile * heads;
+      ps.q0 = q0 + token;
+      ps.head0 = row0 - token * p.group;
+      ps.rows = min(min(fresh * p.group - row0, kRowTile), R);
+      ps.sees = p_len - fresh + token + 1;
+      ps.seen = (ps.sees + token_of(ps.head0 + ps.rows - 1) + kUnitKeys - 1) / kUnitKeys;
+      ps.vis0 = at + kSetupUnits;
+      p_end = at + units;
+      pu = max(0, pw - ps.vis0);
+      pw = max(pw, ps.vis0);
+      // its queries, on their way while its pages are looked up
+      for (int i = lane; i < ps.rows * (D / 64); i += 32) {
+        const uint16_t* q = q_row(ps.q0, ps.h, ps.head0, i / (D / 64), p.q, p.q_stride) + i % (D / 64) * 64;
+        asm volatile("prefetch.global.L1 [%0];" ::"l"(q));
+      }
+    };
+    // copies the next unit of the range that any row sees; nothing where there is none
+    auto issue = [&] {
+      while (pu >= ps.seen || pw >= p_end) {
+        pw = max(pw, p_end);
+        if (pw >= w1) return;
+        find();
+      }
+      if (pw >= w1) return;
+      if (opens || pu >= pg_from + 32) {
+        pg_from = pu;
+        const int32_t* row = p.table + (int64_t)p_b * p.width;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int k0 = u * kUnitKeys + 16 * i;
-        const uint8_t* bl = block_of(k0);
-        const int in = (k0 & ((1 << shift) - 1)) + g;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          if (bl) {
-            load_words<KW>(k.w[i][j], bl + (in + 8 * j) * (D / 2) + t * (D / 8));
-            k.par[i][j] = *(reinterpret_cast<const uint32_t*>(bl + kv4_key_params<D>(shift)) + in + 8 * j);
+        for (int i = 0; i < 2; ++i) {
+          const int64_t k0 = (int64_t)(pu + lane) * kUnitKeys + 16 * i;
+          const int at = (int)(k0 >> shift);
+          page[i] = -1;
+          if (k0 < p_len) {
+            if (at < p.width) page[i] = row[at];
+            if (page[i] < 0 || page[i] >= p.cache.pages) {
+              page[i] = -1;
+              set_status(p.status, kStatusBadIndex);
+            }
+          }
+        }
+      }
+      const int pg0 = __shfl_sync(0xffffffffu, page[0], pu - pg_from), pg1 = __shfl_sync(0xffffffffu, page[1], pu - pg_from);
+      if (lane == 0) {
+        uint8_t* dst = ring + pstage * kStage;
+        uint64_t* full = &bar[pstage];
+        const uint8_t* b0 = p.cache.data + ((int64_t)pg0 * heads + ps.h) * block;
+        Meta& m = s_meta[warp][pstage];
+        m.u = pu;
+        m.ok = shift >= 5 ? (pg0 >= 0 ? 3 : 0) : (pg0 >= 0 ? 1 : 0) | (pg1 >= 0 ? 2 : 0);
+        m.opens = opens;
+        if (opens) m.s = ps;
+        if (shift >= 5) {  // the unit lies in one page
+          if (pg0 >= 0) {
+            const int in = (pu * kUnitKeys) & ((1 << shift) - 1);
+            mbar_arrive_expect_tx(full, kStage);
+            bulk_g2s(dst, b0 + in * (D / 2), kCodes, full);
+            bulk_g2s(dst + kCodes, b0 + kv4_value_codes<D>(shift) + in * (D / 2), kCodes, full);
+            bulk_g2s(dst + 2 * kCodes, b0 + kv4_key_params<D>(shift) + in * 4, kUnitKeys * 4, full);
+            bulk_g2s(dst + 2 * kCodes + kUnitKeys * 4, b0 + kv4_value_params<D>(shift) + in * 4, kUnitKeys * 4, full);
           } else {
+            mbar_arrive(full);
+          }
+        } else {
+          const uint8_t* b1 = p.cache.data + ((int64_t)pg1 * heads + ps.h) * block;
+          mbar_arrive_expect_tx(full, (pg0 >= 0 ? kStage / 2 : 0) + (pg1 >= 0 ? kStage / 2 : 0));
 #pragma unroll
-            for (int x = 0; x < KW; ++x) k.w[i][j][x] = 0;
-            k.par[i][j] = 0;
+          for (int i = 0; i < 2; ++i) {
+            if ((i ? pg1 : pg0) < 0) continue;
+            const uint8_t* bl = i ? b1 : b0;
+            bulk_g2s(dst + i * (kCodes / 2), bl, kCodes / 2, full);
+            bulk_g2s(dst + kCodes + i * (kCodes / 2), bl + kv4_value_codes<D>(shift), kCodes / 2, full);
+            bulk_g2s(dst + 2 * kCodes + i * 64, bl + kv4_key_params<D>(shift), 64, full);
+            bulk_g2s(dst + 2 * kCodes + kUnitKeys * 4 + i * 64, bl + kv4_value_params<D>(shift), 64, full);
           }
         }
       }
+      opens = false;
+      if (++pstage == S) pstage = 0;
+      ++pu;
+      ++pw;
+      ++pending;
     };
-    auto load_v = [&](UnitV<D>& v, int u) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int k0 = u * kUnitKeys + 16 * i;
-        const uint8_t* bl = block_of(k0);
-        const int in = k0 & ((1 << shift) - 1);
+    for (int i = 0; i < S; ++i) issue();
+    __syncwarp();
+
+    // ---------------------------------------------------------------- the segments of the range
+    int stage = 0;
+    uint32_t phase = 0;
+    bool dead = false;
+    while (pending > 0 && !dead) {
+      const Segment s = s_meta[warp][stage].s;
+      int u = s_meta[warp][stage].u;
+      const int u0 = u;
+      // queries: fp16 operand registers, and sums over the channels
+      uint32_t qf[kQShared ? 1 : NT][KW][4];
+      uint64_t qsum[NT];  // of query rows 2t, 2t + 1: c sum(q)
+      int limit[NT][2];   // keys that they see
+      float rs;           // c 2^24 / the queries' scaling
+      {
+        auto load = [&](int nt, uint4(&x)[KW]) {
+          const uint16_t* src = q_row(s.q0, s.h, s.head0, nt * 8 + g, p.q, p.q_stride) + t * (D / 4);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (bl) {
-            load_words<VW>(v.w[i][j],
-                           bl + kv4_value_codes<D>(shift) + (in + 2 * t + (j & 1) + 8 * (j >> 1)) * (D / 2) + g * (D / 16));
-          } else {
+          for (int i = 0; i < KW; ++i) {
+            x[i] = make_uint4(0, 0, 0, 0);
+            if (nt * 8 + g < s.rows) x[i] = *(reinterpret_cast<const uint4*>(src) + i);
+          }
+        };
+        uint32_t big = 0;  // the largest entry's magnitude, as bf16 bits
+        uint4 x4[KW];
+#pragma unroll(kQShared ? 1 : NT)
+        for (int nt = 0; nt < NT; ++nt) {
+          load(nt, x4);
 #pragma unroll
-            for (int x = 0; x < VW; ++x) v.w[i][j][x] = 0;
+          for (int i = 0; i < KW; ++i) {
+            const uint32_t x[4] = {x4[i].x, x4[i].y, x4[i].z, x4[i].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) big = max(big, max(x[j] & 0x7fffu, (x[j] >> 16) & 0x7fffu));
           }
         }
+        // 2^(141 - e): the largest entry, of biased exponent e, comes to 2^14 ... 2^15
+        const uint32_t e = max(15u, min(254u, __reduce_max_sync(0xffffffffu, big) >> 7));
+        const float f = __uint_as_float((268u - e) << 23);
+        rs = __uint_as_float((e - 14u) << 23) * kLo * p.scale_log2;
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-          v.par[i][j] = bl ? *(reinterpret_cast<const uint32_t*>(bl + kv4_value_params<D>(shift)) + in + g + 8 * j) : 0u;
-      }
-    };
-
-    UnitK<D> kn;
-    int u = s.u0 + warp;
-    if (u < u_end) load_k(kn, u);
-    for (; u < u_end; u += kWarps) {
-      const UnitK<D> k = kn;
-      UnitV<D> v;
-      load_v(v, u);
-      if (u + kWarps < u_end) load_k(kn, u + kWarps);
-
-      float x[NT][2][4];  // scores: [16 keys][key g row 2t, row 2t + 1, key g + 8 ...]
+        for (int nt = 0; nt < NT; ++nt) {
+          if (NT > 1) load(nt, x4);
+          float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+          for (int i = 0; i < KW; ++i) {
+            const uint32_t x[4] = {x4[i].x, x4[i].y, x4[i].z, x4[i].w};
+            float y[8];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) x[nt][i][0] = x[nt][i][1] = x[nt][i][2] = x[nt][i][3] = 0.f;
-#pragma unroll
-        for (int j = 0; j < KW; ++j) {
-#pragma unroll
-          for (int hh = 0; hh < 2; ++hh) {
-            const uint32_t a0 = codes128(k.w[i][0][j], 2 * hh), a1 = codes128(k.w[i][1][j], 2 * hh);
-            const uint32_t a2 = codes128(k.w[i][0][j], 2 * hh + 1), a3 = codes128(k.w[i][1][j], 2 * hh + 1);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-              mma_bf16(x[nt][i], a0, a1, a2, a3, qf[nt][j][2 * hh], qf[nt][j][2 * hh + 1]);
+            for (int j = 0; j < 4; ++j) {
+              y[2 * j] = __uint_as_float(x[j] << 16);
+              y[2 * j + 1] = __uint_as_float(x[j] & 0xffff0000u);
+              sum += y[2 * j] + y[2 * j + 1];
+            }
+            const float f2 = f * 0.0625f;
+            const uint4 v = make_uint4(pack_f16(y[0] * f, y[4] * f), pack_f16(y[1] * f2, y[5] * f2),
+                                       pack_f16(y[2] * f, y[6] * f), pack_f16(y[3] * f2, y[7] * f2));
+            if constexpr (kQShared) {
+              q_shared[(i * NT + nt) * 32] = v;  // (read by the lane that writes it)
+            } else {
+              qf[nt][i][0] = v.x, qf[nt][i][1] = v.y, qf[nt][i][2] = v.z, qf[nt][i][3] = v.w;
+            }
           }
+          sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+          sum *= p.scale_log2;
+          qsum[nt] = two(__shfl_sync(0xffffffffu, sum, 8 * t), __shfl_sync(0xffffffffu, sum, 8 * t + 4));
+#pragma unroll
+          for (int c = 0; c < 2; ++c) limit[nt][c] = s.sees + token_of(s.head0 + nt * 8 + 2 * t + c);
         }
       }
-      float ks[2][2], km[2][2], vs[2][2], vm[2][2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float2 kp = __half22float2(*reinterpret_cast<const __half2*>(&k.par[i][j]));
-          const float2 vp = __half22float2(*reinterpret_cast<const __half2*>(&v.par[i][j]));
-          ks[i][j] = kp.x * p.scale_log2;
-          km[i][j] = fmaf(-128.f, kp.x, kp.y);
-          vs[i][j] = vp.x;
-          vm[i][j] = fmaf(8.f, vp.x, vp.y);
-        }
-      uint32_t hi[NT][2][2], lo[NT][2][2];  // p s, transposed: rows g of the tile, keys 2t, 2t + 1 (+ 8)
-      const int key = u * kUnitKeys + g;
+      float o[NT][MT][4];
+      float mx[NT][2];
+      uint64_t l[NT], off[NT];  // sums of the weights, and of the weights times the values' minima
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        bool in[2][2][2];
-        float top[2] = {mx[nt][0], mx[nt][1]};
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < MT; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              in[i][j][c] = key + 16 * i + 8 * j < limit[nt][c];
-              float& y = x[nt][i][2 * j + c];
-              y = in[i][j][c] ? fmaf(ks[i][j], y, km[i][j] * qsum[nt][c]) : -INFINITY;
-              top[c] = fmaxf(top[c], y);
-            }
-        float alpha[2];
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 4));
-          top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 8));
-          top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 16));
-          const float safe = top[c] == -INFINITY ? 0.f : top[c];
-          alpha[c] = exp2_approx(mx[nt][c] - safe);
-          mx[nt][c] = top[c];
-          top[c] = safe;
-          l[nt][c] *= alpha[c];
-          off[nt][c] *= alpha[c];
-        }
-        if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
-#pragma unroll
-          for (int i = 0; i < MT; ++i) {
-            o[nt][i][0] *= alpha[0], o[nt][i][1] *= alpha[1];
-            o[nt][i][2] *= alpha[0], o[nt][i][3] *= alpha[1];
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            float ps[2];
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              const float e = exp2_approx(x[nt][i][2 * j + c] - top[c]);
-              l[nt][c] += e;
-              // what a row does not see may hold anything, in its parameters too
-              if (in[i][j][c]) off[nt][c] = fmaf(e, vm[i][j], off[nt][c]);
-              ps[c] = in[i][j][c] ? e * vs[i][j] : 0.f;
-            }
-            const uint32_t h2 = pack_bf16(ps[0], ps[1]);
-            const uint32_t l2 =
-                pack_bf16(ps[0] - __uint_as_float(h2 << 16), ps[1] - __uint_as_float(h2 & 0xffff0000u));
-            hi[nt][i][j] = transpose8x8(h2);
-            lo[nt][i][j] = transpose8x8(l2);
-          }
+        for (int c = 0; c < 2; ++c) mx[nt][c] = -INFINITY;
+        l[nt] = off[nt] = 0;
       }
+
+      for (;; ++u) {
+        if (!__all_sync(0xffffffffu, mbar_wait(&bar[stage], phase, p.timeout_ns))) {
+          if (lane == 0) set_status(p.status, kStatusTimeout);
+          dead = true;
+          break;
+        }
+        const uint8_t* st = ring + stage * kStage;
+        const int ok = s_meta[warp][stage].ok;
+
+        float x[NT][2][4];  // scores: [16 keys][key g row 2t, row 2t + 1, key g + 8 ...]
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < 2; ++i) {
+          uint32_t k0[KW], k1[KW];
+          load_words<KW>(k0, st + (16 * i + kg) * (D / 2) + t * (D / 8));
+          load_words<KW>(k1, st + (16 * i + 8 + kg) * (D / 2) + t * (D / 8));
 #pragma unroll
-        for (int y = 0; y < VW; ++y) {
+          for (int nt = 0; nt < NT; ++nt) x[nt][i][0] = x[nt][i][1] = x[nt][i][2] = x[nt][i][3] = 0.f;
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const uint32_t sel = half ? 0x7632u : 0x5410u;
-            const uint32_t w01 = __byte_perm(v.w[i][0][y], v.w[i][1][y], sel);
-            const uint32_t w23 = __byte_perm(v.w[i][2][y], v.w[i][3][y], sel);
+          for (int j = 0; j < KW; ++j) {
 #pragma unroll
-            for (int z = 0; z < 2; ++z) {
-              const uint32_t a0 = codes8(w01, 2 * z), a1 = codes8(w01, 2 * z + 1);
-              const uint32_t a2 = codes8(w23, 2 * z), a3 = codes8(w23, 2 * z + 1);
-              const int mt = 4 * y + 2 * half + z;  // channels D/8 g + 2 mt (rows g), + 1 (rows g + 8)
+            for (int hh = 0; hh < 2; ++hh) {
+              const uint32_t y0 = hh ? k0[j] >> 8 : k0[j], y1 = hh ? k1[j] >> 8 : k1[j];
+              const uint32_t a0 = nib_lo(y0), a1 = nib_lo(y1), a2 = nib_hi(y0), a3 = nib_hi(y1);
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) {
-                mma_bf16(o[nt][mt], a0, a1, a2, a3, hi[nt][i][0], hi[nt][i][1]);
-                mma_bf16(o[nt][mt], a0, a1, a2, a3, lo[nt][i][0], lo[nt][i][1]);
+                if constexpr (kQShared) {
+                  const uint2 b = *(reinterpret_cast<const uint2*>(q_shared + (j * NT + nt) * 32) + hh);
+                  mma_f16(x[nt][i], a0, a1, a2, a3, b.x, b.y);
+                } else {
+                  mma_f16(x[nt][i], a0, a1, a2, a3, qf[nt][j][2 * hh], qf[nt][j][2 * hh + 1]);
+                }
               }
             }
           }
         }
-      }
-    }
-
-    // join the warps: sums to shared memory as (row, channel)
+        float ks[2][2], km[2][2], vs[2][2], vm[2][2], vl[2][2];
+        const __half2* kp = reinterpret_cast<const __half2*>(st + 2 * kCodes);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-#pragma unroll
-        for (int d = 4; d < 32; d <<= 1) {
-          l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], d);
-          off[nt][c] += __shfl_xor_sync(0xffffffffu, off[nt][c], d);
-        }
-        const int r = nt * 8 + 2 * t + c;
-        float* dst = s_o + (warp * R + r) * D + g * (D / 8);
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-          *reinterpret_cast<float2*>(dst + 2 * mt) = make_float2(o[nt][mt][c] + off[nt][c], o[nt][mt][2 + c] + off[nt][c]);
-        if (g == 0) s_stat[warp * R + r] = make_float4(mx[nt][c], l[nt][c], 0.f, 0.f);
-      }
-    }
-    __syncthreads();
-    const bool whole = s.u0 == 0 && s.u1 == s.units;
-    // CTAs of the segment: the first of them counts the arrivals
-    const int64_t first = whole ? blockIdx.x : owner_of(seg0, total, ctas);
-    const int64_t last = whole ? blockIdx.x : owner_of(seg0 + s.units - 1, total, ctas);
-    const int64_t slot = (int64_t)blockIdx.x * 2 + (s.u0 > 0 ? 0 : 1);
-    constexpr int kPart = D + 4;
-    for (int i = tid; i < rows * (D / 4); i += kThreads) {
-      const int r = i / (D / 4), d = i % (D / 4) * 4;
-      float m = -INFINITY;
-#pragma unroll
-      for (int k = 0; k < kWarps; ++k) m = fmaxf(m, s_stat[k * R + r].x);
-      const float safe = m == -INFINITY ? 0.f : m;
-      float sum = 0.f;
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int k = 0; k < kWarps; ++k) {
-        const float4 st = s_stat[k * R + r];
-        const float f = exp2_approx(st.x - safe);
-        const float4 a = *reinterpret_cast<const float4*>(s_o + (k * R + r) * D + d);
-        sum = fmaf(st.y, f, sum);
-        acc.x = fmaf(a.x, f, acc.x), acc.y = fmaf(a.y, f, acc.y);
-        acc.z = fmaf(a.z, f, acc.z), acc.w = fmaf(a.w, f, acc.w);
-      }
-      if (whole) {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        const int row = s.row0 + r;
-        uint16_t* dst = p.out + (q0 + row / p.group) * p.out_stride + (int64_t)(s.h * p.group + row % p.group) * D + d;
-        *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-      } else {
-        float* dst = p.part + (slot * R + r) * kPart;
-        __stcg(reinterpret_cast<float4*>(dst + d), acc);
-        if (d == 0) __stcg(reinterpret_cast<float4*>(dst + D), make_float4(m, sum, 0.f, 0.f));
-      }
-    }
-    if (!whole) {
-      __threadfence();
-      __syncthreads();
-      if (tid == 0) s_last = atomicAdd(&p.cnt[first], 1) == (int)(last - first) ? 1 : 0;
-      __syncthreads();
-      if (s_last) {
-        __threadfence();
-        const int n = (int)(last - first) + 1;
-        // a thread per (row, four channels): two passes over the parts, maxima first
-        for (int i = tid; i < rows * (D / 4); i += kThreads) {
-          const int r = i / (D / 4), d = i % (D / 4) * 4;
-          auto part = [&](int k) { return p.part + (((first + k) * 2 + (k == 0 ? 1 : 0)) * R + r) * kPart; };
-          float m = -INFINITY;
-#pragma unroll 4
-          for (int k = 0; k < n; ++k) m = fmaxf(m, __ldcg(part(k) + D));
-          const float safe = m == -INFINITY ? 0.f : m;
-          float sum = 0.f;
-          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-          for (int k = 0; k < n; ++k) {
-            const float* src = part(k);
-            const float2 st = __ldcg(reinterpret_cast<const float2*>(src + D));
-            const float4 a = __ldcg(reinterpret_cast<const float4*>(src + d));
-            const float f = exp2_approx(st.x - safe);
-            sum = fmaf(st.y, f, sum);
-            acc.x = fmaf(a.x, f, acc.x), acc.y = fmaf(a.y, f, acc.y);
-            acc.z = fmaf(a.z, f, acc.z), acc.w = fmaf(a.w, f, acc.w);
+          for (int j = 0; j < 2; ++j) {
+            const float2 a = __half22float2(kp[16 * i + 8 * j + kg]);
+            const float2 v = __half22float2(kp[kUnitKeys + 16 * i + 8 * j + kg]);
+            ks[i][j] = a.x * rs, km[i][j] = a.y;
+            vs[i][j] = v.x, vm[i][j] = v.y;
+            vl[i][j] = lg2(fmaxf(v.x, 1.f / kLo));
           }
-          const float inv = sum == 0.f ? 0.f : 1.f / sum;
-          const int row = s.row0 + r;
-          uint16_t* dst = p.out + (q0 + row / p.group) * p.out_stride + (int64_t)(s.h * p.group + row % p.group) * D + d;
-          *reinterpret_cast<uint2*>(dst) =
-              make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              float *y = &x[nt][i][2 * j], k2 = ks[i][j], m2 = km[i][j];
+              apart(fma2(two(y[0], y[1]), two(k2, k2), mul2(two(m2, m2), qsum[nt])), y[0], y[1]);
+            }
+        const bool edge = (u + 1) * kUnitKeys > s.sees || ok != 3;  // some row does not see all of the unit
+        if (edge) {
+          const int key = u * kUnitKeys + kg;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (key + 16 * i + 8 * (j >> 1) >= limit[nt][j & 1] || !(ok >> i & 1)) x[nt][i][j] = -INFINITY;
         }
-        if (tid == 0) atomicExch(&p.cnt[first], 0);
+        uint32_t pt[NT][2][2];  // weights, transposed: query row g, keys 2t, 2t + 1 of eight
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              float a, b;
+              apart(add2(two(x[nt][i][2 * j], x[nt][i][2 * j + 1]), two(vl[i][j], vl[i][j])), a, b);
+              top[0] = fmaxf(top[0], a), top[1] = fmaxf(top[1], b);
+            }
+          if (__any_sync(0xffffffffu, top[0] > mx[nt][0] + 8.f || top[1] > mx[nt][1] + 8.f)) {
+            float alpha[2];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 4));
+              top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 8));
+              top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 16));
+              top[c] = fmaxf(top[c], mx[nt][c]);
+              alpha[c] = mx[nt][c] == -INFINITY ? 0.f : ex2(mx[nt][c] - top[c]);
+              mx[nt][c] = top[c];
+            }
+            const uint64_t a2 = two(alpha[0], alpha[1]);
+            l[nt] = mul2(l[nt], a2);
+            off[nt] = mul2(off[nt], a2);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+              apart(mul2(two(o[nt][i][0], o[nt][i][1]), a2), o[nt][i][0], o[nt][i][1]);
+              apart(mul2(two(o[nt][i][2], o[nt][i][3]), a2), o[nt][i][2], o[nt][i][3]);
+            }
+          }
+          const uint64_t m2 = two(mx[nt][0] == -INFINITY ? 0.f : -mx[nt][0], mx[nt][1] == -INFINITY ? 0.f : -mx[nt][1]);
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              float a, b;
+              apart(add2(two(x[nt][i][2 * j], x[nt][i][2 * j + 1]), m2), a, b);
+              const uint64_t e = two(ex2(a), ex2(b));
+              l[nt] = add2(l[nt], e);
+              uint64_t om = mul2(e, two(vm[i][j], vm[i][j])), os = mul2(e, two(vs[i][j], vs[i][j]));
+              if (edge) {  // what a row does not see may hold anything, in its parameters too
+                float m0, m1, s0, s1;
+                apart(om, m0, m1);
+                apart(os, s0, s1);
+                if (a == -INFINITY) m0 = s0 = 0.f;
+                if (b == -INFINITY) m1 = s1 = 0.f;
+                om = two(m0, m1);
+                os = two(s0, s1);
+              }
+              off[nt] = add2(off[nt], om);
+              apart(os, a, b);
+              pt[nt][i][j] = transpose8x8(pack_f16(a, b));
+            }
+        }
+        const uint8_t* vc = st + kCodes + g * (D / 16);
+        const int v0 = 2 * t ^ (t & 1), v1 = (2 * t + 1) ^ (t & 1);  // keys of operand columns 2t, 2t + 1
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint32_t v[4][VW];
+          load_words<VW>(v[0], vc + (16 * i + v0) * (D / 2));
+          load_words<VW>(v[1], vc + (16 * i + v1) * (D / 2));
+          load_words<VW>(v[2], vc + (16 * i + 8 + v0) * (D / 2));
+          load_words<VW>(v[3], vc + (16 * i + 8 + v1) * (D / 2));
+#pragma unroll
+          for (int y = 0; y < VW; ++y) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              const uint32_t sel = half ? 0x7632u : 0x5410u;
+              const uint32_t w01 = __byte_perm(v[0][y], v[1][y], sel), w23 = __byte_perm(v[2][y], v[3][y], sel);
+#pragma unroll
+              for (int z = 0; z < 2; ++z) {
+                const uint32_t y01 = z ? w01 >> 8 : w01, y23 = z ? w23 >> 8 : w23;
+                const uint32_t a0 = nib_lo(y01), a1 = nib_hi(y01), a2 = nib_lo(y23), a3 = nib_hi(y23);
+                const int mt = 4 * y + 2 * half + z;  // channels D/8 g + 2 mt (rows g), + 1 (rows g + 8)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][mt], a0, a1, a2, a3, pt[nt][i][0], pt[nt][i][1]);
+              }
+            }
+          }
+        }
+        __syncwarp();  // the stage has been read
+        --pending;
+        issue();
+        __syncwarp();
+        if (++stage == S) {
+          stage = 0;
+          phase ^= 1u;
+        }
+        if (pending == 0 || s_meta[warp][stage].opens) break;
+      }
+
+      // the segment's sums: to `out` if the warp held all of it, else to shared memory
+      const bool first = u0 > 0, last = u < s.seen - 1;
+      if (!dead) {
+        float* dst = reinterpret_cast<float*>(last ? ring : ring + kFirst);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) {
+            l[nt] = add2(l[nt], __shfl_xor_sync(0xffffffffu, l[nt], d));
+            off[nt] = add2(off[nt], __shfl_xor_sync(0xffffffffu, off[nt], d));
+          }
+          float ls[2], as[2];
+          apart(l[nt], ls[0], ls[1]);
+          apart(off[nt], as[0], as[1]);
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const int r = nt * 8 + 2 * t + c;
+            if (r >= s.rows) continue;
+            if (!first && !last) {
+              const float inv = ls[c] == 0.f ? 0.f : 1.f / ls[c];
+              uint16_t* y = q_row(s.q0, s.h, s.head0, r, p.out, p.out_stride) + g * (D / 8);
+#pragma unroll
+              for (int mt = 0; mt < MT; mt += 4) {
+                uint32_t v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  v[i] = pack_bf16(fmaf(o[nt][mt + i][c], kLo, as[c]) * inv, fmaf(o[nt][mt + i][2 + c], kHi, as[c]) * inv);
+                *reinterpret_cast<uint4*>(y + 2 * mt) = make_uint4(v[0], v[1], v[2], v[3]);
+              }
+            } else {
+              float* y = dst + r * kRow + g * (D / 8);
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt)
+                *reinterpret_cast<float2*>(y + 2 * mt) =
+                    make_float2(fmaf(o[nt][mt][c], kLo, as[c]), fmaf(o[nt][mt][2 + c], kHi, as[c]));
+              if (g == 0) *reinterpret_cast<float2*>(dst + r * kRow + D) = make_float2(mx[nt][c], ls[c]);
+            }
+          }
+        }
+        if ((first || last) && lane == 0) s_info[warp][last ? 1 : 0] = PartInfo{s.vis0, s.seen, s.rows, s.h, s.q0, s.head0};
       }
     }
-    __syncthreads();  // shared memory is free for the next segment
+    for (; dead && pending > 0; --pending) {  // the copies that are still on their way
+      mbar_wait(&bar[stage], phase, p.timeout_ns);
+      if (++stage == S) {
+        stage = 0;
+        phase ^= 1u;
+      }
+    }
   }
+
+  // ------------------------------------------------------------------ segments shared by warps
+  __syncthreads();
+  if (warp == 0) {  // the parts in order, and the rows of the segments that begin among them
+    const PartInfo mine = lane < 2 * W ? s_info[lane >> 1][lane & 1] : PartInfo{};
+    const unsigned m = __ballot_sync(0xffffffffu, mine.rows > 0), below = m & ((1u << lane) - 1u);
+    const int prev = __shfl_sync(0xffffffffu, mine.vis0, below ? 31 - __clz(below) : 0);
+    const bool opens = mine.rows > 0 && (below == 0 || prev != mine.vis0);
+    int rows = opens ? mine.rows : 0;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, rows, d);
+      if (lane >= d) rows += x;
+    }
+    if (mine.rows > 0) {
+      const int at = __popc(below);
+      s_order[at] = lane;
+      s_row0[at] = opens ? rows - mine.rows : -1;
+    }
+    if (lane == 31) s_parts = __popc(m), s_rows = rows;
+  }
+  __syncthreads();
+  constexpr int C = D / 32;  // channels of a lane
+  auto write_out = [&](const PartInfo& s, int r, const Row<C>& x) {
+    const float inv = x.sum == 0.f ? 0.f : 1.f / x.sum;
+    uint16_t* dst = q_row(s.q0, s.h, s.head0, r, p.out, p.out_stride) + lane * C;
+#pragma unroll
+    for (int c = 0; c < C; c += 2)
+      *reinterpret_cast<uint32_t*>(dst + c) = pack_bf16(x.acc[c] * inv, x.acc[c + 1] * inv);
+  };
+  const int parts = s_parts;
+  int open[2] = {-1, -1};  // a part of the segment shared with the CTAs before, after
+  if (parts > 0) {
+    const int i = s_order[0], j = s_order[parts - 1];
+    const PartInfo a = s_info[i >> 1][i & 1], b = s_info[j >> 1][j & 1];
+    if (a.vis0 < c0) open[0] = i;
+    if (b.vis0 >= c0 && b.vis0 + b.seen > c1) open[1] = j;
+  }
+  const int own0 = lane < parts ? s_row0[lane] : -1;
+  for (int x = warp; x < s_rows; x += W) {
+    const unsigned m = __ballot_sync(0xffffffffu, own0 >= 0 && own0 <= x);
+    const int i = 31 - __clz(m);  // the segment's first part
+    const unsigned after = __ballot_sync(0xffffffffu, own0 >= 0) & ~((2u << i) - 1u);
+    const int n = (after ? __ffs(after) - 1 : parts) - i;
+    const int r = x - __shfl_sync(0xffffffffu, own0, i);
+    const PartInfo s = s_info[s_order[i] >> 1][s_order[i] & 1];
+    auto at = [&](int k) {
+      const int o = s_order[i + k];
+      return reinterpret_cast<const float*>(smem + (o >> 1) * kWarpBytes + ((o & 1) ? 0 : kFirst)) + r * kRow;
+    };
+    const Row<C> y = join<C>(
+        n, [&](int k) { return *reinterpret_cast<const float2*>(at(k) + D); },
+        [&](int k) {
+          const float* src = at(k) + lane * C;
+          Row<C> a;
+#pragma unroll
+          for (int c = 0; c < C; ++c) a.acc[c] = src[c];
+          return a;
+        });
+    if (s.vis0 >= c0 && s.vis0 + s.seen <= c1) {
+      write_out(s, r, y);
+    } else {
+      float* part = p.part + (((int64_t)blockIdx.x * 2 + (s.vis0 < c0 ? 0 : 1)) * R + r) * kRow;
+#pragma unroll
+      for (int c = 0; c < C; ++c) __stcg(part + lane * C + c, y.acc[c]);
+      if (lane == 0) __stcg(reinterpret_cast<float2*>(part + D), make_float2(y.m, y.sum));
+    }
+  }
+  // ------------------------------------------------------------------ segments shared by CTAs
+  if (open[0] < 0 && open[1] < 0) return;
+  __threadfence();
+  __syncthreads();
+  auto ctas_of = [&](int which, int& f, int& e) {
+    const PartInfo s = s_info[open[which] >> 1][open[which] & 1];
+    f = by_cta.owner(s.vis0);
+    e = by_cta.owner(s.vis0 + s.seen - 1);
+  };
+  if (tid < 2) {
+    s_last[tid] = 0;
+    if ((tid == 0 ? open[0] : open[1]) >= 0) {
+      int f, e;
+      ctas_of(tid, f, e);
+      s_last[tid] = atomicAdd(&p.cnt[f], 1) == e - f ? 1 : 0;
+    }
+  }
+  __syncthreads();
+  if (!s_last[0] && !s_last[1]) return;
+  __threadfence();
+  PartInfo s[2];
+  int f[2], e[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    s[i].rows = 0;
+    if (s_last[i]) {
+      s[i] = s_info[open[i] >> 1][open[i] & 1];
+      ctas_of(i, f[i], e[i]);
+    }
+  }
+  for (int x = warp; x < s[0].rows + s[1].rows; x += W) {
+    const int i = x < s[0].rows ? 0 : 1, r = x - (i ? s[0].rows : 0);
+    const int first = i ? f[1] : f[0], n = (i ? e[1] : e[0]) - first + 1;
+    // the segment is the first CTA's second part and the others' first
+    auto at = [&](int k) { return p.part + (((int64_t)(first + k) * 2 + (k == 0 ? 1 : 0)) * R + r) * kRow; };
+    const Row<C> y = join<C>(
+        n, [&](int k) { return __ldcg(reinterpret_cast<const float2*>(at(k) + D)); },
+        [&](int k) {
+          const float2* src = reinterpret_cast<const float2*>(at(k) + lane * C);
+          Row<C> a;
+#pragma unroll
+          for (int c = 0; c < C / 2; ++c) {
+            const float2 v = __ldcg(src + c);
+            a.acc[2 * c] = v.x, a.acc[2 * c + 1] = v.y;
+          }
+          return a;
+        });
+    write_out(i ? s[1] : s[0], r, y);
+  }
+  if (tid < 2 && s_last[tid]) atomicExch(&p.cnt[tid ? f[1] : f[0]], 0);
 }
 
 template <int D, int NT>
 constexpr size_t smem_bytes() {
-  return (size_t)kWarps * 8 * NT * (D + 4) * sizeof(float);
+  return (size_t)warps_of(D, NT) * (stages_of(D, NT) * (kUnitKeys * D + 2 * kUnitKeys * 4) +
+                                    (queries_shared(D, NT) ? 32 * NT * (D / 32) * 16 : 0) + 8 * NT * (D + 4) * 4);
 }
 
 // CTAs of a full grid; 0 if a lookup failed.
@@ -505,28 +842,25 @@ int grid_of() {
     int n = 0;
     if (cudaFuncSetAttribute(attend_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              (int)smem_bytes<D, NT>()) != cudaSuccess ||
-        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, attend_kernel<D, NT>, kThreads, smem_bytes<D, NT>()) !=
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, attend_kernel<D, NT>, 32 * warps_of(D, NT),
+                                                      smem_bytes<D, NT>()) !=
             cudaSuccess) {
       cudaGetLastError();
       return 0;
     }
-    return n * sms;
+    return n > 0 ? sms : 0;  // one CTA per SM
   });
 }
 
-constexpr int kMaxCtasPerSm = 4;
-
 size_t workspace_bytes(int head_dim, int sms) {
-  const size_t ctas = (size_t)kMaxCtasPerSm * sms;
-  return ws_counter_bytes(sms) + ctas * 2 * kRowTile * (size_t)(head_dim + 4) * sizeof(float);
+  return ws_counter_bytes(sms) + (size_t)sms * 2 * kRowTile * (size_t)(head_dim + 4) * sizeof(float);
 }
 
 template <int D, int NT>
 sp_status launch(AttendParams p, cudaStream_t stream) {
   const int ctas = grid_of<D, NT>();
   if (ctas == 0) return SP_ERR_CUDA;
-  return launch_pdl(attend_kernel<D, NT>, dim3((unsigned)std::min(ctas, kMaxCtasPerSm * current_sms())), kThreads,
-                    smem_bytes<D, NT>(), 1, stream, p);
+  return launch_pdl(attend_kernel<D, NT>, dim3((unsigned)ctas), 32 * warps_of(D, NT), smem_bytes<D, NT>(), 1, stream, p);
 }
 
 }  // namespace
@@ -576,12 +910,14 @@ sp_status sp_kv4_attend(const sp_attend_args* a, void* workspace_dev, size_t wor
   p.requests = a->requests;
   p.width = a->width;
   p.group = a->heads / kv;
+  p.group_inverse = (65536 + p.group - 1) / p.group;
   p.max_new = a->max_new;
   p.tokens = a->tokens;
   p.scale_log2 = a->scale * 1.4426950408889634f;
   p.cnt = static_cast<int*>(workspace_dev);
   p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace_dev) + ws_counter_bytes(sms));
   p.status = device_status_ptr();
+  p.timeout_ns = wait_timeout_ns();
   const int64_t rows = std::min<int64_t>((int64_t)a->max_new * p.group, kRowTile);
   const int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
   cudaStream_t s = (cudaStream_t)stream;

@@ -12,6 +12,7 @@ namespace sp {
 constexpr int kMaxGroup = 64;       // query heads per key head
 constexpr int kUnitKeys = 32;       // keys of one step of attend_kernel
 constexpr int kRowTile = 32;        // query rows (token, head of the group) of its widest form
+constexpr int kSetupUnits = 1;      // what a segment costs beside its units, in units
 
 struct Kv4 {
   uint8_t* data;

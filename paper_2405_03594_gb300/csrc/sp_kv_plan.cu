@@ -40,10 +40,11 @@ __device__ __forceinline__ Request request_at(const sp_kv_plan_args& a, int shif
   return r;
 }
 
-// Shares of the attention kernel: units of kUnitKeys keys for every tile of kRowTile query rows.
+// Shares of the attention kernel: for every tile of kRowTile query rows, units of kUnitKeys keys and what
+// a tile costs beside them.
 __device__ __forceinline__ int64_t units_of(const Request& r, int group) {
   if (r.add == 0) return 0;
-  return (r.add * group + kRowTile - 1) / kRowTile * ((r.len + kUnitKeys - 1) / kUnitKeys);
+  return (r.add * group + kRowTile - 1) / kRowTile * ((r.len + kUnitKeys - 1) / kUnitKeys + kSetupUnits);
 }
 
 // f(j) for j in [0, n) of each lane's own n: long ranges by the whole warp, one after the other.
