@@ -27,7 +27,7 @@
 #include <algorithm>
 #include <climits>
 
-#include "sp_kv4.cuh"
+#include "sp_attend.cuh"
 #include "sp_lookup.h"
 
 namespace sp {
@@ -42,28 +42,6 @@ constexpr int warps_of(int d, int nt) { return nt == 1 ? 16 : nt == 2 ? (d == 64
 constexpr int stages_of(int d, int nt) { return d == 64 ? 4 : nt == 1 ? 2 : nt == 2 ? 4 : 3; }
 constexpr bool queries_shared(int d, int nt) { return nt == 4; }
 
-struct AttendParams {
-  const uint16_t* q;
-  uint16_t* out;
-  int64_t q_stride, out_stride;
-  Kv4 cache;
-  const int32_t *table, *lens, *cu_q, *work;
-  int32_t requests, width, group;
-  int32_t max_new;
-  int64_t tokens;
-  int32_t group_inverse;  // 2^16 / group, rounded up
-  float scale_log2;
-  float* part;  // [2 grid][8 NT] of (D sums, maximum, sum of weights, unused)
-  int* cnt;     // [grid]
-  int32_t* status;
-  uint64_t timeout_ns;
-};
-
-__device__ __forceinline__ float ex2(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
 __device__ __forceinline__ float lg2(float x) {
   float r;
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -80,45 +58,10 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
   return r;
 }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
 // fp16 pairs of the nibbles i and i + 4 of w: n 2^-24 for i = 0 (and 2, of w >> 8), n 2^-20 for i = 1 (3)
 __device__ __forceinline__ uint32_t nib_lo(uint32_t w) { return w & 0x000f000fu; }
 __device__ __forceinline__ uint32_t nib_hi(uint32_t w) { return w & 0x00f000f0u; }
 constexpr float kLo = 16777216.f, kHi = 1048576.f;
-
-// Two fp32 numbers in one register pair, and arithmetic on both at once.
-__device__ __forceinline__ uint64_t two(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ void apart(uint64_t x, float& a, float& b) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x));
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
 
 template <int W>
 __device__ __forceinline__ void load_words(uint32_t (&d)[W], const uint8_t* p) {
@@ -442,7 +385,10 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
           for (int i = 0; i < KW; ++i) {
             const uint32_t x[4] = {x4[i].x, x4[i].y, x4[i].z, x4[i].w};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) big = max(big, max(x[j] & 0x7fffu, (x[j] >> 16) & 0x7fffu));
+            for (int j = 0; j < 8; ++j) {  // (an infinity or NaN is its own row's matter)
+              const uint32_t y = (x[j >> 1] >> (16 * (j & 1))) & 0x7fffu;
+              big = max(big, y < 0x7f80u ? y : 0u);
+            }
           }
         }
         // 2^(141 - e): the largest entry, of biased exponent e, comes to 2^14 ... 2^15
@@ -918,9 +864,14 @@ sp_status sp_kv4_attend(const sp_attend_args* a, void* workspace_dev, size_t wor
   p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace_dev) + ws_counter_bytes(sms));
   p.status = device_status_ptr();
   p.timeout_ns = wait_timeout_ns();
-  const int64_t rows = std::min<int64_t>((int64_t)a->max_new * p.group, kRowTile);
-  const int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
   cudaStream_t s = (cudaStream_t)stream;
+  const int64_t most = (int64_t)a->max_new * p.group;
+  if (most >= kManyRows) {
+    const sp_status st = launch_attend_rows(p, d, s);
+    if (st != SP_OK) return st;
+  }
+  const int64_t rows = std::min<int64_t>(most, kRowTile);
+  const int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
   if (d == 64) return nt == 1 ? launch<64, 1>(p, s) : nt == 2 ? launch<64, 2>(p, s) : launch<64, 4>(p, s);
   return nt == 1 ? launch<128, 1>(p, s) : nt == 2 ? launch<128, 2>(p, s) : launch<128, 4>(p, s);
 }

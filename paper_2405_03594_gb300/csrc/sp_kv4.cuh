@@ -12,6 +12,8 @@ namespace sp {
 constexpr int kMaxGroup = 64;       // query heads per key head
 constexpr int kUnitKeys = 32;       // keys of one step of attend_kernel
 constexpr int kRowTile = 32;        // query rows (token, head of the group) of its widest form
+constexpr int kManyRows = 65;       // query rows of a request from which attend_rows_kernel takes it
+constexpr int kPairRows = 256;      // query rows of one of its items
 constexpr int kSetupUnits = 1;      // what a segment costs beside its units, in units
 
 struct Kv4 {

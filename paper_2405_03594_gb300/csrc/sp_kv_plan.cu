@@ -43,8 +43,13 @@ __device__ __forceinline__ Request request_at(const sp_kv_plan_args& a, int shif
 // Shares of the attention kernel: for every tile of kRowTile query rows, units of kUnitKeys keys and what
 // a tile costs beside them.
 __device__ __forceinline__ int64_t units_of(const Request& r, int group) {
-  if (r.add == 0) return 0;
+  if (r.add == 0 || r.add * group >= kManyRows) return 0;
   return (r.add * group + kRowTile - 1) / kRowTile * ((r.len + kUnitKeys - 1) / kUnitKeys + kSetupUnits);
+}
+
+// Pairs of tiles of the kernel for many rows.
+__device__ __forceinline__ int64_t pairs_of(const Request& r, int group) {
+  return r.add * group >= kManyRows ? (r.add * group + kPairRows - 1) / kPairRows : 0;
 }
 
 // f(j) for j in [0, n) of each lane's own n: long ranges by the whole warp, one after the other.
@@ -87,7 +92,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
                                                             bool fill) {
   __shared__ int64_t s_sum[4];     // pages needed, pages given back, new tokens, units
   __shared__ int s_bad;
-  __shared__ int s_warp[32][4];
+  __shared__ int s_warp[32][5];
   __shared__ int32_t s_cu[kCuShared + 1];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait();
@@ -128,22 +133,23 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
     if (allocate) *a.next_count = bad ? (int32_t)height : (int32_t)(top - s_sum[0]);
     a.cu_q[0] = 0;
     a.work[0] = 0;
+    a.work[a.requests + 1] = 0;
     s_cu[0] = 0;
   }
-  int base[4];  // pages taken, pages given back, tokens, units of the chunks before
+  int base[5];  // pages taken, pages given back, tokens, units, pairs of the chunks before
   const bool one = a.requests <= kPlanThreads;
   for (int phase = s_sum[1] > 0 ? 0 : 1; phase < 2; ++phase) {
     // phase 0: pages given back; phase 1, behind a barrier: everything else
-    base[0] = base[1] = base[2] = base[3] = 0;
+    base[0] = base[1] = base[2] = base[3] = base[4] = 0;
     for (int b0 = 0; b0 < a.requests; b0 += kPlanThreads) {
       const int b = b0 + tid;
       Request r = {};
       if (b < a.requests && !bad) r = request_at(a, shift, b);
-      const int v[4] = {allocate && !r.gone ? (int)(r.after - r.before) : 0, allocate && r.gone ? (int)r.before : 0,
-                        (int)r.add, (int)units_of(r, a.group)};
-      int x[4];
+      const int v[5] = {allocate && !r.gone ? (int)(r.after - r.before) : 0, allocate && r.gone ? (int)r.before : 0,
+                        (int)r.add, (int)units_of(r, a.group), (int)pairs_of(r, a.group)};
+      int x[5];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < 5; ++k) {
         int s = v[k];
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -154,7 +160,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
         if (lane == 31) s_warp[warp][k] = s;
       }
       __syncthreads();
-      if (warp < 4) {  // a warp per quantity
+      if (warp < 5) {  // a warp per quantity
         int s = s_warp[lane][warp];
         const int own = s;
 #pragma unroll
@@ -167,7 +173,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
       }
       __syncthreads();
 #pragma unroll
-      for (int k = 0; k < 4; ++k) x[k] += base[k] + s_warp[warp][k];
+      for (int k = 0; k < 5; ++k) x[k] += base[k] + s_warp[warp][k];
       if (phase == 0) {
         each_page(v[1], ((int64_t)b << 32) | (uint32_t)x[1], [&](int64_t key, int j) {
           const int64_t rb = key >> 32;
@@ -185,6 +191,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
         if (b < a.requests) {
           a.cu_q[b + 1] = x[2] + v[2];
           a.work[b + 1] = x[3] + v[3];
+          a.work[a.requests + 2 + b] = x[4] + v[4];
           if (b < kCuShared) s_cu[b + 1] = x[2] + v[2];
         }
       }
@@ -192,11 +199,11 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
         __syncthreads();
         if (tid == kPlanThreads - 1) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) s_warp[0][k] = x[k] + v[k];
+          for (int k = 0; k < 5; ++k) s_warp[0][k] = x[k] + v[k];
         }
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) base[k] = s_warp[0][k];
+        for (int k = 0; k < 5; ++k) base[k] = s_warp[0][k];
         __syncthreads();
       }
     }
