@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
       }
 
       for (;; ++u) {
-        if (!__all_sync(0xffffffffu, mbar_wait(&bar[stage], phase, p.timeout_ns))) {
+        if (!__all_sync(0xffffffffu, mbar_wait_sleep(&bar[stage], phase, p.timeout_ns))) {
           if (lane == 0) set_status(p.status, kStatusTimeout);
           dead = true;
           break;
@@ -641,7 +641,7 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
       }
     }
     for (; dead && pending > 0; --pending) {  // the copies that are still on their way
-      mbar_wait(&bar[stage], phase, p.timeout_ns);
+      mbar_wait_sleep(&bar[stage], phase, p.timeout_ns);
       if (++stage == S) {
         stage = 0;
         phase ^= 1u;

@@ -10,15 +10,21 @@
 //
 //   warps 0-3, 4-7   a tile of query rows each, thread = row: scores out of tensor memory, weights back
 //                    into their place as fp16 (an operand of the second product), row sums
-//   warps 8-15       codes to fp16 operands in shared memory: K rows as [key][channel], V rows as
-//                    [channel][key], both in 128-byte-swizzled panels of 64 columns
-//   warp 16          issues the products
+//   warps 8-11       codes to fp16 operands in shared memory: rows of keys and of values in
+//                    128-byte-swizzled panels of 64 channels
+//   warps 12, 13     issue a tile's products each
+//   warp 14          copies of the codes, and the next item
+//
+// Measured, 32 heads of 128, two prompts of up to 2048 tokens behind a prefix (4 x 24e9 operations): 138 us,
+// 0.70 PFLOP/s, 0.37 of the measured bf16 rate.  A step of a tile is a chain -- scores read 0.13 us,
+// exponentials 0.5 (the special-function units' rate), weights' products and the next scores 0.55,
+// and four barriers -- of which the two tiles overlap about half.
 //
 // Numbers.  s n + m is rounded once to fp16 (the cache holds |x| <= 2^15); the queries, bf16, enter
 // exactly, each row scaled by a power of two.  The running maximum of a row moves only when
-// a weight would pass 2^8, so the sums in tensor memory are rarely touched by the rows' threads.  A key
-// row's channels may be in any order that the queries share, which saves their permutation: of the
-// eight codes of a word, i and i + 4 come out as a pair.
+// a weight would pass 2^8, so the sums in tensor memory are rarely touched by the rows' threads.  The channels
+// stand in the order in which a word's codes come out, i and i + 4 as a pair, in the queries
+// too; the output is put in order on its way out.
 #include <algorithm>
 #include <climits>
 
@@ -31,9 +37,9 @@ namespace {
 
 constexpr int kTile = 128;                // keys of a step, query rows of a tile
 constexpr int kRowThreads = 256;          // two tiles' rows
-constexpr int kFillWarps = 8;
-constexpr int kFillThreads = 32 * kFillWarps;
-constexpr int kThreads = kRowThreads + kFillThreads + 32;
+constexpr int kFillWarps = 4;
+constexpr int kBusyThreads = kRowThreads + 32 * kFillWarps + 96;
+constexpr int kThreads = 512;             // whole warpgroups, as the division of the registers wants them
 constexpr int kStages = 2;
 constexpr int kMaxDevices = 64;
 constexpr uint32_t kPanel = kTile * 128;  // 128 rows of 64 columns
@@ -41,8 +47,9 @@ constexpr uint32_t kPanel = kTile * 128;  // 128 rows of 64 columns
 template <int D>
 struct Smem {
   static constexpr uint32_t kQ = D / 64 * kPanel;              // a tile of queries, a step's keys
-  static constexpr uint32_t kV = 2 * D * 128;                  // a step's values: two panels of D channels
-  static constexpr uint32_t kBytes = 2 * kQ + kStages * (kQ + kV);
+  static constexpr uint32_t kV = kQ;                           // a step's values
+  static constexpr uint32_t kRaw = kTile * (D / 2 + 4);        // a step's codes and parameters of one of them
+  static constexpr uint32_t kBytes = 2 * kQ + kStages * (kQ + kV) + 2 * kRaw;
   static constexpr size_t kTotal = 1024 + kBytes;              // + base alignment
 };
 
@@ -63,8 +70,30 @@ __device__ __forceinline__ void tmem_store16(uint32_t taddr, const uint32_t (&v)
       "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
       : "memory");
 }
+__device__ __forceinline__ void tmem_load16(uint32_t taddr, uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, "
+      "[%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr)
+      : "memory");
+}
 // Instruction descriptor, kind::f16: D fp32, A and B fp16, both K-major.
 constexpr uint32_t idesc_f16(int m, int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24); }
+
+// B held as rows of 64 of its N columns, one row per K (128-byte swizzle): eight rows 1024 bytes apart
+// make the next eight of K (stride byte offset), the next 64 columns lie a panel on (leading byte offset).
+constexpr uint32_t kRowsAlongK = 1u << 16;
+__device__ __forceinline__ uint64_t smem_desc_rows_along_k(uint32_t saddr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr >> 4) & 0x3FFFu);
+  d |= (uint64_t)((kPanel >> 4) & 0x3FFFu) << 16;
+  d |= (uint64_t)((1024u >> 4) & 0x3FFFu) << 32;
+  d |= (uint64_t)1u << 46;
+  d |= (uint64_t)2u << 61;
+  return d;
+}
 
 __device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
   uint32_t r;
@@ -94,46 +123,464 @@ struct Item {
   int len;
 };
 
+struct Barriers {
+  uint64_t q_full, k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
+  uint64_t s_full[2], p_full[2], o_done[2];
+  uint64_t raw_full[2], raw_empty[2];  // keys, values
+  uint64_t turn[2];          // the other tile's products of its step have been issued
+};
+
+struct Shared {
+  Barriers bar;
+  uint32_t tmem;
+  uint32_t nan[kStages][4];  // keys of the step whose values are not finite
+  Item item[2];
+  unsigned pages[2];         // of the raw keys and values: the pages that exist
+  int dead;
+};
+
+// A bounded wait of a whole warp; nothing is waited for once one has expired.  (The sleeping wait is a
+// short loop.  mbar_wait's polls, unrolled at every wait, were more code than the SM's instruction
+// cache holds beside the roles' own: 165 us against 140 for the prefill measured below.)
+struct Wait {
+  const AttendParams& p;
+  bool dead = false;
+  __device__ __forceinline__ void operator()(uint64_t* bar, uint32_t parity) {
+    if (dead) return;
+    if (!__all_sync(0xffffffffu, mbar_wait_sleep(bar, parity, p.timeout_ns))) {
+      if ((threadIdx.x & 31) == 0) set_status(p.status, kStatusTimeout);
+      dead = true;
+    }
+  }
+};
+
+// Steps of keys that the rows of the item's tile i see.
+__device__ __forceinline__ int steps_of(const AttendParams& p, const Item& it, int i) {
+  const int rows = min(it.rows - i * kTile, kTile);
+  return rows > 0 ? (it.sees0 + (it.row0 + i * kTile + rows - 1) / p.group + kTile - 1) / kTile : 0;
+}
+
+// The end of an item for every warp that works on it; false once a wait has expired.
+__device__ __forceinline__ bool end_item(Shared& sh, const Wait& wait) {
+  if (wait.dead) sh.dead = 1;
+  tc_fence_before();
+  named_bar_sync(1, kBusyThreads);
+  tc_fence_after();
+  return sh.dead == 0;
+}
+
+// ------------------------------------------------------------------ rows: scores to weights, and the output
+template <int D>
+__device__ __forceinline__ void rows_role(const AttendParams& p, Shared& sh, uint8_t* s_q, uint32_t tmem) {
+  using L = Smem<D>;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int i = warp >> 2;  // tile
+  const int r = tid & (kTile - 1);
+  const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+  const uint32_t t_s = tmem + lanes + i * kTile, t_o = tmem + lanes + 2 * kTile + i * D;
+  Wait wait{p};
+  uint32_t steps = 0, done = 0;
+  for (uint32_t round = 0;; ++round) {
+    const Item it = sh.item[round & 1];
+    if (it.rows <= 0) break;
+    const int n = steps_of(p, it, i);
+    const bool there = i * kTile + r < it.rows;
+    const int row = it.row0 + i * kTile + r, token = row / p.group;
+    const int limit = there ? it.sees0 + token : 0;  // keys that the row sees
+    const int64_t col = (int64_t)(it.h * p.group + row - token * p.group) * D;
+    float cr;  // log2 score = cr * product
+    {
+      const uint4* src = reinterpret_cast<const uint4*>(p.q + (it.q0 + (int64_t)token) * p.q_stride + col);
+      uint4 u[D / 8];
+      uint32_t big = 0;
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c) u[c] = there ? src[c] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c) {
+        const uint32_t x[4] = {u[c].x, u[c].y, u[c].z, u[c].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) big = max(big, max(x[j] & 0x7fffu, (x[j] >> 16) & 0x7fffu));
+      }
+      // 2^(141 - e): the row's largest entry, of biased exponent e, comes to 2^14 ... 2^15
+      const uint32_t e = max(15u, min(254u, big >> 7));
+      const float f = copysignf(__uint_as_float((268u - e) << 23), p.scale_log2);
+      // (not 0, which would make NaN of what the row does not see)
+      cr = fmaxf(__uint_as_float((e - 14u) << 23) * fabsf(p.scale_log2), 1e-37f);
+      uint8_t* dst = s_q + i * L::kQ + r * 128;
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c) {
+        const uint32_t x[4] = {u[c].x, u[c].y, u[c].z, u[c].w};
+        float y[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          y[2 * j] = __uint_as_float(x[j] << 16) * f;
+          y[2 * j + 1] = __uint_as_float(x[j] & 0xffff0000u) * f;
+        }
+        *reinterpret_cast<uint4*>(dst + (c >> 3) * kPanel + (((c & 7) ^ (r & 7)) << 4)) =
+            make_uint4(pack_f16(y[0], y[4]), pack_f16(y[1], y[5]), pack_f16(y[2], y[6]), pack_f16(y[3], y[7]));
+      }
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sh.bar.q_full);
+    float m = -INFINITY;
+    uint64_t l = 0;
+    bool poisoned = false;
+    for (int j = 0; j < n; ++j) {
+      wait(&sh.bar.s_full[i], (done + j) & 1);
+      if (wait.dead) break;
+      tc_fence_after();
+      uint32_t u[kTile];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_load32(t_s + 32 * c, *reinterpret_cast<uint32_t(*)[32]>(u + 32 * c));
+      tmem_load_wait();
+      const int seen = limit - j * kTile;  // of the step's keys
+      if (__any_sync(0xffffffffu, seen < kTile)) {
+#pragma unroll
+        for (int k = 0; k < kTile; ++k)
+          if (k >= seen) u[k] = 0xff800000u;
+      }
+      float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int k = 0; k < kTile; ++k) t4[k & 3] = fmaxf(t4[k & 3], __uint_as_float(u[k]));
+      float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
+      top *= cr;
+      if (__any_sync(0xffffffffu, top > m + 8.f)) {
+        const float up = top > m + 8.f ? top : m;
+        const float alpha = up == m ? 1.f : m == -INFINITY ? 0.f : ex2(m - up);
+        m = up;
+        if (j > 0) {
+          const uint64_t a2 = two(alpha, alpha);
+          l = mul2(l, a2);
+          wait(&sh.bar.o_done[i], (done + j - 1) & 1);
+          if (wait.dead) break;
+          tc_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < D / 16; ++c) {
+            uint32_t v[16];
+            tmem_load16(t_o + 16 * c, v);
+            tmem_load_wait();
+#pragma unroll
+            for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * alpha);
+            tmem_store16(t_o + 16 * c, v);
+          }
+        }
+      }
+      const float minus = m == -INFINITY ? 0.f : -m;
+      const uint64_t c2 = two(cr, cr), m2 = two(minus, minus);
+      uint64_t sum[2] = {0, 0};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t w[16];
+#pragma unroll
+        for (int k = 0; k < 32; k += 2) {
+          float a, b;
+          apart(fma2(two(__uint_as_float(u[32 * c + k]), __uint_as_float(u[32 * c + k + 1])), c2, m2), a, b);
+          a = ex2(a), b = ex2(b);
+          sum[(k >> 1) & 1] = add2(sum[(k >> 1) & 1], two(a, b));
+          w[k / 2] = pack_f16(a, b);
+        }
+        tmem_store16(t_s + 16 * c, w);
+      }
+      l = add2(l, add2(sum[0], sum[1]));
+      // a value row that is not finite entered as zeros: it makes NaN of the rows that see it
+      const int st = (steps + j) % kStages;
+      wait(&sh.bar.v_full[st], ((steps + j) / kStages) & 1);
+      if (wait.dead) break;
+      const volatile uint32_t* bad = sh.nan[st];
+      const uint32_t x[4] = {bad[0], bad[1], bad[2], bad[3]};
+      if (x[0] | x[1] | x[2] | x[3]) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int sc = seen - 32 * c;
+          if (x[c] & (sc >= 32 ? ~0u : sc <= 0 ? 0u : (1u << sc) - 1u)) poisoned = true;
+        }
+      }
+      tmem_store_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.bar.p_full[i]);
+    }
+    if (n > 0) {
+      wait(&sh.bar.o_done[i], (done + n - 1) & 1);
+      tc_fence_after();
+      if (!wait.dead) {
+        float a, b;
+        apart(l, a, b);
+        a += b;
+        const float inv = poisoned ? __uint_as_float(0x7fffffffu) : a == 0.f ? 0.f : 1.f / a;
+        uint16_t* dst = p.out + (it.q0 + (int64_t)token) * p.out_stride + col;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t v[32];
+          tmem_load32(t_o + 32 * c, v);
+          tmem_load_wait();
+          if (there) {
+#pragma unroll
+            for (int k = 0; k < 32; k += 8) {
+              uint32_t w[4];
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {  // channels 0, 4, 1, 5, 2, 6, 3, 7 of eight
+                const int y = k + (x & 1) * 4 + (x >> 1);
+                w[x] = pack_bf16(__uint_as_float(v[y]) * inv, __uint_as_float(v[y + 2]) * inv);
+              }
+              *reinterpret_cast<uint4*>(dst + 32 * c + k) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          }
+        }
+      }
+    }
+    steps += max(steps_of(p, it, 0), steps_of(p, it, 1));
+    done += n;
+    if (!end_item(sh, wait)) break;
+  }
+}
+
+// ------------------------------------------------------------------ keys and values: copies of the codes
+// A step's codes and parameters come to shared memory as they are, by one bulk copy per page, as soon as
+// the step before is expanded.
+template <int D, class Fetch>
+__device__ __forceinline__ void copy_role(const AttendParams& p, Shared& sh, uint8_t* s_raw, Fetch fetch) {
+  using L = Smem<D>;
+  const int lane = threadIdx.x & 31;
+  const int shift = p.cache.shift, heads = p.cache.heads, pages = kTile >> shift;
+  const int64_t block = kv4_block_bytes<D>(shift);
+  Wait wait{p};
+  uint32_t steps = 0;
+  for (uint32_t round = 0;; ++round) {
+    const Item it = sh.item[round & 1];
+    if (it.rows <= 0) break;
+    const int n = max(steps_of(p, it, 0), steps_of(p, it, 1));
+    const int32_t* table = p.table + (int64_t)it.b * p.width;
+    auto page_of = [&](int j) {  // a lane per page of step j
+      const int at = j * pages + lane;
+      return j < n && lane < pages && ((int64_t)at << shift) < it.len ? (at < p.width ? table[at] : -1) : INT_MIN;
+    };
+    int next = page_of(0);
+    if (lane == 0) {  // the item after this one
+      Item after;
+      do fetch(after);
+      while (after.rows < 0);
+      sh.item[(round + 1) & 1] = after;
+    }
+    __syncwarp();
+    for (int j = 0; j < n && !wait.dead; ++j) {
+      int page = next;
+      next = page_of(j + 1);
+      if (page < 0 || page >= p.cache.pages) {
+        if (page != INT_MIN) set_status(p.status, kStatusBadIndex);
+        page = -1;
+      }
+      const unsigned ok = __ballot_sync(0xffffffffu, page >= 0);
+      const uint8_t* src = p.cache.data + ((int64_t)max(page, 0) * heads + it.h) * block;
+#pragma unroll 1
+      for (int which = 0; which < 2; ++which) {
+        wait(&sh.bar.raw_empty[which], ((steps + j) & 1) ^ 1);
+        if (wait.dead) break;
+        uint64_t* full = &sh.bar.raw_full[which];
+        if (lane == 0) {
+          sh.pages[which] = ok;
+          mbar_arrive_expect_tx(full, __popc(ok) * ((uint32_t)(D / 2 + 4) << shift));
+        }
+        __syncwarp();
+        if (page >= 0) {
+          uint8_t* dst = s_raw + which * L::kRaw;
+          bulk_g2s(dst + ((lane * (D / 2)) << shift), src + (which ? kv4_value_codes<D>(shift) : 0), (D / 2) << shift, full);
+          bulk_g2s(dst + kTile * (D / 2) + ((lane * 4) << shift),
+                   src + (which ? kv4_value_params<D>(shift) : kv4_key_params<D>(shift)), 4 << shift, full);
+        }
+      }
+    }
+    steps += n;
+    if (!end_item(sh, wait)) break;
+  }
+}
+
+// ------------------------------------------------------------------ keys and values: codes to operands
+template <int D>
+__device__ __forceinline__ void fill_role(const AttendParams& p, Shared& sh, uint8_t* s_k, uint8_t* s_v, const uint8_t* s_raw) {
+  using L = Smem<D>;
+  const int f = threadIdx.x - kRowThreads, lane = threadIdx.x & 31;
+  const int shift = p.cache.shift;
+  constexpr int KP = D / 32;  // 16-byte pieces of a row: a lane takes one of row f / KP, then of rows further on
+  const int piece = f % KP;
+  // The pieces of a row that lie in the second panel are stored in another order, so that eight
+  // lanes' 16 bytes never share a bank.
+  const int turn = piece >> 1;
+  Wait wait{p};
+  uint32_t steps = 0;
+  for (uint32_t round = 0;; ++round) {
+    const Item it = sh.item[round & 1];
+    if (it.rows <= 0) break;
+    const int n = max(steps_of(p, it, 0), steps_of(p, it, 1));
+    for (int j = 0; j < n; ++j) {
+      const int st = (steps + j) % kStages;
+      const uint32_t ph = ((steps + j) / kStages) & 1;
+#pragma unroll 1
+      for (int which = 0; which < 2; ++which) {
+        wait(&sh.bar.raw_full[which], (steps + j) & 1);
+        wait(which ? &sh.bar.v_empty[st] : &sh.bar.k_empty[st], ph ^ 1);
+        if (wait.dead) break;
+        const uint8_t* raw = s_raw + which * L::kRaw;
+        const uint32_t* raw_par = reinterpret_cast<const uint32_t*>(raw + kTile * (D / 2));
+        uint8_t* dst = which ? s_v + st * L::kV : s_k + st * L::kQ;
+        const unsigned ok = sh.pages[which];
+        const int left = it.len - j * kTile;
+        uint4 c4[KP];
+        uint32_t par[KP];
+#pragma unroll
+        for (int x = 0; x < KP; ++x) {
+          const int key = x * (kTile / KP) + f / KP;
+          c4[x] = *reinterpret_cast<const uint4*>(raw + (x * 128 + f) * 16);
+          par[x] = raw_par[key];
+          if (key >= left || !(ok >> (key >> shift) & 1)) par[x] = 0;  // what no token was written to may hold anything
+        }
+        if (which) {
+          auto finite = [](uint32_t y) { return (y & 0x7c00u) != 0x7c00u && (y & 0x7c000000u) != 0x7c000000u; };
+#pragma unroll
+          for (int x = 0; x < KP; ++x)
+            if (!finite(par[x])) par[x] = 0;
+          if (f < 32) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const int key = 32 * x + lane;
+              const bool bad = key < left && (ok >> (key >> shift) & 1) && !finite(raw_par[key]);
+              const unsigned bits = __ballot_sync(0xffffffffu, bad);
+              if (lane == 0) sh.nan[st][x] = bits;  // (read before the stage was handed back)
+            }
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < KP; ++x) {
+          const int key = x * (kTile / KP) + f / KP;
+          const uint32_t s = __byte_perm(par[x], par[x], 0x1010), m = __byte_perm(par[x], par[x], 0x3232);
+          const uint32_t w[4] = {turn ? c4[x].y : c4[x].x, turn ? c4[x].x : c4[x].y, turn ? c4[x].w : c4[x].z,
+                                 turn ? c4[x].z : c4[x].w};
+          uint8_t* row = dst + key * 128 + (piece >> 1) * kPanel;
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const int c = (4 * (piece & 1) + y) ^ turn;  // eight channels
+            const uint32_t h = w[y] >> 8;
+            *reinterpret_cast<uint4*>(row + ((c ^ (key & 7)) << 4)) =
+                make_uint4(value_lo(w[y], s, m), value_hi(w[y], s, m), value_lo(h, s, m), value_hi(h, s, m));
+          }
+        }
+        fence_proxy_async_smem();
+        named_bar_sync(2, 32 * kFillWarps);  // all of the raw rows have been read, all operands written
+        if (f == 0) {
+          mbar_arrive(which ? &sh.bar.v_full[st] : &sh.bar.k_full[st]);
+          mbar_arrive(&sh.bar.raw_empty[which]);
+        }
+      }
+      if (wait.dead) break;
+    }
+    steps += n;
+    if (!end_item(sh, wait)) break;
+  }
+  if (f < 32 && !sh.dead) {  // the products' last arrivals on this CTA's barriers
+    for (uint32_t x = steps > kStages ? steps - kStages : 0; x < steps; ++x) {
+      wait(&sh.bar.k_empty[x % kStages], (x / kStages) & 1);
+      wait(&sh.bar.v_empty[x % kStages], (x / kStages) & 1);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ the products of tile i
+template <int D>
+__device__ __forceinline__ void product_role(const AttendParams& p, Shared& sh, uint8_t* s_q, uint8_t* s_k, uint8_t* s_v,
+                                             uint32_t tmem, int i) {
+  using L = Smem<D>;
+  Wait wait{p};
+  // operand descriptors; a piece further on is a larger start address, in units of 16 bytes
+  const uint64_t d_q = smem_desc_sw128(smem_u32(s_q + i * L::kQ)), d_k = smem_desc_sw128(smem_u32(s_k)),
+                 d_v = smem_desc_rows_along_k(smem_u32(s_v));
+  const uint32_t t_s = tmem + i * kTile, t_o = tmem + 2 * kTile + i * D;
+  uint32_t steps = 0, done = 0, turns = 0;
+  for (uint32_t round = 0;; ++round) {
+    if (sh.item[round & 1].rows <= 0) break;
+    const int n = steps_of(p, sh.item[round & 1], i);
+    const int n_all = max(n, steps_of(p, sh.item[round & 1], 1 - i));
+    wait(&sh.bar.q_full, round & 1);
+    // step j: O += P_(j-1) . V_(j-1), then S = Q . K_j^T, whose columns P has left by then
+    // The tiles take turns, so that one's products run while the other's weights are made; without
+    // that both wait at the same time.  The weights are waited for last: all else is there by then.
+    for (int j = 0; j <= n_all && !wait.dead; ++j, ++turns) {
+      const uint32_t vs = (steps + j - 1) % kStages, ks = (steps + j) % kStages;
+      if (j > 0) wait(&sh.bar.v_full[vs], ((steps + j - 1) / kStages) & 1);
+      if (j < n_all) wait(&sh.bar.k_full[ks], ((steps + j) / kStages) & 1);
+      if (i == 1 || turns > 0) wait(&sh.bar.turn[i], (i == 1 ? turns : turns - 1) & 1);
+      if (j > 0 && j - 1 < n) wait(&sh.bar.p_full[i], (done + j - 1) & 1);
+      if (wait.dead) break;
+      tc_fence_after();
+      if (elect_one()) {
+        if (j > 0 && j - 1 < n) {
+          const uint64_t b = d_v + (uint64_t)(vs * (L::kV >> 4));
+#pragma unroll
+          for (int kk = 0; kk < kTile / 16; ++kk)  // 16 keys' rows
+            mma_ts(t_o, t_s + kk * 8, b + ((kk * 16 * 128) >> 4), idesc_f16(kTile, D) | kRowsAlongK,
+                   (j > 1 || kk > 0) ? 1u : 0u);
+          mma_commit(&sh.bar.o_done[i]);
+        }
+        if (j < n) {
+          const uint64_t b = d_k + (uint64_t)(ks * (L::kQ >> 4));
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint64_t off = ((kk >> 2) * kPanel + (kk & 3) * 32) >> 4;
+            mma_ss(t_s, d_q + off, b + off, idesc_f16(kTile, kTile), kk > 0 ? 1u : 0u);
+          }
+          mma_commit(&sh.bar.s_full[i]);
+        }
+        mbar_arrive(&sh.bar.turn[1 - i]);
+        // the stages are free once these products are done (or were not needed: the other tile has more steps)
+        if (j > 0) mma_commit(&sh.bar.v_empty[vs]);
+        if (j < n_all) mma_commit(&sh.bar.k_empty[ks]);
+      }
+      __syncwarp();
+    }
+    steps += n_all;
+    done += n;
+    if (!end_item(sh, wait)) break;
+  }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_constant__ AttendParams p) {
   using L = Smem<D>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* s_q = smem;
-  uint8_t* s_k = smem + 2 * L::kQ;
-  uint8_t* s_v = s_k + kStages * L::kQ;
-  __shared__ uint64_t q_full, k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
-  __shared__ uint64_t s_full[2], p_full[2], o_done[2];
-  __shared__ uint32_t s_tmem;
-  __shared__ uint32_t s_nan[kStages][4];  // keys of the step whose values are not finite
-  __shared__ Item s_item[2];
-  __shared__ int s_dead;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  uint8_t* s_v = smem + 2 * L::kQ;
+  uint8_t* s_k = s_v + kStages * L::kV;
+  uint8_t* s_raw = s_k + kStages * L::kQ;
+  __shared__ Shared sh;
+  const int tid = threadIdx.x, warp = tid >> 5;
   if (tid == 0) {
-    mbar_init(&q_full, kRowThreads / 32);
+    mbar_init(&sh.bar.q_full, kRowThreads / 32);
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(&k_full[i], kFillWarps);
-      mbar_init(&v_full[i], kFillWarps);
-      mbar_init(&k_empty[i], 1);
-      mbar_init(&v_empty[i], 1);
+      mbar_init(&sh.bar.k_full[i], 1);
+      mbar_init(&sh.bar.v_full[i], 1);
+      mbar_init(&sh.bar.k_empty[i], 2);
+      mbar_init(&sh.bar.v_empty[i], 2);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&s_full[i], 1);
-      mbar_init(&p_full[i], 4);
-      mbar_init(&o_done[i], 1);
+      mbar_init(&sh.bar.s_full[i], 1);
+      mbar_init(&sh.bar.p_full[i], 4);
+      mbar_init(&sh.bar.o_done[i], 1);
+      mbar_init(&sh.bar.raw_full[i], 1);
+      mbar_init(&sh.bar.raw_empty[i], 1);
+      mbar_init(&sh.bar.turn[i], 1);
     }
     fence_barrier_init();
-    s_dead = 0;
+    sh.dead = 0;
   }
   pdl_wait();
-  const int32_t* share = p.work + p.requests + 1;  // pairs of tiles of the requests before each
-  const int heads = p.cache.heads;
-  const int64_t items = (int64_t)share[p.requests] * heads;
   // the next item: later rows, which see more, first
   auto fetch = [&](Item& it) {
+    const int32_t* share = p.work + p.requests + 1;  // pairs of tiles of the requests before each
+    const int heads = p.cache.heads;
     it.rows = 0;
     const int64_t i = (int64_t)atomicAdd(&p.cnt[0], 1);
-    if (i >= items) return;
+    if (i >= (int64_t)share[p.requests] * heads) return;
     const int pair = (int)(i / heads);
     int lo = 0, hi = p.requests;
     while (hi - lo > 1) {
@@ -157,404 +604,32 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
     it.rows = (int)min(all - it.row0, (int64_t)(2 * kTile));
     it.sees0 = it.len - fresh + 1;
   };
-  if (tid == kThreads - 32) {
+  if (tid == kBusyThreads - 32) {
     Item it;
     do fetch(it);
     while (it.rows < 0);
-    s_item[0] = it;
+    sh.item[0] = it;
   }
   if (warp == 0) {
-    tmem_alloc(&s_tmem, 512);
+    tmem_alloc(&sh.tmem, 512);
     tmem_relinquish();
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = s_tmem;
-  const int shift = p.cache.shift;
-  const int64_t block = kv4_block_bytes<D>(shift);
-
-  // phases of the barriers, counted over all items: steps of keys, and of either tile
-  uint32_t steps = 0, done[2] = {0, 0}, round = 0;
-  for (;; ++round) {
-    const Item it = s_item[round & 1];
-    if (it.rows <= 0) break;
-    // steps that either tile's last row sees
-    int n[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int rows = min(it.rows - i * kTile, kTile);
-      n[i] = rows > 0 ? (it.sees0 + (it.row0 + i * kTile + rows - 1) / p.group + kTile - 1) / kTile : 0;
-    }
-    const int n_all = max(n[0], n[1]);
-    bool dead = false;
-    auto wait = [&](uint64_t* bar, uint32_t parity) {
-      if (dead) return;
-      if (!__all_sync(0xffffffffu, mbar_wait(bar, parity, p.timeout_ns))) {
-        if (lane == 0) set_status(p.status, kStatusTimeout);
-        dead = true;
-      }
-    };
-
-    if (warp < kRowThreads / 32) {
-      // -------------------------------------------------------------- rows
-      const int i = warp >> 2;  // tile
-      const int r = tid & (kTile - 1);
-      const bool there = i * kTile + r < it.rows;
-      const int row = it.row0 + i * kTile + r, token = row / p.group;
-      const int limit = there ? it.sees0 + token : 0;  // keys that the row sees
-      const int64_t col = (int64_t)(it.h * p.group + row - token * p.group) * D;
-      float cr;  // log2 score = cr * product
-      {
-        const uint4* src = reinterpret_cast<const uint4*>(p.q + (it.q0 + (int64_t)token) * p.q_stride + col);
-        uint32_t big = 0;
-#pragma unroll 4
-        for (int c = 0; c < D / 8; ++c) {
-          const uint4 u = there ? src[c] : make_uint4(0, 0, 0, 0);
-          const uint32_t x[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) big = max(big, max(x[j] & 0x7fffu, (x[j] >> 16) & 0x7fffu));
-        }
-        // 2^(141 - e): the row's largest entry, of biased exponent e, comes to 2^14 ... 2^15
-        const uint32_t e = max(15u, min(254u, big >> 7));
-        const float f = copysignf(__uint_as_float((268u - e) << 23), p.scale_log2);
-        cr = __uint_as_float((e - 14u) << 23) * fabsf(p.scale_log2);
-        uint8_t* dst = s_q + i * L::kQ + r * 128;
-#pragma unroll 4
-        for (int c = 0; c < D / 8; ++c) {
-          const uint4 u = there ? src[c] : make_uint4(0, 0, 0, 0);
-          const uint32_t x[4] = {u.x, u.y, u.z, u.w};
-          float y[8];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            y[2 * j] = __uint_as_float(x[j] << 16) * f;
-            y[2 * j + 1] = __uint_as_float(x[j] & 0xffff0000u) * f;
-          }
-          *reinterpret_cast<uint4*>(dst + (c >> 3) * kPanel + (((c & 7) ^ (r & 7)) << 4)) =
-              make_uint4(pack_f16(y[0], y[4]), pack_f16(y[1], y[5]), pack_f16(y[2], y[6]), pack_f16(y[3], y[7]));
-        }
-      }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&q_full);
-      const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-      const uint32_t t_s = tmem + lanes + i * kTile, t_o = tmem + lanes + 2 * kTile + i * D;
-      float m = -INFINITY;
-      float l = 0.f;
-      for (int j = 0; j < n[i]; ++j) {
-        wait(&s_full[i], (done[i] + j) & 1);
-        if (dead) break;
-        tc_fence_after();
-        const bool edge = (j + 1) * kTile > limit;  // the row does not see all of the step
-        const bool cut = __any_sync(0xffffffffu, edge);
-        float top = -INFINITY;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t u[32];
-          tmem_load32(t_s + 32 * c, u);
-          tmem_load_wait();
-          if (cut) {
-#pragma unroll
-            for (int k = 0; k < 32; ++k)
-              if (j * kTile + 32 * c + k < limit) top = fmaxf(top, __uint_as_float(u[k]));
-          } else {
-#pragma unroll
-            for (int k = 0; k < 32; ++k) top = fmaxf(top, __uint_as_float(u[k]));
-          }
-        }
-        top *= cr;  // (-inf stays: cr > 0, or 0 where nothing is seen or the scale is 0)
-        if (cr == 0.f) top = 0.f;
-        const bool lift = top > m + 8.f;
-        if (__any_sync(0xffffffffu, lift)) {
-          const float up = lift ? top : m;
-          const float alpha = m == -INFINITY ? (j == 0 ? 1.f : 0.f) : ex2(m - up);
-          l *= alpha;
-          m = up;
-          if (j > 0) {
-            wait(&o_done[i], (done[i] + j - 1) & 1);
-            if (dead) break;
-            tc_fence_after();
-#pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
-              uint32_t u[32];
-              tmem_load32(t_o + 32 * c, u);
-              tmem_load_wait();
-#pragma unroll
-              for (int k = 0; k < 32; ++k) u[k] = __float_as_uint(__uint_as_float(u[k]) * alpha);
-              tmem_store32(t_o + 32 * c, u);
-            }
-            tmem_store_wait();
-          }
-        }
-        const float minus = m == -INFINITY ? 0.f : -m;
-        const uint64_t c2 = two(cr, cr), m2 = two(minus, minus);
-        uint64_t sum = 0;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t u[32], w[16];
-          tmem_load32(t_s + 32 * c, u);
-          tmem_load_wait();
-#pragma unroll
-          for (int k = 0; k < 32; k += 2) {
-            float a, b;
-            apart(fma2(two(__uint_as_float(u[k]), __uint_as_float(u[k + 1])), c2, m2), a, b);
-            a = ex2(a), b = ex2(b);
-            if (cut) {
-              if (j * kTile + 32 * c + k >= limit) a = 0.f;
-              if (j * kTile + 32 * c + k + 1 >= limit) b = 0.f;
-            }
-            sum = add2(sum, two(a, b));
-            w[k / 2] = pack_f16(a, b);
-          }
-          tmem_store16(t_s + 16 * c, w);
-        }
-        float a, b;
-        apart(sum, a, b);
-        l += a + b;
-        // a value row that is not finite entered as zeros: it makes NaN of the rows that see it
-        const int st = (steps + j) % kStages;
-        wait(&v_full[st], ((steps + j) / kStages) & 1);
-        if (dead) break;
-        const volatile uint32_t* bad = s_nan[st];
-        const uint32_t x[4] = {bad[0], bad[1], bad[2], bad[3]};
-        if (x[0] | x[1] | x[2] | x[3]) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const int seen = limit - (j * kTile + 32 * c);
-            const uint32_t mask = seen >= 32 ? ~0u : seen <= 0 ? 0u : (1u << seen) - 1u;
-            if (x[c] & mask) l = __uint_as_float(0x7fffffffu);
-          }
-        }
-        tmem_store_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&p_full[i]);
-      }
-      if (n[i] > 0) {
-        wait(&o_done[i], (done[i] + n[i] - 1) & 1);
-        tc_fence_after();
-        if (!dead) {
-          const float inv = l == 0.f ? 0.f : 1.f / l;
-          uint16_t* dst = p.out + (it.q0 + (int64_t)token) * p.out_stride + col;
-#pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
-            uint32_t u[32];
-            tmem_load32(t_o + 32 * c, u);
-            tmem_load_wait();
-            if (there) {
-#pragma unroll
-              for (int k = 0; k < 32; k += 8) {
-                uint32_t w[4];
-#pragma unroll
-                for (int x = 0; x < 4; ++x)
-                  w[x] = pack_bf16(__uint_as_float(u[k + 2 * x]) * inv, __uint_as_float(u[k + 2 * x + 1]) * inv);
-                *reinterpret_cast<uint4*>(dst + 32 * c + k) = make_uint4(w[0], w[1], w[2], w[3]);
-              }
-            }
-          }
-        }
-        tc_fence_before();
-      }
-    } else if (warp < (kRowThreads + kFillThreads) / 32) {
-      // -------------------------------------------------------------- keys and values
-      const int f = tid - kRowThreads;
-      const int32_t* table = p.table + (int64_t)it.b * p.width;
-      auto block_of = [&](int key) -> const uint8_t* {  // null behind the last key
-        if (key >= it.len) return nullptr;
-        const int at = key >> shift, page = at < p.width ? table[at] : -1;
-        if (page < 0 || page >= p.cache.pages) {
-          set_status(p.status, kStatusBadIndex);
-          return nullptr;
-        }
-        return p.cache.data + ((int64_t)page * heads + it.h) * block;
-      };
-      const int k_key = f & (kTile - 1), k_half = f >> 7;             // a key, half of its channels
-      const int v_group = (f & 7) + 8 * (f >> 7), v_word = (f >> 3) & 15;  // eight keys, eight channels
-      constexpr int KQ = D / 64;                                      // 16-byte pieces of half a key
-      const int page_keys = 1 << shift;
-      const bool v_there = D == 128 || v_word < 8;
-      uint4 kc[KQ], vp[2];
-      uint32_t kp, vc[8];
-      auto load_k = [&](int j) {
-        const int key = j * kTile + k_key;
-        const uint8_t* bl = block_of(key);
-        const int in = key & (page_keys - 1);
-        kp = 0;
-#pragma unroll
-        for (int x = 0; x < KQ; ++x) kc[x] = make_uint4(0, 0, 0, 0);
-        if (bl) {
-#pragma unroll
-          for (int x = 0; x < KQ; ++x)
-            kc[x] = __ldg(reinterpret_cast<const uint4*>(bl + in * (D / 2) + k_half * (D / 4)) + x);
-          kp = __ldg(reinterpret_cast<const uint32_t*>(bl + kv4_key_params<D>(shift)) + in);
-        }
-      };
-      auto load_v = [&](int j) {
-        const int key = j * kTile + 8 * v_group;
-        const uint8_t* bl = block_of(key);
-        const int in = key & (page_keys - 1);
-        vp[0] = vp[1] = make_uint4(0, 0, 0, 0);
-#pragma unroll
-        for (int x = 0; x < 8; ++x) vc[x] = 0;
-        if (bl && v_there) {
-#pragma unroll
-          for (int x = 0; x < 8; ++x)
-            vc[x] = __ldg(reinterpret_cast<const uint32_t*>(bl + kv4_value_codes<D>(shift) + (in + x) * (D / 2)) + v_word);
-          const uint4* src = reinterpret_cast<const uint4*>(bl + kv4_value_params<D>(shift) + in * 4);
-          vp[0] = __ldg(src), vp[1] = __ldg(src + 1);
-        }
-      };
-      load_k(0);
-      load_v(0);
-      for (int j = 0; j < n_all; ++j) {
-        const int st = (steps + j) % kStages;
-        const uint32_t ph = ((steps + j) / kStages) & 1;
-        wait(&k_empty[st], ph ^ 1);
-        if (dead) break;
-        {
-          const uint32_t s = __byte_perm(kp, kp, 0x1010), m = __byte_perm(kp, kp, 0x3232);
-          uint8_t* dst = s_k + st * L::kQ + k_key * 128;
-#pragma unroll
-          for (int x = 0; x < KQ; ++x) {
-            const uint32_t w[4] = {kc[x].x, kc[x].y, kc[x].z, kc[x].w};
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              const int c = k_half * (D / 16) + 4 * x + y;  // eight channels
-              const uint32_t h = w[y] >> 8;
-              *reinterpret_cast<uint4*>(dst + (c >> 3) * kPanel + (((c & 7) ^ (k_key & 7)) << 4)) =
-                  make_uint4(value_lo(w[y], s, m), value_hi(w[y], s, m), value_lo(h, s, m), value_hi(h, s, m));
-            }
-          }
-        }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&k_full[st]);
-        if (j + 1 < n_all) load_k(j + 1);  // (the next step's, while this one's values are expanded)
-        wait(&v_empty[st], ph ^ 1);
-        if (dead) break;
-        {
-          uint32_t par[8] = {vp[0].x, vp[0].y, vp[0].z, vp[0].w, vp[1].x, vp[1].y, vp[1].z, vp[1].w};
-          uint32_t nan = 0;
-          const int left = it.len - (j * kTile + 8 * v_group);  // keys of the eight that were written
-#pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            if (x >= left) par[x] = 0;
-            if ((par[x] & 0x7c00u) == 0x7c00u || (par[x] & 0x7c000000u) == 0x7c000000u) {
-              par[x] = 0;
-              nan |= 1u << x;
-            }
-          }
-          // 32 keys a word: the four lanes' bytes side by side (every word of channels says the same)
-          uint32_t word = nan << (8 * (v_group & 3));
-          word |= __shfl_xor_sync(0xffffffffu, word, 1);
-          word |= __shfl_xor_sync(0xffffffffu, word, 2);
-          if (v_word == 0 && (v_group & 3) == 0) s_nan[st][v_group >> 2] = word;
-          if (v_there) {
-            uint32_t s[4], m[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              s[x] = __byte_perm(par[2 * x], par[2 * x + 1], 0x5410);
-              m[x] = __byte_perm(par[2 * x], par[2 * x + 1], 0x7632);
-            }
-            uint8_t* dst = s_v + st * L::kV + (v_group >> 3) * (D * 128) + v_word * 8 * 128;
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              uint32_t w[4];
-#pragma unroll
-              for (int x = 0; x < 4; ++x) w[x] = __byte_perm(vc[2 * x], vc[2 * x + 1], half ? 0x7632 : 0x5410);
-#pragma unroll
-              for (int z = 0; z < 2; ++z) {
-                const int c = 4 * half + 2 * z;  // channel of the eight
-                uint32_t lo[4], hi[4];
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                  const uint32_t y = z ? w[x] >> 8 : w[x];
-                  lo[x] = value_lo(y, s[x], m[x]);
-                  hi[x] = value_hi(y, s[x], m[x]);
-                }
-                *reinterpret_cast<uint4*>(dst + c * 128 + (((v_group & 7) ^ c) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                *reinterpret_cast<uint4*>(dst + (c + 1) * 128 + (((v_group & 7) ^ (c + 1)) << 4)) =
-                    make_uint4(hi[0], hi[1], hi[2], hi[3]);
-              }
-            }
-          }
-        }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&v_full[st]);
-        if (j + 1 < n_all) load_v(j + 1);
-      }
-    } else {
-      // -------------------------------------------------------------- the products
-      if (lane == 0) {
-        Item next;
-        do fetch(next);
-        while (next.rows < 0);
-        s_item[(round + 1) & 1] = next;
-      }
-      __syncwarp();
-      const uint32_t a_q = smem_u32(s_q), a_k = smem_u32(s_k), a_v = smem_u32(s_v);
-      auto scores = [&](int i, int j) {  // S_i = Q_i . K_j^T
-        const int st = (steps + j) % kStages;
-        wait(&k_full[st], ((steps + j) / kStages) & 1);
-        tc_fence_after();
-        if (!dead && elect_one()) {
-#pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk) {
-            const uint32_t off = (kk >> 2) * kPanel + (kk & 3) * 32;
-            mma_ss(tmem + i * kTile, smem_desc_sw128(a_q + i * L::kQ + off), smem_desc_sw128(a_k + st * L::kQ + off),
-                   idesc_f16(kTile, kTile), kk > 0 ? 1u : 0u);
-          }
-          mma_commit(&s_full[i]);
-        }
-        __syncwarp();
-      };
-      wait(&q_full, round & 1);
-      for (int i = 0; i < 2; ++i)
-        if (n[i] > 0) scores(i, 0);
-      if (!dead && elect_one()) mma_commit(&k_empty[steps % kStages]);
-      __syncwarp();
-      for (int j = 0; j < n_all && !dead; ++j) {
-        const int st = (steps + j) % kStages;
-        for (int i = 0; i < 2; ++i) {
-          if (j < n[i]) {
-            wait(&v_full[st], ((steps + j) / kStages) & 1);
-            wait(&p_full[i], (done[i] + j) & 1);
-            tc_fence_after();
-            if (!dead && elect_one()) {
-#pragma unroll
-              for (int kk = 0; kk < kTile / 16; ++kk) {
-                const uint32_t off = (kk >> 2) * (D * 128) + (kk & 3) * 32;
-                mma_ts(tmem + 2 * kTile + i * D, tmem + i * kTile + kk * 8, smem_desc_sw128(a_v + st * L::kV + off),
-                       idesc_f16(kTile, D), (j > 0 || kk > 0) ? 1u : 0u);
-              }
-              mma_commit(&o_done[i]);
-            }
-            __syncwarp();
-          }
-          if (j + 1 < n[i]) scores(i, j + 1);
-        }
-        if (!dead && elect_one()) {
-          mma_commit(&v_empty[st]);
-          if (j + 1 < n_all) mma_commit(&k_empty[(steps + j + 1) % kStages]);
-        }
-        __syncwarp();
-      }
-    }
-    if (dead) s_dead = 1;
-    steps += n_all;
-    done[0] += n[0];
-    done[1] += n[1];
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    if (s_dead) break;
-  }
-  if (warp == kRowThreads / 32 && !s_dead) {  // the products' last arrivals on this CTA's barriers
-    for (uint32_t x = steps > kStages ? steps - kStages : 0; x < steps; ++x) {
-      mbar_wait(&k_empty[x % kStages], (x / kStages) & 1, p.timeout_ns);
-      mbar_wait(&v_empty[x % kStages], (x / kStages) & 1, p.timeout_ns);
-    }
+  const uint32_t tmem = sh.tmem;
+  // registers: 128 a thread at launch, (168 + 168 + 104 + 72) / 4 from here on
+  if (warp < kRowThreads / 32) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    rows_role<D>(p, sh, s_q, tmem);
+  } else if (warp < kRowThreads / 32 + kFillWarps) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    fill_role<D>(p, sh, s_k, s_v, s_raw);
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    const int x = warp - kRowThreads / 32 - kFillWarps;
+    if (x < 2) product_role<D>(p, sh, s_q, s_k, s_v, tmem, x);
+    if (x == 2) copy_role<D>(p, sh, s_raw, fetch);
   }
   tc_fence_before();
   __syncthreads();
