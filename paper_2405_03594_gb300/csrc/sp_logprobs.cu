@@ -2,9 +2,9 @@
 // entries (include/sp_serve.h).
 //
 // One pass over the row keeps, per thread and around its running maximum m,
-//     s = sum e^(x - m),   z = sum (x - m) e^(x - m),
+//     s = sum 2^d,   z = sum d 2^d,   d = (x - m) log2(e),
 // which join as sums do once rescaled to the larger maximum; then
-//     log p(i) = (x_i - m) - log s,   H = log s - z / s.
+//     log p(i) = (x_i - m) - log s,   H = log s - log(2) z / s.
 // The pass is bound by reading the row.  A row goes to one CTA, or, where rows are few, to a cluster
 // of up to eight that exchange their sums through shared memory.
 //
@@ -14,23 +14,16 @@
 // entries again (L2 has them) and the handful that reach tau are ranked by counting.
 #include <cfloat>
 
-#include "sp_kv4.cuh"
+#include "sp_attend.cuh"
 
 namespace sp {
 namespace {
 
-constexpr int kLpThreads = 512;
-constexpr int kLpWarps = kLpThreads / 32;
+constexpr int kFewThreads = 128, kManyThreads = 512;  // of a row's CTA: where rows are many, few
 constexpr int kMaxTop = 64;
 constexpr int kMaxCluster = 8;
 constexpr int kCandidates = 1024;
 constexpr float kLog2e = 1.4426950408889634f;
-
-__device__ __forceinline__ float ex2(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
 
 // Keys in the order of the numbers, NaN above all; none is 0.
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -55,8 +48,8 @@ struct Stat {
 __device__ __forceinline__ Stat join(const Stat& a, const Stat& b) {
   Stat r;
   r.m = fmaxf(a.m, b.m);
-  const float da = a.m == -INFINITY ? 0.f : a.m - r.m, db = b.m == -INFINITY ? 0.f : b.m - r.m;
-  const float fa = ex2(da * kLog2e), fb = ex2(db * kLog2e);
+  const float da = a.m == -INFINITY ? 0.f : (a.m - r.m) * kLog2e, db = b.m == -INFINITY ? 0.f : (b.m - r.m) * kLog2e;
+  const float fa = ex2(da), fb = ex2(db);
   // a side that has seen nothing but -inf has s = z = 0; one so far below that its factor is 0 may
   // be an infinite distance below, and adds nothing (a NaN stays in s)
   r.s = a.s * fa + b.s * fb;
@@ -69,42 +62,77 @@ struct Vec;
 template <>
 struct Vec<uint16_t> {
   static constexpr int N = 8;
+  static constexpr uint32_t kNothing = 0xff80ff80u;  // -inf
   static __device__ __forceinline__ float one(uint16_t u) { return __uint_as_float((uint32_t)u << 16); }
+  static __device__ __forceinline__ float2 two_of(uint32_t w) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  }
+  template <int W>
+  static __device__ __forceinline__ float largest(const uint32_t (&w)[W]) {
+    uint32_t m = w[0];
+#pragma unroll
+    for (int i = 1; i < W; ++i) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(w[i]));
+    const float2 x = two_of(m);
+    return max_nan(x.x, x.y);
+  }
   static __device__ __forceinline__ void get(const uint4& u, float (&x)[8]) {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    for (int i = 0; i < 4; ++i) {
+      const float2 y = two_of(w[i]);
+      x[2 * i] = y.x, x[2 * i + 1] = y.y;
+    }
   }
 };
 template <>
 struct Vec<float> {
   static constexpr int N = 4;
+  static constexpr uint32_t kNothing = 0xff800000u;
   static __device__ __forceinline__ float one(float u) { return u; }
+  template <int W>
+  static __device__ __forceinline__ float largest(const uint32_t (&w)[W]) {
+    float m[2] = {__uint_as_float(w[0]), __uint_as_float(w[1])};
+#pragma unroll
+    for (int i = 2; i < W; ++i) m[i & 1] = max_nan(m[i & 1], __uint_as_float(w[i]));
+    return max_nan(m[0], m[1]);
+  }
   static __device__ __forceinline__ void get(const uint4& u, float (&x)[4]) {
     x[0] = __uint_as_float(u.x), x[1] = __uint_as_float(u.y), x[2] = __uint_as_float(u.z), x[3] = __uint_as_float(u.w);
   }
 };
 
-template <int N>
-__device__ __forceinline__ void take(Stat& st, float& top, const float (&x)[N]) {
-  float vm = x[0];
-#pragma unroll
-  for (int i = 1; i < N; ++i) vm = max_nan(vm, x[i]);
-  top = max_nan(top, vm);
-  if (vm > st.m) {  // (never for a NaN, which makes s NaN below)
-    const float d = st.m == -INFINITY ? 0.f : st.m - vm, f = ex2(d * kLog2e);
-    st.z = f > 0.f ? fmaf(st.s, d, st.z) * f : 0.f;
-    st.s *= f;
-    st.m = vm;
+// A thread's numbers, the sums in pairs.
+struct Running {
+  float m, top;  // maximum of the numbers (m: so far as the sums know it; top: a NaN if there is one)
+  uint64_t s, z;
+  __device__ __forceinline__ void lift(float vm) {
+    top = max_nan(top, vm);
+    if (vm > m) {  // (never for a NaN, which makes s NaN below)
+      const float d = m == -INFINITY ? 0.f : (m - vm) * kLog2e, f = ex2(d);
+      const uint64_t f2 = two(f, f);
+      z = f > 0.f ? mul2(fma2(s, two(d, d), z), f2) : 0;
+      s = mul2(s, f2);
+      m = vm;
+    }
   }
-  const float m = st.m == -INFINITY ? 0.f : st.m;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const float d = x[i] - m, e = ex2(d * kLog2e);
-    st.s += e;
-    st.z = e > 0.f ? fmaf(e, d, st.z) : st.z;
+  // Two numbers, neither above m.  The distance is bounded so that an infinite one adds nothing
+  // (2^-150 is 0 here), and a NaN stays one.
+  __device__ __forceinline__ void add(float a, float b, uint64_t minus) {
+    float x, y;
+    apart(mul2(add2(two(a, b), minus), two(kLog2e, kLog2e)), x, y);
+    x = max_nan(x, -150.f), y = max_nan(y, -150.f);
+    const uint64_t e = two(ex2(x), ex2(y));
+    s = add2(s, e);
+    z = fma2(e, two(x, y), z);
   }
-}
+  __device__ __forceinline__ uint64_t minus() const { return two(m == -INFINITY ? 0.f : -m, m == -INFINITY ? 0.f : -m); }
+  __device__ __forceinline__ Stat stat() const {
+    float s0, s1, z0, z1;
+    apart(s, s0, s1);
+    apart(z, z0, z1);
+    return Stat{m, s0 + s1, z0 + z1};
+  }
+};
 
 struct LogprobParams {
   const void* logits;
@@ -122,14 +150,32 @@ __device__ __forceinline__ uint64_t ld_cluster_u64(uint32_t caddr) {
   return v;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kLpThreads) logprobs_kernel(const __grid_constant__ LogprobParams p) {
+// The warp's lanes joined, in every lane: the maximum first, then one rescaling and plain sums.
+__device__ __forceinline__ Stat join_warp(Stat a) {
+  float m = a.m;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  const float d = a.m == -INFINITY ? 0.f : (a.m - m) * kLog2e, f = ex2(d);
+  uint64_t sz = two(a.s * f, f > 0.f ? fmaf(a.s, d, a.z) * f : 0.f);
+#pragma unroll
+  for (int d2 = 16; d2 > 0; d2 >>= 1) sz = add2(sz, __shfl_xor_sync(0xffffffffu, sz, d2));
+  Stat r;
+  r.m = m;
+  apart(sz, r.s, r.z);
+  return r;
+}
+
+template <typename T, int kLpThreads>
+__global__ void __launch_bounds__(kLpThreads, 1536 / kLpThreads)
+    logprobs_kernel(const __grid_constant__ LogprobParams p) {
+  constexpr int kLpWarps = kLpThreads / 32;
   using V = Vec<T>;
   constexpr int N = V::N;
   __shared__ uint64_t s_cand[kCandidates];
   __shared__ uint64_t s_top[kMaxTop];
-  __shared__ Stat s_stat[kLpWarps];
+  __shared__ Stat s_stat[kLpWarps > kMaxCluster ? kLpWarps : kMaxCluster];
   __shared__ Stat s_row;
+  __shared__ uint32_t s_keys[kLpWarps][2];  // the least and the largest of the warp's threads' best
   __shared__ float s_lse[2];
   __shared__ int s_count;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -146,58 +192,62 @@ __global__ void __launch_bounds__(kLpThreads) logprobs_kernel(const __grid_const
   const int loose = rank == 0 ? (int)(head + (p.vocab - tail)) : 0;
   auto loose_at = [&](int i) { return i < head ? (int64_t)i : tail + (i - head); };
 
-  Stat st = {-INFINITY, 0.f, 0.f};
-  float top = -INFINITY;
+  Running run = {-INFINITY, -INFINITY, 0, 0};
   bool any = false;
   constexpr int kBatch = 4;
   for (int64_t i = v0 + tid; i < v1; i += kBatch * kLpThreads) {
-    uint4 u[kBatch];
-#pragma unroll
-    for (int j = 0; j < kBatch; ++j)
-      if (i + j * kLpThreads < v1) u[j] = __ldg(xv + i + j * kLpThreads);
+    uint32_t u[4 * kBatch];
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
-      if (i + j * kLpThreads < v1) {
-        float f[N];
-        V::get(u[j], f);
-        take<N>(st, top, f);
-        any = true;
+      uint4 v = make_uint4(V::kNothing, V::kNothing, V::kNothing, V::kNothing);
+      if (i + j * kLpThreads < v1) v = __ldg(xv + i + j * kLpThreads);
+      u[4 * j] = v.x, u[4 * j + 1] = v.y, u[4 * j + 2] = v.z, u[4 * j + 3] = v.w;
+    }
+    any = true;
+    run.lift(V::largest(u));
+    const uint64_t minus = run.minus();
+    if constexpr (N == 8) {
+#pragma unroll
+      for (int j = 0; j < 4 * kBatch; ++j) {
+        const float2 y = V::two_of(u[j]);
+        run.add(y.x, y.y, minus);
       }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4 * kBatch; j += 2) run.add(__uint_as_float(u[j]), __uint_as_float(u[j + 1]), minus);
     }
   }
   if (tid < loose) {
-    const float f[1] = {V::one(x[loose_at(tid)])};
-    take<1>(st, top, f);
+    const float f = V::one(x[loose_at(tid)]);
     any = true;
+    run.lift(f);
+    run.add(f, -INFINITY, run.minus());
   }
-  Stat w = st;
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    const Stat o = {__shfl_xor_sync(0xffffffffu, w.m, d), __shfl_xor_sync(0xffffffffu, w.s, d),
-                    __shfl_xor_sync(0xffffffffu, w.z, d)};
-    w = join(w, o);
+  const float top = run.top;
+  Stat w = join_warp(run.stat());
+  const uint32_t own = any ? key_of(top) : 0u;  // the thread's best key
+  if (p.top > 0) {
+    const uint32_t least = __reduce_min_sync(0xffffffffu, any ? own : 0xffffffffu), best = __reduce_max_sync(0xffffffffu, own);
+    if (lane == 0) s_keys[warp][0] = least, s_keys[warp][1] = best;
   }
   if (lane == 0) s_stat[warp] = w;
   if (tid == 0) s_count = 0;
   if (tid < kMaxTop) s_top[tid] = 0;
   __syncthreads();
   if (warp == 0) {
-    w = lane < kLpWarps ? s_stat[lane] : Stat{-INFINITY, 0.f, 0.f};
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-      const Stat o = {__shfl_xor_sync(0xffffffffu, w.m, d), __shfl_xor_sync(0xffffffffu, w.s, d),
-                      __shfl_xor_sync(0xffffffffu, w.z, d)};
-      w = join(w, o);
-    }
+    w = join_warp(lane < kLpWarps ? s_stat[lane] : Stat{-INFINITY, 0.f, 0.f});
     if (lane == 0) s_row = w;
   }
 
   if (p.top > 0) {
-    // tau: a key that at least `top` threads reach (0 if there are not so many)
-    const uint32_t own = any ? key_of(top) : 0u;
-    uint32_t lo = 0, hi = 0xffffffffu;  // count(lo) >= top, or lo = 0
+    // tau: a key that at least `top` threads reach, and few more, between the least and the largest of
+    // the threads' maxima (0 if there are not so many threads with entries)
+    uint32_t lo = 0xffffffffu, hi = 0;
+#pragma unroll
+    for (int i = 0; i < kLpWarps; ++i) lo = min(lo, s_keys[i][0]), hi = max(hi, s_keys[i][1]);
+    if (__syncthreads_count(any) < p.top) lo = hi = 0;
     while (lo < hi) {
-      const uint32_t mid = lo + (hi - lo) / 2 + 1;
+      const uint32_t mid = hi - (hi - lo) / 2;
       const int n = __syncthreads_count(own >= mid);
       if (n >= p.top) {
         lo = mid;
@@ -214,16 +264,26 @@ __global__ void __launch_bounds__(kLpThreads) logprobs_kernel(const __grid_const
         if (c < kCandidates) s_cand[c] = ((uint64_t)k << 32) | (uint32_t)~(uint32_t)at;
       }
     };
-    if (any && own >= tau) {
-#pragma unroll 4
-      for (int64_t i = v0 + tid; i < v1; i += kLpThreads) {
-        float f[N];
-        V::get(__ldg(xv + i), f);
+    // the entries of the threads that reach tau: looked at by the thread where it has few vectors, else by
+    // its whole warp, a vector per lane (2048 rows of 32000, one entry: 31 us against 55; 16 rows, 64
+    // entries, a vector a thread: 20 us by the threads, 23 by the warps)
+    auto look_at = [&](int64_t i) {
+      float f[N];
+      V::get(__ldg(xv + i), f);
 #pragma unroll
-        for (int j = 0; j < N; ++j) offer(f[j], head + i * N + j);
+      for (int j = 0; j < N; ++j) offer(f[j], head + i * N + j);
+    };
+    if (v1 - v0 <= 4 * kLpThreads) {
+      if (any && own >= tau)
+        for (int64_t i = v0 + tid; i < v1; i += kLpThreads) look_at(i);
+    } else {
+      for (unsigned hit = __ballot_sync(0xffffffffu, any && own >= tau); hit; hit &= hit - 1) {
+        const int64_t of = v0 + warp * 32 + __ffs(hit) - 1;
+#pragma unroll 1
+        for (int64_t i = of + (int64_t)lane * kLpThreads; i < v1; i += 32 * kLpThreads) look_at(i);
       }
-      if (tid < loose) offer(V::one(x[loose_at(tid)]), loose_at(tid));
     }
+    if (tid < loose && own >= tau) offer(V::one(x[loose_at(tid)]), loose_at(tid));
     __syncthreads();
     int n = s_count;
     if (n > kCandidates) {
@@ -300,7 +360,7 @@ __global__ void __launch_bounds__(kLpThreads) logprobs_kernel(const __grid_const
     const bool empty = a.m == -INFINITY && a.s == 0.f;
     s_lse[0] = a.m;
     s_lse[1] = ls;
-    p.entropy[row] = empty ? 0.f : ls - a.z / a.s;
+    p.entropy[row] = empty ? 0.f : ls - a.z / a.s * 0.6931471805599453f;
     const int64_t id = p.ids[row];
     float r = 0.f;
     if (id >= p.vocab) {
@@ -340,11 +400,13 @@ extern "C" sp_status sp_token_logprobs(const void* logits, sp_logits_dtype dtype
   if (reinterpret_cast<uintptr_t>(logits) % es) return SP_ERR_ALIGNMENT;
   const int sms = current_sms();
   if (sms == 0) return SP_ERR_CUDA;
-  // as many CTAs per row as the SMs have room for two of, each with a vector for half its threads
+  // as many CTAs per row as the SMs have room for at once (two each), each with a vector for half
+  // its threads
   int cluster = 1;
   while (cluster < kMaxCluster && tokens * cluster * 2 <= 2 * sms &&
-         vocab * es / 16 >= (int64_t)cluster * 2 * (kLpThreads / 2))
+         vocab * es / 16 >= (int64_t)cluster * 2 * (kManyThreads / 2))
     cluster *= 2;
+  const bool few = tokens >= 4 * sms;
   if (tokens * cluster > ((int64_t)1 << 31) - 1) return SP_ERR_UNSUPPORTED;
   LogprobParams p = {};
   p.logits = logits;
@@ -358,6 +420,9 @@ extern "C" sp_status sp_token_logprobs(const void* logits, sp_logits_dtype dtype
   p.top_logp = top_logp_out;
   p.top_ids = top_ids_out;
   p.status = device_status_ptr();
-  auto kern = dtype == SP_LOGITS_BF16 ? logprobs_kernel<uint16_t> : logprobs_kernel<float>;
-  return launch_pdl(kern, dim3((unsigned)(tokens * cluster)), kLpThreads, 0, cluster, (cudaStream_t)stream, p);
+  auto kern = dtype == SP_LOGITS_BF16
+                  ? (few ? logprobs_kernel<uint16_t, kFewThreads> : logprobs_kernel<uint16_t, kManyThreads>)
+                  : (few ? logprobs_kernel<float, kFewThreads> : logprobs_kernel<float, kManyThreads>);
+  return launch_pdl(kern, dim3((unsigned)(tokens * cluster)), few ? kFewThreads : kManyThreads, 0, cluster,
+                    (cudaStream_t)stream, p);
 }

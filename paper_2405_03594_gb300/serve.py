@@ -16,6 +16,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 
 import torch
 
@@ -24,58 +25,90 @@ from .sp import SpAttendArgs, SpKv4, SpKvPlanArgs, SpRopeArgs, _check, _lib, _st
 
 PLAN_PAGES, PLAN_WIDTH, PLAN_TOKENS, PLAN_INPUT = 1, 2, 4, 8  # SP_PLAN_*
 
+_BF16, _F32, _I32, _I64 = torch.bfloat16, torch.float32, torch.int32, torch.int64
+_CODES = {ctypes.c_void_p: "P", ctypes.c_int64: "q", ctypes.c_int32: "i", ctypes.c_float: "f"}
 
-def _heads(x: torch.Tensor, heads: int | None, dim: int, name: str) -> int:
+
+def _packed(name: str, args):
+    """(packer of the argument struct's fields, the library function that takes the packed bytes).  A
+    packed call costs a small part of a ctypes struct filled field by field: a decode step makes
+    several calls per layer, each a few microseconds of GPU time."""
+    fmt = struct.Struct("@" + "".join(_CODES.get(t, "P") for _, t in args._fields_) + "0q")  # (padded to whole words)
+    assert fmt.size == ctypes.sizeof(args)
+    fn = _lib[name]  # a function object of its own, with its own argument types
+    fn.argtypes = [ctypes.c_char_p, *getattr(_lib, name).argtypes[1:]]
+    fn.restype = ctypes.c_int
+    return fmt.pack, fn
+
+
+_pack_plan, _plan = _packed("sp_kv_plan", SpKvPlanArgs)
+_pack_rope, _rope = _packed("sp_qk_norm_rope", SpRopeArgs)
+_pack_attend, _attend = _packed("sp_kv4_attend", SpAttendArgs)
+_read = _lib["sp_kv4_read"]  # (the cache by its address)
+_read.argtypes, _read.restype = [ctypes.c_void_p, *_lib.sp_kv4_read.argtypes[1:]], ctypes.c_int
+
+
+def _heads(x: torch.Tensor, heads: int | None, dim: int, name: str) -> tuple[int, int, int]:
     """Checks x [tokens, heads, dim] bf16 with contiguous heads (a view of a fused row serves) and
-    returns its token stride."""
-    if x.dtype != torch.bfloat16 or x.dim() != 3 or x.shape[2] != dim or (heads is not None and x.shape[1] != heads):
+    returns its tokens, heads and token stride."""
+    shape, stride = x.shape, x.stride()
+    if x.dtype is not _BF16 or len(shape) != 3 or shape[2] != dim or (heads is not None and shape[1] != heads):
         raise ValueError(f"{name}: bf16 [tokens, {'heads' if heads is None else heads}, {dim}] wanted, "
-                         f"got {x.dtype} {list(x.shape)}")
-    if x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != dim):
+                         f"got {x.dtype} {list(shape)}")
+    t, h, _ = shape
+    if stride[2] != 1 or (h > 1 and stride[1] != dim):
         raise ValueError(f"{name}: the heads of a token must be contiguous")
-    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0), x.shape[1] * dim)
+    return t, h, stride[0] if t > 1 else max(stride[0], h * dim)
 
 
-def _index(x: torch.Tensor, n: int, dtype, name: str):
-    if x.dtype != dtype or x.dim() != 1 or x.shape[0] < n or not x.is_contiguous():
+def _index(x: torch.Tensor, n: int, dtype, name: str) -> int:
+    """Checks a contiguous vector of n entries or more and returns its address."""
+    if x.dtype is not dtype or x.dim() != 1 or x.shape[0] < n or not x.is_contiguous():
         raise ValueError(f"{name}: contiguous {dtype} [{n}] wanted, got {x.dtype} {list(x.shape)}")
+    return x.data_ptr()
 
 
-def _rope_args(q, k, v, positions, cos_sin, q_weight, k_weight, eps, pairs, q_out, k_out, cache, slots):
-    t, dim = q.shape[0], q.shape[2]
-    a = SpRopeArgs()
-    a.q_stride, a.k_stride = _heads(q, None, dim, "q"), _heads(k, None, dim, "k")
-    if k.shape[0] != t:
+def _weight(w: torch.Tensor | None, dim: int, name: str) -> int:
+    if w is None:
+        return 0
+    if w.dtype is not _BF16 or w.shape != (dim,) or not w.is_contiguous():
+        raise ValueError(f"{name}: contiguous bf16 [{dim}] wanted")
+    return w.data_ptr()
+
+
+def _output(out: torch.Tensor | None, t: int, h: int, dim: int, like: torch.Tensor, name: str) -> torch.Tensor:
+    if out is None:
+        return like.new_empty((t, h, dim))
+    if out.dtype is not _BF16 or out.shape != (t, h, dim) or not out.is_contiguous():
+        raise ValueError(f"{name}: contiguous bf16 {[t, h, dim]} wanted")
+    return out
+
+
+def _run_rope(q, k, v, positions, cos_sin, q_weight, k_weight, eps, pairs, q_out, k_out, cache, slots, stream):
+    dim = q.shape[-1]
+    t, h, q_stride = _heads(q, None, dim, "q")
+    tk, kv, k_stride = _heads(k, None, dim, "k")
+    if tk != t:
         raise ValueError("q and k hold different numbers of tokens")
-    _index(positions, t, torch.int32, "positions")
-    if cos_sin.dtype != torch.float32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous():
+    if cos_sin.dtype is not _F32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous():
         raise ValueError("cos_sin: contiguous float32 [rows, rot] wanted")
-    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if w is not None and (w.dtype != torch.bfloat16 or w.shape != (dim,) or not w.is_contiguous()):
-            raise ValueError(f"{name}: contiguous bf16 [{dim}] wanted")
-    if q_out is None:
-        q_out = torch.empty((t, q.shape[1], dim), dtype=torch.bfloat16, device=q.device)
-    elif q_out.dtype != torch.bfloat16 or q_out.shape != q.shape or not q_out.is_contiguous():
-        raise ValueError("q_out: contiguous bf16 of q's shape wanted")
-    a.q, a.k, a.q_out = q.data_ptr(), k.data_ptr(), q_out.data_ptr()
-    a.positions, a.cos_sin, a.rows, a.rot = positions.data_ptr(), cos_sin.data_ptr(), cos_sin.shape[0], cos_sin.shape[1]
-    a.q_weight = None if q_weight is None else q_weight.data_ptr()
-    a.k_weight = None if k_weight is None else k_weight.data_ptr()
-    a.eps, a.pairs = eps, 1 if pairs else 0
-    a.tokens, a.heads, a.kv_heads, a.head_dim = t, q.shape[1], k.shape[1], dim
+    rows, rot = cos_sin.shape
+    pos = _index(positions, t, _I32, "positions")
+    qw, kw = _weight(q_weight, dim, "q_weight"), _weight(k_weight, dim, "k_weight")
+    q_out = _output(q_out, t, h, dim, q, "q_out")
     if cache is None:
-        if k_out is None:
-            k_out = torch.empty((t, k.shape[1], dim), dtype=torch.bfloat16, device=k.device)
-        elif k_out.dtype != torch.bfloat16 or k_out.shape != k.shape or not k_out.is_contiguous():
-            raise ValueError("k_out: contiguous bf16 of k's shape wanted")
-        a.k_out = k_out.data_ptr()
+        k_out = _output(k_out, t, kv, dim, k, "k_out")
+        v_ptr = v_stride = slot = where = 0
+        k_ptr = k_out.data_ptr()
     else:
-        a.v_stride = _heads(v, k.shape[1], dim, "v")
-        if v.shape[0] != t:
+        tv, _, v_stride = _heads(v, kv, dim, "v")
+        if tv != t:
             raise ValueError("k and v hold different numbers of tokens")
-        _index(slots, t, torch.int64, "slots")
-        a.v, a.slots, a.cache = v.data_ptr(), slots.data_ptr(), ctypes.pointer(cache._c)
-    return a, q_out, k_out
+        slot, where, v_ptr, k_ptr = _index(slots, t, _I64, "slots"), cache._address, v.data_ptr(), 0
+    _check(_rope(_pack_rope(q.data_ptr(), k.data_ptr(), v_ptr, q_stride, k_stride, v_stride, q_out.data_ptr(), k_ptr,
+                            where, slot, pos, cos_sin.data_ptr(), rows, qw, kw, eps, t, h, kv, dim, rot,
+                            1 if pairs else 0), _stream(stream, q.device.index)), "sp_qk_norm_rope")
+    return q_out, k_out
 
 
 def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, cos_sin: torch.Tensor,
@@ -85,9 +118,7 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, cos_
     k [T, Hkv, D], bf16 views with contiguous heads, by rows `positions` (int32 [T]) of cos_sin
     (fp32 [rows, rot]: rot / 2 cosines, then as many sines).  pairs: channel 2i turns with 2i + 1
     instead of i with i + rot / 2.  Returns (q_out, k_out)."""
-    a, q_out, k_out = _rope_args(q, k, None, positions, cos_sin, q_weight, k_weight, eps, pairs, q_out, k_out, None, None)
-    _check(_lib.sp_qk_norm_rope(a, _stream(stream, q.device.index)), "sp_qk_norm_rope")
-    return q_out, k_out
+    return _run_rope(q, k, None, positions, cos_sin, q_weight, k_weight, eps, pairs, q_out, k_out, None, None, stream)
 
 
 class KvCache:
@@ -107,6 +138,7 @@ class KvCache:
         self.pages, self.kv_heads, self.head_dim, self.page_size = pages, kv_heads, head_dim, page_size
         self.data = data
         self._c.data = data.data_ptr()
+        self._address = ctypes.addressof(self._c)
         self._ws_bytes = 0
 
     def append(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor,
@@ -114,18 +146,16 @@ class KvCache:
                eps: float = 1e-5, pairs: bool = False, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
         """qk_norm_rope, with the keys and the values v (as they are) written to the cache at `slots`
         (int64 [T]; a negative one writes nothing).  Returns the queries."""
-        a, out, _ = _rope_args(q, k, v, positions, cos_sin, q_weight, k_weight, eps, pairs, out, None, self, slots)
-        _check(_lib.sp_qk_norm_rope(a, _stream(stream, q.device.index)), "sp_qk_norm_rope")
-        return out
+        return _run_rope(q, k, v, positions, cos_sin, q_weight, k_weight, eps, pairs, out, None, self, slots, stream)[0]
 
     def read(self, slots: torch.Tensor, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
         """The cached keys and values at `slots` (int64 [n]) as bf16 [n, kv_heads, head_dim]."""
-        _index(slots, 0, torch.int64, "slots")
+        at = _index(slots, 0, _I64, "slots")
         n = slots.shape[0]
-        k, v = (torch.empty((n, self.kv_heads, self.head_dim), dtype=torch.bfloat16, device=slots.device)
-                for _ in range(2))
-        _check(_lib.sp_kv4_read(self._c, slots.data_ptr(), n, k.data_ptr(), v.data_ptr(),
-                                _stream(stream, slots.device.index)), "sp_kv4_read")
+        device = slots.device
+        shape = (n, self.kv_heads, self.head_dim)
+        k, v = torch.empty(shape, dtype=_BF16, device=device), torch.empty(shape, dtype=_BF16, device=device)
+        _check(_read(self._address, at, n, k.data_ptr(), v.data_ptr(), _stream(stream, device.index)), "sp_kv4_read")
         return k, v
 
     def attend(self, q: torch.Tensor, batch: "Batch", max_new: int, scale: float | None = None,
@@ -134,23 +164,24 @@ class KvCache:
         the tables of `batch`; max_new: at least the most new tokens of a request; scale: 1 / sqrt(D)
         by default.  A token that sees nothing gets zeros; rows behind the step's last token keep what
         `out` held."""
-        a = batch._attend
-        a.q_stride = _heads(q, batch.heads, self.head_dim, "q")
+        dim = self.head_dim
+        t, h, q_stride = _heads(q, batch.heads, dim, "q")
         if out is None:
-            out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
-        a.out_stride = _heads(out, batch.heads, self.head_dim, "out")
-        if out.shape[0] != q.shape[0]:
-            raise ValueError("q and out hold different numbers of tokens")
+            out, out_stride = q.new_empty((t, h, dim)), h * dim
+        else:
+            to, _, out_stride = _heads(out, h, dim, "out")
+            if to != t:
+                raise ValueError("q and out hold different numbers of tokens")
         if self.kv_heads != batch.kv_heads or self.page_size != batch.page_size:
             raise ValueError("the batch was planned for another kind of cache")
-        a.q, a.out, a.tokens, a.max_new = q.data_ptr(), out.data_ptr(), q.shape[0], max_new
-        a.cache = ctypes.pointer(self._c)
-        a.table, a.lens = batch.table.data_ptr(), batch.lens.data_ptr()
-        a.scale = 1.0 / math.sqrt(self.head_dim) if scale is None else scale
+        device = q.device
         if workspace is None:
-            workspace = sp.workspace_for(self.workspace_size(), q.device, stream)
-        _check(_lib.sp_kv4_attend(a, workspace.data_ptr(), workspace.numel(), _stream(stream, q.device.index)),
-               "sp_kv4_attend")
+            workspace = sp.workspace_for(self.workspace_size(), device, stream)
+        _check(_attend(_pack_attend(q.data_ptr(), out.data_ptr(), q_stride, out_stride, self._address,
+                                    batch.table.data_ptr(), batch.lens.data_ptr(), batch.cu_q.data_ptr(),
+                                    batch.work.data_ptr(), t, batch.requests, batch.width, h, max_new,
+                                    1.0 / math.sqrt(dim) if scale is None else scale, 0),
+                       workspace.data_ptr(), workspace.numel(), _stream(stream, device.index)), "sp_kv4_attend")
         return out
 
     def workspace_size(self) -> int:
@@ -191,14 +222,6 @@ class Batch:
         self.slots = torch.full((tokens,), -1, dtype=torch.int64, device=dev)
         self.positions = torch.zeros(tokens, **i32)
         self.status = torch.zeros(1, **i32)
-        a = self._plan = SpKvPlanArgs()
-        a.cu_q, a.work, a.slots = self.cu_q.data_ptr(), self.work.data_ptr(), self.slots.data_ptr()
-        a.positions, a.status = self.positions.data_ptr(), self.status.data_ptr()
-        a.max_tokens, a.pages, a.requests, a.width = tokens, cache.pages, requests, width
-        a.page_size, a.group = cache.page_size, heads // cache.kv_heads
-        a = self._attend = SpAttendArgs()
-        a.cu_q, a.work = self.cu_q.data_ptr(), self.work.data_ptr()
-        a.requests, a.width, a.heads = requests, width, heads
 
     def plan(self, new: torch.Tensor, advance: bool = False, allocate: bool = True, stream=None) -> "Batch":
         """sp_kv_plan: the tables of a step that adds new[b] tokens (int32 [requests]) to request b, or
@@ -206,14 +229,16 @@ class Batch:
         (cached, free_count); otherwise they stay, and the step can be planned again.  allocate=False:
         `table` already holds every page of the step.  A step that does not fit leaves everything as it
         is, has no tokens, and says why in `status` (PLAN_*)."""
-        _index(new, self.requests, torch.int32, "new")
-        a = self._plan
+        at = _index(new, self.requests, _I32, "new")
         self.lens = self.cached if advance else self._lens
         self.next_count = self.free_count if advance else self._next_count
-        a.cached, a.new_tokens, a.table = self.cached.data_ptr(), new.data_ptr(), self.table.data_ptr()
-        a.free_pages = self.free.data_ptr() if allocate else None
-        a.free_count, a.next_count, a.lens = self.free_count.data_ptr(), self.next_count.data_ptr(), self.lens.data_ptr()
-        _check(_lib.sp_kv_plan(a, _stream(stream, new.device.index)), "sp_kv_plan")
+        _check(_plan(_pack_plan(self.cached.data_ptr(), at, self.table.data_ptr(),
+                                self.free.data_ptr() if allocate else 0, self.free_count.data_ptr(),
+                                self.next_count.data_ptr(), self.lens.data_ptr(), self.cu_q.data_ptr(),
+                                self.work.data_ptr(), self.slots.data_ptr(), self.positions.data_ptr(),
+                                self.status.data_ptr(), self.tokens, self.pages, self.requests, self.width,
+                                self.page_size, self.heads // self.kv_heads),
+                     _stream(stream, new.device.index)), "sp_kv_plan")
         return self
 
 
@@ -222,19 +247,18 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, str
     probability of tokens[t] (int64; a negative one asks for nothing and gets 0) and the entropy, both
     float32 [T]; with top > 0 also the `top` most likely entries: log probabilities [T, top] and ids
     (int64), by falling logit and, among equal ones, rising id."""
-    if logits.dtype not in (torch.bfloat16, torch.float32) or logits.dim() != 2 or logits.stride(1) != 1:
+    dtype = logits.dtype
+    if (dtype is not _BF16 and dtype is not _F32) or logits.dim() != 2 or logits.stride(1) != 1:
         raise ValueError("logits: bf16 or float32 [T, V] with unit column stride wanted")
     t, v = logits.shape
-    _index(tokens, t, torch.int64, "tokens")
-    out = torch.empty((2, t), dtype=torch.float32, device=logits.device)
-    logp, entropy = out[0], out[1]
+    ids = _index(tokens, t, _I64, "tokens")
+    device = logits.device
+    logp, entropy = torch.empty(t, dtype=_F32, device=device), torch.empty(t, dtype=_F32, device=device)
     tl = ti = None
     if top:
-        tl = torch.empty((t, top), dtype=torch.float32, device=logits.device)
-        ti = torch.empty((t, top), dtype=torch.int64, device=logits.device)
-    _check(_lib.sp_token_logprobs(logits.data_ptr(), 0 if logits.dtype == torch.bfloat16 else 1,
-                                  logits.stride(0) if t > 1 else v, t, v, tokens.data_ptr(), top, logp.data_ptr(),
-                                  entropy.data_ptr(), None if tl is None else tl.data_ptr(),
-                                  None if ti is None else ti.data_ptr(), _stream(stream, logits.device.index)),
+        tl, ti = torch.empty((t, top), dtype=_F32, device=device), torch.empty((t, top), dtype=_I64, device=device)
+    _check(_lib.sp_token_logprobs(logits.data_ptr(), 0 if dtype is _BF16 else 1, logits.stride(0) if t > 1 else v, t, v,
+                                  ids, top, logp.data_ptr(), entropy.data_ptr(), tl.data_ptr() if top else None,
+                                  ti.data_ptr() if top else None, _stream(stream, device.index)),
            "sp_token_logprobs")
     return (logp, entropy, tl, ti) if top else (logp, entropy)
