@@ -19,8 +19,9 @@
  *     [P][D/2]  value codes
  *     [P]       keys' (s, m), fp16 each, s first
  *     [P]       values' (s, m)
- * A row x becomes, in fp32 with each operation rounded on its own:
- *     m = fp16(min x)   s = fp16((max x - min x) * (1/15))   (both clamped to +-65504 first)
+ * A row x becomes, with its entries clamped to +-2^15 and in fp32 with each operation rounded on
+ * its own:
+ *     m = fp16(min x)   s = fp16((max x - min x) * (1/15))
  *     n = clamp(rint((x - m) * (1 / s)), 0, 15), or 0 where s = 0
  * and a row with a NaN or an infinity becomes s = 0, m = NaN.  A buffer needs no initial value:
  * what no token was written to takes no part in any result.

@@ -9,6 +9,7 @@
 
 namespace sp {
 
+constexpr float kKvMost = 32768.f;  // largest magnitude that the cache holds
 constexpr int kMaxGroup = 64;       // query heads per key head
 constexpr int kUnitKeys = 32;       // keys of one step of attend_kernel
 constexpr int kRowTile = 32;        // query rows (token, head of the group) of its widest form

@@ -1,11 +1,11 @@
 // sp_rope.cu -- per-head norms of queries and keys, the position rotation and the write of keys and
 // values into the 4-bit cache, in one pass; and the cached rows back (include/sp_serve.h).
 //
-// Every byte is touched once, so the pass is bound by memory: a head of D channels is a row of D / 8
-// lanes with 16 bytes each, and norm, rotation and the row's extremes are shuffles among them.  A
-// warp takes one token and several heads of one kind (queries, keys or values), so that the angles
-// and the norm's weights are loaded once per warp and stay in registers.
-#include "sp_kv4.cuh"
+// Every byte is touched once, so the pass is bound by memory: a head of D channels is a row of D / 16
+// lanes with twice 16 bytes each, half a head apart, so that a channel and the one it usually turns with
+// are in one lane, and norm and the row's extremes are few shuffles.  A warp takes one token and several
+// heads of one kind (queries, keys or values), so that the angles are loaded once per warp.
+#include "sp_attend.cuh"
 #include "sp_lookup.h"
 
 namespace sp {
@@ -39,60 +39,78 @@ __device__ __forceinline__ void unpack8(const uint4& u, float (&x)[8]) {
     x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
   }
 }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
 __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
   return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
 }
-__device__ __forceinline__ float min_nan(float a, float b) {
+__device__ __forceinline__ float min3_nan(float a, float b, float c) {
   float r;
-  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-__device__ __forceinline__ float max_nan(float a, float b) {
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
   float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 
-// The row's codes (eight per lane) and its parameter, as the header defines them.
+// The row's codes (two times eight per lane) and its parameter, as the header defines them.
 template <int LH>
-__device__ __forceinline__ uint32_t quantize(const float (&x)[8], __half2* param) {
-  float lo = x[0], hi = x[0];
+__device__ __forceinline__ uint2 quantize(const float (&x)[2][8], __half2* param) {
+  float lo = min3_nan(x[0][0], x[0][1], x[0][2]), hi = max3_nan(x[0][0], x[0][1], x[0][2]);
 #pragma unroll
-  for (int i = 1; i < 8; ++i) lo = min_nan(lo, x[i]), hi = max_nan(hi, x[i]);
+  for (int i = 3; i < 15; i += 2) {
+    lo = min3_nan(lo, x[i >> 3][i & 7], x[(i + 1) >> 3][(i + 1) & 7]);
+    hi = max3_nan(hi, x[i >> 3][i & 7], x[(i + 1) >> 3][(i + 1) & 7]);
+  }
+  lo = min3_nan(lo, lo, x[1][7]), hi = max3_nan(hi, hi, x[1][7]);
 #pragma unroll
   for (int d = 1; d < LH; d <<= 1) {
-    lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-    hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+    const float lo2 = __shfl_xor_sync(0xffffffffu, lo, d), hi2 = __shfl_xor_sync(0xffffffffu, hi, d);
+    lo = min3_nan(lo, lo, lo2), hi = max3_nan(hi, hi, hi2);
   }
-  if (!finite(lo) || !finite(hi)) {
-    *param = __halves2half2(__ushort_as_half(0), __ushort_as_half(0x7fff));
-    return 0;
-  }
-  const __half m = __float2half_rn(fminf(fmaxf(lo, -65504.f), 65504.f));
-  const __half s = __float2half_rn(fminf(__fmul_rn(__fsub_rn(hi, lo), (float)(1.0 / 15.0)), 65504.f));
-  *param = __halves2half2(s, m);
+  const bool ok = finite(lo) && finite(hi);
+  lo = fminf(fmaxf(lo, -kKvMost), kKvMost), hi = fminf(fmaxf(hi, -kKvMost), kKvMost);
+  const __half m = __float2half_rn(lo);
+  const __half s = __float2half_rn(__fmul_rn(__fsub_rn(hi, lo), (float)(1.0 / 15.0)));
+  *param = ok ? __halves2half2(s, m) : __halves2half2(__ushort_as_half(0), __ushort_as_half(0x7fff));
   const float sf = __half2float(s), mf = __half2float(m);
-  if (!(sf > 0.f)) return 0;
-  const float inv = __fdiv_rn(1.f, sf);
-  uint32_t w = 0;
+  if (!ok || !(sf > 0.f)) return make_uint2(0, 0);
+  const float inv = __frcp_rn(sf);
+  const uint64_t inv2 = two(inv, inv), m2 = two(-mf, -mf), magic2 = two(12582912.f, 12582912.f);
+  uint32_t w[2];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float n = fminf(fmaxf(rintf(__fmul_rn(__fsub_rn(x[i], mf), inv)), 0.f), 15.f);
-    w |= (uint32_t)n << (4 * i);
+  for (int y = 0; y < 2; ++y) {
+    uint32_t n[8];  // a code in the low byte: 1.5 * 2^23 + n rounds to whole numbers, ties to even
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      float a, b;
+      apart(mul2(add2(two(x[y][i], x[y][i + 1]), m2), inv2), a, b);
+      a = fminf(fmaxf(a, 0.f), 15.f), b = fminf(fmaxf(b, 0.f), 15.f);
+      apart(add2(two(a, b), magic2), a, b);
+      n[i] = __float_as_uint(a), n[i + 1] = __float_as_uint(b);
+    }
+    const uint32_t even = __byte_perm(__byte_perm(n[0], n[2], 0x0040), __byte_perm(n[4], n[6], 0x0040), 0x5410);
+    const uint32_t odd = __byte_perm(__byte_perm(n[1], n[3], 0x0040), __byte_perm(n[5], n[7], 0x0040), 0x5410);
+    w[y] = even + odd * 16u;
   }
-  return w;
+  return make_uint2(w[0], w[1]);
 }
 
-// D channels; PAIRS: how channels pair up; CACHE: keys and values go to the cache.
-template <int D, bool PAIRS, bool CACHE>
+// How the channels turn: each with the one half a head further on, which the same lane holds; with
+// one rot / 2 further on; with its neighbour.
+enum : int { kTurnHalf = 0, kTurnShort = 1, kTurnPairs = 2 };
+
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+}
+
+// D channels; TURN: as above; CACHE: keys and values go to the cache.
+template <int D, int TURN, bool CACHE>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeParams p) {
-  constexpr int LH = D / 8, GW = 32 / LH;  // lanes of a head, heads of a warp
+  constexpr int LH = D / 16, GW = 32 / LH;  // lanes of a head, heads of a warp
+  constexpr int S = TURN == kTurnShort ? 2 : 1;  // sets of angles
   const int lane = threadIdx.x & 31, gl = lane % LH, gi = lane / LH;
   const int64_t u = (int64_t)blockIdx.x * (kRopeThreads / 32) + (threadIdx.x >> 5);
   const int token = (int)(u / p.units);
@@ -104,12 +122,10 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
   const int h0 = r * p.iters * GW + gi, h1 = min(heads, (r + 1) * p.iters * GW);
   pdl_wait();
   const uint16_t* src = kind == 0 ? p.q + token * p.qs : kind == 1 ? p.k + token * p.ks : p.v + token * p.vs;
-  const int d0 = gl * 8;
+  const int d0 = gl * 8;  // the lane's channels: eight from here on, and from D / 2 + here on
 
-  // angles of the lane's channels; sn has the sign of the other channel's product
-  float cs[8], sn[8];
-  const bool turns = kind < 2 && d0 < p.rot;
-  if (turns) {
+  float cs[S][8], sn[S][8];
+  if (kind < 2) {
     int64_t pos = p.positions[token];
     if (pos < 0 || pos >= p.rows) {
       set_status(p.status, kStatusBadIndex);
@@ -117,30 +133,39 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
     }
     const float* t = p.cos_sin + pos * p.rot;
     const int half = p.rot / 2;
-    if constexpr (PAIRS) {
-      const float4 c = *reinterpret_cast<const float4*>(t + d0 / 2), s = *reinterpret_cast<const float4*>(t + half + d0 / 2);
-      const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+    if constexpr (TURN == kTurnHalf) {
+      load8(t + d0, cs[0]);
+      load8(t + half + d0, sn[0]);
+    } else if constexpr (TURN == kTurnShort) {
+      // sn has the sign of the other channel's product
 #pragma unroll
-      for (int i = 0; i < 4; ++i) cs[2 * i] = cs[2 * i + 1] = cc[i], sn[2 * i] = -ss[i], sn[2 * i + 1] = ss[i];
-    } else {
-      const int a = d0 < half ? d0 : d0 - half;
-      const float sign = d0 < half ? -1.f : 1.f;
-      const float4 *c = reinterpret_cast<const float4*>(t + a), *s = reinterpret_cast<const float4*>(t + half + a);
-      const float4 c0 = c[0], c1 = c[1], s0 = s[0], s1 = s[1];
-      const float cc[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
-      const float ss[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+      for (int y = 0; y < 2; ++y) {
+        const int d = d0 + y * (D / 2), at = d < half ? d : d - half;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) cs[i] = cc[i], sn[i] = sign * ss[i];
+        for (int i = 0; i < 8; ++i) cs[y][i] = 1.f, sn[y][i] = 0.f;
+        if (d < p.rot) {
+          load8(t + at, cs[y]);
+          load8(t + half + at, sn[y]);
+          if (d < half)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sn[y][i] = -sn[y][i];
+        }
+      }
+    } else {  // four angles for each eight channels
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int d = d0 + y * (D / 2);
+        float4 c = make_float4(1.f, 1.f, 1.f, 1.f), s = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (d < p.rot) {
+          c = *reinterpret_cast<const float4*>(t + d / 2);
+          s = *reinterpret_cast<const float4*>(t + half + d / 2);
+        }
+        cs[0][4 * y] = c.x, cs[0][4 * y + 1] = c.y, cs[0][4 * y + 2] = c.z, cs[0][4 * y + 3] = c.w;
+        sn[0][4 * y] = s.x, sn[0][4 * y + 1] = s.y, sn[0][4 * y + 2] = s.z, sn[0][4 * y + 3] = s.w;
+      }
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) cs[i] = 1.f, sn[i] = 0.f;
   }
   const uint16_t* wp = kind == 0 ? p.qw : kind == 1 ? p.kw : nullptr;
-  float w[8];
-  if (wp) unpack8(*reinterpret_cast<const uint4*>(wp + d0), w);
-  // the lane that holds the other channels of this lane's pairs
-  const int other = !turns || PAIRS ? lane : (d0 < p.rot / 2 ? lane + p.rot / 16 : lane - p.rot / 16);
 
   uint8_t* codes = nullptr;  // the token's rows of the first head
   __half2* params = nullptr;
@@ -159,57 +184,102 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
     }
   }
 
-  constexpr int kBatch = 4;  // loads in flight per lane
+  constexpr int kBatch = 2;  // rows in flight per lane
+#pragma unroll 1
   for (int it = 0; it < p.iters; it += kBatch) {
-    uint4 in[kBatch];
+    uint4 in[kBatch][2];
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
       const int h = h0 + (it + j) * GW;
-      in[j] = make_uint4(0, 0, 0, 0);
-      if (it + j < p.iters && h < h1) in[j] = *reinterpret_cast<const uint4*>(src + (int64_t)h * D + d0);
+      in[j][0] = in[j][1] = make_uint4(0, 0, 0, 0);
+      if (it + j < p.iters && h < h1) {
+        in[j][0] = *reinterpret_cast<const uint4*>(src + (int64_t)h * D + d0);
+        in[j][1] = *reinterpret_cast<const uint4*>(src + (int64_t)h * D + D / 2 + d0);
+      }
     }
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
       const int h = h0 + (it + j) * GW;
       if (it + j >= p.iters || h - gi >= h1) break;  // the same in the whole warp
-      float x[8];
-      unpack8(in[j], x);
+      float x[2][8];
+      unpack8(in[j][0], x[0]);
+      unpack8(in[j][1], x[1]);
       if (wp) {
-        float s = __fadd_rn(__fadd_rn(__fadd_rn(__fmul_rn(x[0], x[0]), __fmul_rn(x[1], x[1])),
-                                      __fadd_rn(__fmul_rn(x[2], x[2]), __fmul_rn(x[3], x[3]))),
-                            __fadd_rn(__fadd_rn(__fmul_rn(x[4], x[4]), __fmul_rn(x[5], x[5])),
-                                      __fadd_rn(__fmul_rn(x[6], x[6]), __fmul_rn(x[7], x[7]))));
+        float s[2];
 #pragma unroll
-        for (int d = 1; d < LH; d <<= 1) s = __fadd_rn(s, __shfl_xor_sync(0xffffffffu, s, d));
-        const float rs = __fdiv_rn(1.f, __fsqrt_rn(__fadd_rn(__fmul_rn(s, 1.f / D), p.eps)));
+        for (int y = 0; y < 2; ++y) {
+          s[y] = __fadd_rn(__fadd_rn(__fadd_rn(__fmul_rn(x[y][0], x[y][0]), __fmul_rn(x[y][1], x[y][1])),
+                                     __fadd_rn(__fmul_rn(x[y][2], x[y][2]), __fmul_rn(x[y][3], x[y][3]))),
+                           __fadd_rn(__fadd_rn(__fmul_rn(x[y][4], x[y][4]), __fmul_rn(x[y][5], x[y][5])),
+                                     __fadd_rn(__fmul_rn(x[y][6], x[y][6]), __fmul_rn(x[y][7], x[y][7]))));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = __fmul_rn(__fmul_rn(x[i], rs), w[i]);
+          for (int d = 1; d < LH; d <<= 1) s[y] = __fadd_rn(s[y], __shfl_xor_sync(0xffffffffu, s[y], d));
+        }
+        const float rs = __frcp_rn(__fsqrt_rn(__fadd_rn(__fmul_rn(__fadd_rn(s[0], s[1]), 1.f / D), p.eps)));
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          float w[8];
+          unpack8(__ldg(reinterpret_cast<const uint4*>(wp + y * (D / 2) + d0)), w);
+#pragma unroll
+          for (int i = 0; i < 8; i += 2)
+            apart(mul2(mul2(two(x[y][i], x[y][i + 1]), two(rs, rs)), two(w[i], w[i + 1])), x[y][i], x[y][i + 1]);
+        }
       }
       if (kind < 2) {
-        // a * cos - b * sin and b * cos + a * sin: the sign of a product or a sum of rounded
-        // products changes no bit of it
-        float y[8];
+        // a * cos - b * sin and b * cos + a * sin, unpacked: a packed product and sum would become one
+        // fused operation.  The sign of a product or of a sum of rounded products changes no bit of it.
+        if constexpr (TURN == kTurnHalf) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = PAIRS ? x[i ^ 1] : __shfl_sync(0xffffffffu, x[i], other);
-        if (turns) {
+          for (int i = 0; i < 8; ++i) {
+            const float a = x[0][i], b = x[1][i];
+            x[0][i] = __fsub_rn(__fmul_rn(a, cs[0][i]), __fmul_rn(b, sn[0][i]));
+            x[1][i] = __fadd_rn(__fmul_rn(b, cs[0][i]), __fmul_rn(a, sn[0][i]));
+          }
+        } else if constexpr (TURN == kTurnShort) {
+          // chunk c of eight channels turns with c + rot / 16 or c - rot / 16, in the lane c % LH
+          const int hc = p.rot / 16;
+          float o[2][8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = __fadd_rn(__fmul_rn(x[i], cs[i]), __fmul_rn(y[i], sn[i]));
+          for (int y = 0; y < 2; ++y) {
+            const int c = gl + y * LH, pc = c >= 2 * hc ? c : c < hc ? c + hc : c - hc;
+            const int from = gi * LH + pc % LH;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float a = __shfl_sync(0xffffffffu, x[0][i], from), b = __shfl_sync(0xffffffffu, x[1][i], from);
+              o[y][i] = pc < LH ? a : b;
+            }
+          }
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+            if (d0 + y * (D / 2) < p.rot)
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                x[y][i] = __fadd_rn(__fmul_rn(x[y][i], cs[y][i]), __fmul_rn(o[y][i], sn[y][i]));
+        } else {
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+            if (d0 + y * (D / 2) < p.rot)
+#pragma unroll
+              for (int i = 0; i < 8; i += 2) {
+                const float a = x[y][i], b = x[y][i + 1], c = cs[0][4 * y + i / 2], s = sn[0][4 * y + i / 2];
+                x[y][i] = __fsub_rn(__fmul_rn(a, c), __fmul_rn(b, s));
+                x[y][i + 1] = __fadd_rn(__fmul_rn(b, c), __fmul_rn(a, s));
+              }
         }
       }
       const bool there = h < h1;
-      if (kind == 0) {
-        if (there)
-          *reinterpret_cast<uint4*>(p.q_out + ((int64_t)token * p.heads + h) * D + d0) = pack8(x);
-      } else if constexpr (CACHE) {
+      if (CACHE && kind > 0) {
         __half2 par;
-        const uint32_t n = quantize<LH>(x, &par);
+        const uint2 n = quantize<LH>(x, &par);
         if (there && codes) {
-          *reinterpret_cast<uint32_t*>(codes + h * block) = n;
+          *reinterpret_cast<uint32_t*>(codes + h * block) = n.x;
+          *reinterpret_cast<uint32_t*>(codes + h * block + D / 4) = n.y;
           if (gl == 0) *reinterpret_cast<__half2*>(reinterpret_cast<uint8_t*>(params) + h * block) = par;
         }
-      } else {
-        if (there)
-          *reinterpret_cast<uint4*>(p.k_out + ((int64_t)token * p.kv_heads + h) * D + d0) = pack8(x);
+      } else if (there) {
+        uint16_t* dst = (kind == 0 ? p.q_out + ((int64_t)token * p.heads + h) * D : p.k_out + ((int64_t)token * p.kv_heads + h) * D) + d0;
+        *reinterpret_cast<uint4*>(dst) = pack8(x[0]);
+        *reinterpret_cast<uint4*>(dst + D / 2) = pack8(x[1]);
       }
     }
   }
@@ -280,10 +350,10 @@ sp_status check_cache(const sp_kv4* c) {
   return al16(c->data) ? SP_OK : SP_ERR_ALIGNMENT;
 }
 
-template <int D>
-sp_status launch_rope(const RopeParams& p, bool pairs, bool cache, int64_t warps, cudaStream_t stream) {
-  auto kern = cache ? (pairs ? rope_kernel<D, true, true> : rope_kernel<D, false, true>)
-                    : (pairs ? rope_kernel<D, true, false> : rope_kernel<D, false, false>);
+template <int D, bool CACHE>
+sp_status launch_rope(const RopeParams& p, bool pairs, int64_t warps, cudaStream_t stream) {
+  auto kern = pairs ? rope_kernel<D, kTurnPairs, CACHE>
+                    : p.rot == D ? rope_kernel<D, kTurnHalf, CACHE> : rope_kernel<D, kTurnShort, CACHE>;
   const int64_t blocks = (warps + kRopeThreads / 32 - 1) / (kRopeThreads / 32);
   return launch_pdl(kern, dim3((unsigned)blocks), kRopeThreads, 0, 1, stream, p);
 }
@@ -345,7 +415,7 @@ sp_status sp_qk_norm_rope(const sp_rope_args* a, void* stream) {
   p.rot = a->rot;
   p.status = device_status_ptr();
   // heads per warp: as many as still leave every SM its warps
-  const int gw = 32 / ((int)dim / 8);
+  const int gw = 32 / ((int)dim / 16);
   const int64_t nq = (a->heads + gw - 1) / gw, nk = (a->kv_heads + gw - 1) / gw;
   const int64_t total = a->tokens * (nq + (a->cache ? 2 : 1) * nk);
   const int64_t iters = total / ((int64_t)sms * 48);
@@ -355,8 +425,10 @@ sp_status sp_qk_norm_rope(const sp_rope_args* a, void* stream) {
   p.units = p.uq + (a->cache ? 2 : 1) * p.uk;
   const int64_t warps = (int64_t)a->tokens * p.units;
   if (warps / (kRopeThreads / 32) >= ((int64_t)1 << 31) - 1) return SP_ERR_UNSUPPORTED;
-  return dim == 64 ? launch_rope<64>(p, a->pairs != 0, a->cache != nullptr, warps, (cudaStream_t)stream)
-                   : launch_rope<128>(p, a->pairs != 0, a->cache != nullptr, warps, (cudaStream_t)stream);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (dim == 64)
+    return a->cache ? launch_rope<64, true>(p, a->pairs != 0, warps, st) : launch_rope<64, false>(p, a->pairs != 0, warps, st);
+  return a->cache ? launch_rope<128, true>(p, a->pairs != 0, warps, st) : launch_rope<128, false>(p, a->pairs != 0, warps, st);
 }
 
 sp_status sp_kv4_read(const sp_kv4* c, const int64_t* slots, int64_t n, void* k_out, void* v_out, void* stream) {

@@ -77,8 +77,9 @@ def quantize(x):
     with np.errstate(all="ignore"):
         lo, hi = x.min(-1, keepdims=True), x.max(-1, keepdims=True)
         bad = ~np.isfinite(x).all(-1, keepdims=True)
-        m = np.where(bad, f32(np.nan), np.clip(lo, f32(-65504), f32(65504))).astype(np.float16)
-        s = np.where(bad, f32(0), np.clip((hi - lo) * f32(1 / 15), f32(0), f32(65504))).astype(np.float16)
+        lo, hi = np.clip(lo, f32(-32768), f32(32768)), np.clip(hi, f32(-32768), f32(32768))
+        m = np.where(bad, f32(np.nan), lo).astype(np.float16)
+        s = np.where(bad, f32(0), (hi - lo) * f32(1 / 15)).astype(np.float16)
         sf, mf = s.astype(f32), m.astype(f32)
         n = np.clip(np.rint((x - mf) * (f32(1) / sf)), f32(0), f32(15))
         n = np.where(sf > 0, n, f32(0))
