@@ -62,7 +62,7 @@ typedef struct sp_kv_plan_args {
   int32_t* next_count;       /* [1] its height after the step (may be free_count)                    */
   int32_t* lens;             /* [requests] tokens after the step (may be `cached`)                   */
   int32_t* cu_q;             /* [requests + 1] first of the step's tokens of each request, their sum */
-  int32_t* work;             /* [2 * (requests + 1)] shares of sp_kv4_attend, of its own format      */
+  int32_t* work;             /* [3 * (requests + 1)] shares of sp_kv4_attend, of its own format      */
   int64_t* slots;            /* [max_tokens] slot of each of the step's tokens; -1 behind the last   */
   int32_t* positions;        /* [max_tokens] position in its request; 0 behind the last              */
   int32_t* status;           /* [1] 0, or why the step does not fit: a sum of SP_PLAN_*              */

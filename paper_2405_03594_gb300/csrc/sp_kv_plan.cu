@@ -4,8 +4,10 @@
 // A few kilobytes move, so the time is latency: one CTA takes the requests 1024 at a time, two
 // passes over their lengths.  The first adds up what the step needs, and whether it fits; the second
 // has the exclusive sums (one shuffle scan for all five quantities) at which each request's pages
-// and tokens begin.  Pages go on the stack before others come off it.  Slots are filled by token: a
-// binary search among the sums finds a token's request.
+// and tokens begin, and puts the pages of ended requests on the stack.  Slots are filled by token, where
+// there are many by a grid of their own; a token whose page is new finds it on the stack, and the page's
+// first token writes it to the table.  A warp looks for the request of its first token among 32
+// shares at a time, and then among 32 requests, so that a search is few loads.
 #include <climits>
 
 #include "sp_kv4.cuh"
@@ -68,24 +70,57 @@ __device__ __forceinline__ void each_page(int n, int64_t key, F f) {
     for (int j = 0; j < n; ++j) f(key, j);
 }
 
-// Slot and position of token t; cu[0..requests] are the sums.
-__device__ __forceinline__ void fill_token(const sp_kv_plan_args& a, int shift, const volatile int32_t* cu, int64_t t) {
-  if (t >= cu[a.requests]) {
+// Slot and position of the warp's tokens t (one per lane, in a row); cu[0..requests] are the sums.
+__device__ __forceinline__ void fill_tokens(const sp_kv_plan_args& a, int shift, const int32_t* cu, int64_t t) {
+  const int lane = threadIdx.x & 31, total = cu[a.requests];
+  const int64_t t0 = t - lane;
+  if (t0 < total) {
+    // the first token's request: among 32 shares at a time, then 32 requests, one per lane
+    int lo = 0, n = a.requests;
+    while (n > 32) {
+      const int step = (n + 31) / 32, at = min(n, (lane + 1) * step);
+      const unsigned past = __ballot_sync(0xffffffffu, cu[lo + at] > t0);
+      const int k = __ffs(past) - 1;
+      lo += k * step;
+      n = min(step, n - k * step);
+    }
+    const int end = cu[min(lo + lane + 1, a.requests)];
+    int b = 0;  // requests of the 32 that end at or before the lane's token
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1)
+      if (__shfl_sync(0xffffffffu, end, b + d - 1) <= t) b += d;
+    if (__shfl_sync(0xffffffffu, end, 31) <= t) b = 32;
+    b += lo;
+    if (t < total) {
+      if (b == lo + 32) {  // further on
+        int hi = a.requests;
+        while (hi - b > 1) {
+          const int mid = (b + hi) >> 1;
+          if (cu[mid] <= t) b = mid;
+          else hi = mid;
+        }
+      }
+      const int32_t *lens = a.lens, *work = a.work, *free_pages = a.free_pages;
+      const int len = lens[b], at = cu[b], pos = len - (cu[b + 1] - (int)t), j = pos >> shift;
+      int32_t* entry = a.table + (int64_t)b * a.width + j;
+      int page;
+      // a page that begins among the new tokens comes off the stack; its first token extends the table
+      const int cached = pos - ((int)t - at);
+      if (free_pages && j >= (int)(((int64_t)cached + ((int64_t)1 << shift) - 1) >> shift)) {
+        page = free_pages[work[2 * (a.requests + 1) + b] - j];
+        if ((pos & ((1 << shift) - 1)) == 0) *entry = page;
+      } else {
+        page = *entry;
+      }
+      a.slots[t] = ((int64_t)page << shift) + (pos & ((1 << shift) - 1));
+      a.positions[t] = pos;
+      return;
+    }
+  }
+  if (t < a.max_tokens) {
     a.slots[t] = -1;
     a.positions[t] = 0;
-    return;
   }
-  int lo = 0, hi = a.requests;  // cu[lo] <= t < cu[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (cu[mid] <= t) lo = mid;
-    else hi = mid;
-  }
-  const volatile int32_t* lens = a.lens;
-  const int pos = lens[lo] - (cu[lo + 1] - (int)t);
-  const int page = *(const volatile int32_t*)(a.table + (int64_t)lo * a.width + (pos >> shift));
-  a.slots[t] = ((int64_t)page << shift) + (pos & ((1 << shift) - 1));
-  a.positions[t] = pos;
 }
 
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constant__ sp_kv_plan_args a, int shift,
@@ -101,11 +136,13 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
   if (tid < 4) s_sum[tid] = 0;
   if (tid == 0) s_bad = height < 0 || height > a.pages ? SP_PLAN_INPUT : 0;
   __syncthreads();
+  Request own = {};  // of a batch of one chunk, read once
   {
     int64_t sum[4] = {};
     int bad = 0;
     for (int b = tid; b < a.requests; b += kPlanThreads) {
       const Request r = request_at(a, shift, b);
+      own = r;
       bad |= r.bad;
       if (allocate && !r.gone) sum[0] += r.after - r.before;
       if (allocate && r.gone) sum[1] += r.before;
@@ -144,7 +181,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
     for (int b0 = 0; b0 < a.requests; b0 += kPlanThreads) {
       const int b = b0 + tid;
       Request r = {};
-      if (b < a.requests && !bad) r = request_at(a, shift, b);
+      if (b < a.requests && !bad) r = one ? own : request_at(a, shift, b);
       const int v[5] = {allocate && !r.gone ? (int)(r.after - r.before) : 0, allocate && r.gone ? (int)r.before : 0,
                         (int)r.add, (int)units_of(r, a.group), (int)pairs_of(r, a.group)};
       int x[5];
@@ -174,24 +211,17 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
       __syncthreads();
 #pragma unroll
       for (int k = 0; k < 5; ++k) x[k] += base[k] + s_warp[warp][k];
-      if (phase == 0) {
+      if (phase == 0)
         each_page(v[1], ((int64_t)b << 32) | (uint32_t)x[1], [&](int64_t key, int j) {
-          const int64_t rb = key >> 32;
-          a.free_pages[height + (int32_t)key + j] = a.table[rb * a.width + j];
+          a.free_pages[height + (int32_t)key + j] = a.table[(key >> 32) * a.width + j];
         });
-      } else {
-        if (allocate)
-          each_page(v[0], ((int64_t)b << 32) | (uint32_t)x[0], [&](int64_t key, int j) {
-            const int64_t rb = key >> 32;
-            // the first new page of the request: its length before the step, read again
-            const Request q = request_at(a, shift, (int)rb);
-            a.table[rb * a.width + q.before + j] =
-                *(volatile int32_t*)(a.free_pages + (top - 1 - ((int32_t)key + j)));
-          });
+      if (phase == 1) {
         if (b < a.requests) {
           a.cu_q[b + 1] = x[2] + v[2];
           a.work[b + 1] = x[3] + v[3];
           a.work[a.requests + 2 + b] = x[4] + v[4];
+          // where its new pages are on the stack: page j of the request at this less j
+          a.work[2 * (a.requests + 1) + b] = (int32_t)(top - 1 - x[0] + r.before);
           if (b < kCuShared) s_cu[b + 1] = x[2] + v[2];
         }
       }
@@ -210,26 +240,18 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
     __syncthreads();
   }
   // lengths last: they may be written over the ones that the passes above read
-  for (int b = tid; b < a.requests; b += kPlanThreads) {
-    int32_t n;
-    if (bad) {
-      n = a.cached[b];
-    } else {
-      n = (int32_t)request_at(a, shift, b).len;
-    }
-    a.lens[b] = n;
-  }
+  for (int b = tid; b < a.requests; b += kPlanThreads)
+    a.lens[b] = bad ? a.cached[b] : (int32_t)(one ? own : request_at(a, shift, b)).len;
   __syncthreads();
   if (fill) {
-    const volatile int32_t* cu = a.requests <= kCuShared ? s_cu : a.cu_q;
-    for (int64_t t = tid; t < a.max_tokens; t += kPlanThreads) fill_token(a, shift, cu, t);
+    const int32_t* cu = a.requests <= kCuShared ? s_cu : a.cu_q;
+    for (int64_t t = tid; t < (a.max_tokens + 31) / 32 * 32; t += kPlanThreads) fill_tokens(a, shift, cu, t);
   }
 }
 
 __global__ void __launch_bounds__(kFillThreads) fill_kernel(const __grid_constant__ sp_kv_plan_args a, int shift) {
   pdl_wait();
-  const int64_t t = blockIdx.x * (int64_t)kFillThreads + threadIdx.x;
-  if (t < a.max_tokens) fill_token(a, shift, a.cu_q, t);
+  fill_tokens(a, shift, a.cu_q, blockIdx.x * (int64_t)kFillThreads + threadIdx.x);
 }
 
 }  // namespace

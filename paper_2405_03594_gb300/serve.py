@@ -218,7 +218,7 @@ class Batch:
         self._next_count = torch.zeros(1, **i32)
         self.lens, self.next_count = self._lens, self._next_count
         self.cu_q = torch.zeros(requests + 1, **i32)
-        self.work = torch.zeros(2 * (requests + 1), **i32)
+        self.work = torch.zeros(3 * (requests + 1), **i32)
         self.slots = torch.full((tokens,), -1, dtype=torch.int64, device=dev)
         self.positions = torch.zeros(tokens, **i32)
         self.status = torch.zeros(1, **i32)
