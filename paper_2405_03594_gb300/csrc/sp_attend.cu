@@ -38,9 +38,11 @@ constexpr int kMinUnits = 8;  // units of a CTA, before more CTAs share the work
 
 // Warps of a CTA, stages of a warp's ring and place of its query operands, for NT tiles of eight query
 // rows: what the registers and shared memory of an SM hold.
-constexpr int warps_of(int d, int nt) { return nt == 1 ? 16 : nt == 2 ? (d == 64 ? 12 : 8) : d == 64 ? 8 : 6; }
-constexpr int stages_of(int d, int nt) { return d == 64 ? 4 : nt == 1 ? 2 : nt == 2 ? 4 : 3; }
-constexpr bool queries_shared(int d, int nt) { return nt == 4; }
+constexpr int warps_of(int d, int nt) { return nt == 1 || d == 64 ? 12 : nt < 4 ? 8 : 6; }
+constexpr int stages_of(int d, int nt) {
+  return d == 64 ? (nt == 4 ? 2 : nt == 3 ? 3 : 4) : nt == 1 || nt == 4 ? 3 : nt == 2 ? 4 : 2;
+}
+constexpr bool queries_shared(int d, int nt) { return nt > 2; }
 
 __device__ __forceinline__ float lg2(float x) {
   float r;
@@ -188,6 +190,21 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
   __syncwarp();
   pdl_wait();
 
+  // 32 requests from wb on, one per lane: where their units end, lengths, rows of q
+  int wb = 0, w_end, w_len, w_q0, w_q1, w_base;
+  auto window = [&] {
+    const int b = wb + lane;
+    w_base = p.work[wb];
+    w_end = b < p.requests ? p.work[b + 1] : INT_MAX;
+    w_len = b < p.requests ? p.lens[b] : 0;
+    w_q0 = b < p.requests ? p.cu_q[b] : 0;
+    w_q1 = b < p.requests ? p.cu_q[b + 1] : 0;
+  };
+  // the loads that do not need the list's length go out with the one that gives it
+  const int step0 = (p.requests + 31) / 32;
+  int probe = 0;
+  if (p.requests > 32) probe = p.work[min(p.requests, (lane + 1) * step0)];
+  else window();
   const int heads = p.cache.heads;
   const int64_t all = (int64_t)p.work[p.requests] * heads;
   const int total = (int)min(all, (int64_t)INT_MAX);
@@ -210,31 +227,22 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
 
   if (w0 < w1) {
     // ---------------------------------------------------------------- the copies
-    // 32 requests from wb on, one per lane: where their units end, lengths, rows of q
-    int wb = 0, w_end, w_len, w_q0, w_q1, w_base;
-    auto window = [&] {
-      const int b = wb + lane;
-      w_base = p.work[wb];
-      w_end = b < p.requests ? p.work[b + 1] : INT_MAX;
-      w_len = b < p.requests ? p.lens[b] : 0;
-      w_q0 = b < p.requests ? p.cu_q[b] : 0;
-      w_q1 = b < p.requests ? p.cu_q[b + 1] : 0;
-    };
     if (p.requests > 32) {
       // a window that holds the first unit's request: 32 shares at a time
       int lo = 0, n = p.requests;
       const int first = w0 / heads;
-      while (n > 32) {
-        const int step = (n + 31) / 32;
-        const int at = lo + min(n, (lane + 1) * step);
-        const unsigned past = __ballot_sync(0xffffffffu, p.work[at] > first);
+      for (int step = step0;;) {
+        const unsigned past = __ballot_sync(0xffffffffu, probe > first);
         const int k = past ? __ffs(past) - 1 : 31;
         n = min(step, n - min(n, k * step));
         lo += k * step;
+        if (n <= 32) break;
+        step = (n + 31) / 32;
+        probe = p.work[lo + min(n, (lane + 1) * step)];
       }
-      wb = min(lo, p.requests - 1);
+      wb = max(0, min(lo, p.requests - 1));
+      window();
     }
-    window();
     Segment ps = {};
     int pw = w0, p_end = w0, pu = 0;         // the next unit; where its segment ends; its place there
     int p_b = 0, p_len = 0;                  // its request, that one's tokens
@@ -350,7 +358,7 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
       ++pw;
       ++pending;
     };
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < S; ++i) issue();
     __syncwarp();
 
@@ -871,9 +879,13 @@ sp_status sp_kv4_attend(const sp_attend_args* a, void* workspace_dev, size_t wor
     if (st != SP_OK) return st;
   }
   const int64_t rows = std::min<int64_t>(most, kRowTile);
-  const int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
-  if (d == 64) return nt == 1 ? launch<64, 1>(p, s) : nt == 2 ? launch<64, 2>(p, s) : launch<64, 4>(p, s);
-  return nt == 1 ? launch<128, 1>(p, s) : nt == 2 ? launch<128, 2>(p, s) : launch<128, 4>(p, s);
+  const int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= 24 ? 3 : 4;
+  switch (nt) {
+    case 1: return d == 64 ? launch<64, 1>(p, s) : launch<128, 1>(p, s);
+    case 2: return d == 64 ? launch<64, 2>(p, s) : launch<128, 2>(p, s);
+    case 3: return d == 64 ? launch<64, 3>(p, s) : launch<128, 3>(p, s);
+  }
+  return d == 64 ? launch<64, 4>(p, s) : launch<128, 4>(p, s);
 }
 
 }  // extern "C"
