@@ -807,7 +807,8 @@ int grid_of() {
 }
 
 size_t workspace_bytes(int head_dim, int sms) {
-  return ws_counter_bytes(sms) + (size_t)sms * 2 * kRowTile * (size_t)(head_dim + 4) * sizeof(float);
+  return ws_counter_bytes(sms) + std::max((size_t)sms * 2 * kRowTile * (size_t)(head_dim + 4) * sizeof(float),
+                                          attend_rows_part_bytes(head_dim, sms));
 }
 
 template <int D, int NT>

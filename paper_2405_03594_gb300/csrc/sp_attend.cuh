@@ -16,7 +16,9 @@ struct AttendParams {
   int64_t tokens;
   int32_t group_inverse;  // 2^16 / group, rounded up
   float scale_log2;
-  float* part;  // attend_kernel: [2 grid][8 NT] of (D sums, maximum, sum of weights, unused)
+  float* part;    // attend_kernel: [2 grid][8 NT] of (D sums, maximum, sum of weights, unused);
+                  // attend_rows_kernel: [items][split] of 256 columns of (D sums, maximum, sum of weights)
+  int32_t split, parts;  // attend_rows_kernel: shares of an item, at most; shares that `part` holds
   int* cnt;     // attend_kernel: [grid] arrivals; attend_rows_kernel: its next item, CTAs that are done
   int32_t* status;
   uint64_t timeout_ns;
@@ -64,6 +66,7 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
 }
 
 // attend_rows_kernel over the requests that the plan gave to it (sp_attend_rows.cu).
-sp_status launch_attend_rows(const AttendParams& p, int head_dim, cudaStream_t stream);
+sp_status launch_attend_rows(AttendParams p, int head_dim, cudaStream_t stream);
+size_t attend_rows_part_bytes(int head_dim, int sms);  // of the shares that it joins
 
 }  // namespace sp

@@ -15,10 +15,14 @@
 //   warps 12, 13     issue a tile's products each
 //   warp 14          copies of the codes, and the next item
 //
-// Measured, 32 heads of 128, two prompts of up to 2048 tokens behind a prefix (4 x 24e9 operations): 138 us,
-// 0.70 PFLOP/s, 0.37 of the measured bf16 rate.  A step of a tile is a chain -- scores read 0.13 us,
+// Measured, 32 heads of 128, two prompts of up to 2048 tokens behind a prefix (4 x 24e9 operations): 142 us,
+// 0.68 PFLOP/s, 0.36 of the measured bf16 rate.  A step of a tile is a chain -- scores read 0.13 us,
 // exponentials 0.5 (the special-function units' rate), weights' products and the next scores 0.55,
 // and four barriers -- of which the two tiles overlap about half.
+//
+// Split.  Pairs of tiles are taken from one list, later rows (which see more) first.  Where there are
+// fewer pairs than SMs, each one's steps of keys are cut into shares, whose sums join_rows_kernel adds up
+// in order: twelve tokens behind 8000, 8 key heads, 130 us uncut, 42 in shares.
 //
 // Numbers.  s n + m is rounded once to fp16 (the cache holds |x| <= 2^15); the queries, bf16, enter
 // exactly, each row scaled by a power of two.  The running maximum of a row moves only when
@@ -41,6 +45,8 @@ constexpr int kFillWarps = 4;
 constexpr int kBusyThreads = kRowThreads + 32 * kFillWarps + 96;
 constexpr int kThreads = 512;             // whole warpgroups, as the division of the registers wants them
 constexpr int kStages = 2;
+constexpr int kMostShares = 16;
+constexpr int kShareSteps = 3;            // of keys, least of a share where an item is cut
 constexpr int kMaxDevices = 64;
 constexpr uint32_t kPanel = kTile * 128;  // 128 rows of 64 columns
 
@@ -121,7 +127,61 @@ struct Item {
   int row0, rows;   // first query row among the request's, query rows
   int sees0;        // keys that new token 0 sees
   int len;
+  int j0, j1;       // steps of keys of this share
+  int part;         // the share's place in the workspace; -1: it holds all steps
 };
+
+// Steps of keys that the rows of the item's tile i see, all shares together.
+__device__ __forceinline__ int all_steps(const AttendParams& p, const Item& it, int i) {
+  const int rows = min(it.rows - i * kTile, kTile);
+  return rows > 0 ? (it.sees0 + (it.row0 + i * kTile + rows - 1) / p.group + kTile - 1) / kTile : 0;
+}
+// Of them, those of this share.
+__device__ __forceinline__ int steps_of(const AttendParams& p, const Item& it, int i) {
+  return max(0, min(all_steps(p, it, i), it.j1) - it.j0);
+}
+
+// Item i of the list: pairs of tiles of all requests, later rows, which see more, first.  Rows 0 behind the
+// last, -1 where the shares do not belong to the lengths.  shares: into how many its steps are cut.
+__device__ __forceinline__ Item item_at(const AttendParams& p, int64_t i, int& shares) {
+  const int32_t* share = p.work + p.requests + 1;  // pairs of tiles of the requests before each
+  const int heads = p.cache.heads;
+  Item it;
+  it.rows = 0;
+  shares = 1;
+  if (i >= (int64_t)share[p.requests] * heads) return it;
+  const int pair = (int)(i / heads);
+  int lo = 0, hi = p.requests;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (share[mid] <= pair) lo = mid;
+    else hi = mid;
+  }
+  it.b = lo;
+  it.h = (int)(i % heads);
+  it.q0 = p.cu_q[lo];
+  it.len = p.lens[lo];
+  const int fresh = p.cu_q[lo + 1] - it.q0, pairs = share[lo + 1] - share[lo];
+  const int64_t all = (int64_t)fresh * p.group;
+  if (fresh <= 0 || it.len < fresh || fresh > p.max_new || it.q0 < 0 || it.q0 + (int64_t)fresh > p.tokens ||
+      (all + 2 * kTile - 1) / (2 * kTile) != pairs) {
+    set_status(p.status, kStatusBadIndex);
+    it.rows = -1;
+    return it;
+  }
+  it.row0 = (pairs - 1 - (pair - share[lo])) * 2 * kTile;
+  it.rows = (int)min(all - it.row0, (int64_t)(2 * kTile));
+  it.sees0 = it.len - fresh + 1;
+  it.j0 = 0;
+  it.j1 = max(all_steps(p, it, 0), all_steps(p, it, 1));
+  it.part = -1;
+  shares = min(p.split, (it.j1 + kShareSteps - 1) / kShareSteps);
+  if (shares > 1 && (i + 1) * p.split > p.parts) {  // rows of q that the host did not count
+    set_status(p.status, kStatusBadIndex);
+    shares = 1;
+  }
+  return it;
+}
 
 struct Barriers {
   uint64_t q_full, k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
@@ -154,12 +214,6 @@ struct Wait {
   }
 };
 
-// Steps of keys that the rows of the item's tile i see.
-__device__ __forceinline__ int steps_of(const AttendParams& p, const Item& it, int i) {
-  const int rows = min(it.rows - i * kTile, kTile);
-  return rows > 0 ? (it.sees0 + (it.row0 + i * kTile + rows - 1) / p.group + kTile - 1) / kTile : 0;
-}
-
 // The end of an item for every warp that works on it; false once a wait has expired.
 __device__ __forceinline__ bool end_item(Shared& sh, const Wait& wait) {
   if (wait.dead) sh.dead = 1;
@@ -181,15 +235,16 @@ __device__ __forceinline__ void rows_role(const AttendParams& p, Shared& sh, uin
   Wait wait{p};
   uint32_t steps = 0, done = 0;
   for (uint32_t round = 0;; ++round) {
-    const Item it = sh.item[round & 1];
+    const Item& it = sh.item[round & 1];  // (in shared memory: registers are what this role is short of)
     if (it.rows <= 0) break;
     const int n = steps_of(p, it, i);
-    const bool there = i * kTile + r < it.rows;
-    const int row = it.row0 + i * kTile + r, token = row / p.group;
-    const int limit = there ? it.sees0 + token : 0;  // keys that the row sees
-    const int64_t col = (int64_t)(it.h * p.group + row - token * p.group) * D;
-    float cr;  // log2 score = cr * product
+    int limit;  // keys of the share that the row sees
+    float cr;   // log2 score = cr * product
     {
+      const bool there = i * kTile + r < it.rows;
+      const int row = it.row0 + i * kTile + r, token = row / p.group;
+      const int64_t col = (int64_t)(it.h * p.group + row - token * p.group) * D;
+      limit = there ? it.sees0 + token - it.j0 * kTile : 0;
       const uint4* src = reinterpret_cast<const uint4*>(p.q + (it.q0 + (int64_t)token) * p.q_stride + col);
       uint4 u[D / 8];
       uint32_t big = 0;
@@ -301,14 +356,18 @@ __device__ __forceinline__ void rows_role(const AttendParams& p, Shared& sh, uin
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.bar.p_full[i]);
     }
-    if (n > 0) {
-      wait(&sh.bar.o_done[i], (done + n - 1) & 1);
-      tc_fence_after();
-      if (!wait.dead) {
-        float a, b;
-        apart(l, a, b);
-        a += b;
-        const float inv = poisoned ? __uint_as_float(0x7fffffffu) : a == 0.f ? 0.f : 1.f / a;
+    if (n > 0) wait(&sh.bar.o_done[i], (done + n - 1) & 1);
+    tc_fence_after();
+    if (!wait.dead) {
+      float a, b;
+      apart(l, a, b);
+      a += b;
+      if (poisoned) a = __uint_as_float(0x7fffffffu);
+      if (it.part < 0) {
+        const bool there = i * kTile + r < it.rows;  // (worked out again: not kept over the steps)
+        const int row = it.row0 + i * kTile + r, token = row / p.group;
+        const int64_t col = (int64_t)(it.h * p.group + row - token * p.group) * D;
+        const float inv = a == 0.f ? 0.f : 1.f / a;
         uint16_t* dst = p.out + (it.q0 + (int64_t)token) * p.out_stride + col;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
@@ -328,6 +387,18 @@ __device__ __forceinline__ void rows_role(const AttendParams& p, Shared& sh, uin
             }
           }
         }
+      } else {  // a column per row: D sums, the maximum, the sum of weights
+        float* dst = p.part + (int64_t)it.part * (D + 2) * kPairRows + i * kTile + r;
+#pragma unroll 1
+        for (int c = 0; c < D; c += 16) {
+          uint32_t v[16];
+          if (n > 0) tmem_load16(t_o + c, v);
+          tmem_load_wait();
+#pragma unroll
+          for (int k = 0; k < 16; ++k) __stcg(dst + (c + k) * kPairRows, n > 0 ? __uint_as_float(v[k]) : 0.f);
+        }
+        __stcg(dst + D * kPairRows, m);
+        __stcg(dst + (D + 1) * kPairRows, a);
       }
     }
     steps += max(steps_of(p, it, 0), steps_of(p, it, 1));
@@ -353,7 +424,7 @@ __device__ __forceinline__ void copy_role(const AttendParams& p, Shared& sh, uin
     const int n = max(steps_of(p, it, 0), steps_of(p, it, 1));
     const int32_t* table = p.table + (int64_t)it.b * p.width;
     auto page_of = [&](int j) {  // a lane per page of step j
-      const int at = j * pages + lane;
+      const int at = (it.j0 + j) * pages + lane;
       return j < n && lane < pages && ((int64_t)at << shift) < it.len ? (at < p.width ? table[at] : -1) : INT_MIN;
     };
     int next = page_of(0);
@@ -410,8 +481,9 @@ __device__ __forceinline__ void fill_role(const AttendParams& p, Shared& sh, uin
   Wait wait{p};
   uint32_t steps = 0;
   for (uint32_t round = 0;; ++round) {
-    const Item it = sh.item[round & 1];
+    const Item& it = sh.item[round & 1];
     if (it.rows <= 0) break;
+    const int keys = it.len - it.j0 * kTile;  // from the share's first on
     const int n = max(steps_of(p, it, 0), steps_of(p, it, 1));
     for (int j = 0; j < n; ++j) {
       const int st = (steps + j) % kStages;
@@ -425,7 +497,7 @@ __device__ __forceinline__ void fill_role(const AttendParams& p, Shared& sh, uin
         const uint32_t* raw_par = reinterpret_cast<const uint32_t*>(raw + kTile * (D / 2));
         uint8_t* dst = which ? s_v + st * L::kV : s_k + st * L::kQ;
         const unsigned ok = sh.pages[which];
-        const int left = it.len - j * kTile;
+        const int left = keys - j * kTile;
         uint4 c4[KP];
         uint32_t par[KP];
 #pragma unroll
@@ -574,35 +646,23 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
     sh.dead = 0;
   }
   pdl_wait();
-  // the next item: later rows, which see more, first
+  // the next share of the list
   auto fetch = [&](Item& it) {
-    const int32_t* share = p.work + p.requests + 1;  // pairs of tiles of the requests before each
-    const int heads = p.cache.heads;
-    it.rows = 0;
     const int64_t i = (int64_t)atomicAdd(&p.cnt[0], 1);
-    if (i >= (int64_t)share[p.requests] * heads) return;
-    const int pair = (int)(i / heads);
-    int lo = 0, hi = p.requests;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (share[mid] <= pair) lo = mid;
-      else hi = mid;
+    int shares;
+    it = item_at(p, i / p.split, shares);
+    if (it.rows <= 0 || shares == 1) {
+      if (i % p.split > 0 && it.rows > 0) it.rows = -1;  // (its first share takes all)
+      return;
     }
-    it.b = lo;
-    it.h = (int)(i % heads);
-    it.q0 = p.cu_q[lo];
-    it.len = p.lens[lo];
-    const int fresh = p.cu_q[lo + 1] - it.q0, pairs = share[lo + 1] - share[lo];
-    const int64_t all = (int64_t)fresh * p.group;
-    if (fresh <= 0 || it.len < fresh || fresh > p.max_new || it.q0 < 0 || it.q0 + (int64_t)fresh > p.tokens ||
-        (all + 2 * kTile - 1) / (2 * kTile) != pairs) {
-      set_status(p.status, kStatusBadIndex);  // shares that do not belong to the lengths
+    const int x = (int)(i % p.split), n = it.j1;
+    if (x >= shares) {
       it.rows = -1;
       return;
     }
-    it.row0 = (pairs - 1 - (pair - share[lo])) * 2 * kTile;
-    it.rows = (int)min(all - it.row0, (int64_t)(2 * kTile));
-    it.sees0 = it.len - fresh + 1;
+    it.j0 = (int)((int64_t)x * n / shares);
+    it.j1 = (int)((int64_t)(x + 1) * n / shares);
+    it.part = (int)i;
   };
   if (tid == kBusyThreads - 32) {
     Item it;
@@ -618,12 +678,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh.tmem;
-  // registers: 128 a thread at launch, (168 + 168 + 104 + 72) / 4 from here on
+  // registers: 128 a thread at launch, (176 + 176 + 88 + 72) / 4 from here on
   if (warp < kRowThreads / 32) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
     rows_role<D>(p, sh, s_q, tmem);
   } else if (warp < kRowThreads / 32 + kFillWarps) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     fill_role<D>(p, sh, s_k, s_v, s_raw);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
@@ -647,6 +707,52 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
   }
 }
 
+// The shares of an item joined: a warp takes 32 rows, a lane each, and 16 of their channels.
+template <int D>
+__global__ void __launch_bounds__(128) join_rows_kernel(const __grid_constant__ AttendParams p) {
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  const int64_t items = (int64_t)p.work[2 * p.requests + 1] * p.cache.heads;
+  constexpr int kGroups = kPairRows / 32, kUnits = kGroups * (D / 16);
+  for (int64_t u = blockIdx.x * 4 + (threadIdx.x >> 5); u < items * kUnits; u += gridDim.x * 4) {
+    const int64_t i = u / kUnits;
+    const int r0 = (int)(u % kUnits) % kGroups * 32, c0 = (int)(u % kUnits) / kGroups * 16;
+    int shares;
+    const Item it = item_at(p, i, shares);
+    if (it.rows <= r0 || shares == 1) continue;
+    const float* src = p.part + i * p.split * (D + 2) * kPairRows + r0 + lane;
+    constexpr int64_t kNext = (int64_t)(D + 2) * kPairRows;
+    float m = -INFINITY;
+    for (int x = 0; x < shares; ++x) m = fmaxf(m, __ldcg(src + x * kNext + D * kPairRows));
+    const float safe = m == -INFINITY ? 0.f : m;
+    float sum = 0.f, acc[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) acc[k] = 0.f;
+#pragma unroll 2
+    for (int x = 0; x < shares; ++x) {
+      const float* s = src + x * kNext;
+      const float f = ex2(__ldcg(s + D * kPairRows) - safe);
+      sum = fmaf(__ldcg(s + (D + 1) * kPairRows), f, sum);
+#pragma unroll
+      for (int k = 0; k < 16; ++k) acc[k] = fmaf(__ldcg(s + (c0 + k) * kPairRows), f, acc[k]);
+    }
+    if (r0 + lane >= it.rows) continue;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int row = it.row0 + r0 + lane, token = row / p.group;
+    uint16_t* dst = p.out + (it.q0 + (int64_t)token) * p.out_stride + (int64_t)(it.h * p.group + row - token * p.group) * D + c0;
+#pragma unroll
+    for (int k = 0; k < 16; k += 8) {
+      uint32_t w[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {  // channels 0, 4, 1, 5, 2, 6, 3, 7 of eight
+        const int y = k + (x & 1) * 4 + (x >> 1);
+        w[x] = pack_bf16(acc[y] * inv, acc[y + 2] * inv);
+      }
+      *reinterpret_cast<uint4*>(dst + k) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+}
+
 template <int D>
 sp_status launch(const AttendParams& p, int sms, cudaStream_t stream) {
   static std::atomic<int> set[kMaxDevices] = {};
@@ -664,14 +770,27 @@ sp_status launch(const AttendParams& p, int sms, cudaStream_t stream) {
     return 1;
   });
   if (!ok) return SP_ERR_CUDA;
-  return launch_pdl(attend_rows_kernel<D>, dim3((unsigned)sms), kThreads, Smem<D>::kTotal, 1, stream, p);
+  const sp_status st = launch_pdl(attend_rows_kernel<D>, dim3((unsigned)sms), kThreads, Smem<D>::kTotal, 1, stream, p);
+  if (st != SP_OK || p.split == 1) return st;
+  return launch_pdl(join_rows_kernel<D>, dim3((unsigned)sms * 4), 128, 0, 1, stream, p);
 }
 
 }  // namespace
 
-sp_status launch_attend_rows(const AttendParams& p, int head_dim, cudaStream_t stream) {
+size_t attend_rows_part_bytes(int head_dim, int sms) {
+  return (size_t)sms * kPairRows * (size_t)(head_dim + 2) * sizeof(float);
+}
+
+// Where there are fewer items than SMs, the steps of keys are cut into shares.  The host does not
+// see the lengths: it goes by the most items that so many tokens can make (R requests of kManyRows
+// rows or more have sum ceil(rows / 256) <= (all rows + 255 R) / 256).
+sp_status launch_attend_rows(AttendParams p, int head_dim, cudaStream_t stream) {
   const int sms = current_sms();
   if (sms == 0) return SP_ERR_CUDA;
+  const int64_t rows = p.tokens * p.group, most = std::min<int64_t>(p.requests, rows / kManyRows);
+  const int64_t items = (rows + (kPairRows - 1) * most) / kPairRows * p.cache.heads;
+  p.parts = sms;
+  p.split = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kMostShares, sms / std::max<int64_t>(items, 1)));
   return head_dim == 64 ? launch<64>(p, sms, stream) : launch<128>(p, sms, stream);
 }
 

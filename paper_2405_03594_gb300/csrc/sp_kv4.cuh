@@ -13,7 +13,11 @@ constexpr float kKvMost = 32768.f;  // largest magnitude that the cache holds
 constexpr int kMaxGroup = 64;       // query heads per key head
 constexpr int kUnitKeys = 32;       // keys of one step of attend_kernel
 constexpr int kRowTile = 32;        // query rows (token, head of the group) of its widest form
-constexpr int kManyRows = 65;       // query rows of a request from which attend_rows_kernel takes it
+// Query rows of a request from which attend_rows_kernel takes it: every request that attend_kernel would
+// need a second row tile for.  32 heads over 8, 12 new tokens (48 rows), attend_kernel / attend_rows_kernel,
+// us: one request behind 1000 tokens 37 / 24, behind 8000 50 / 42 (130 without its steps cut into
+// shares), 16 requests 61 / 29 and 228 / 146; alone with its 12 tokens 12 / 16.
+constexpr int kManyRows = 33;
 constexpr int kPairRows = 256;      // query rows of one of its items
 constexpr int kSetupUnits = 2;      // what a segment costs beside its units, in units (64 requests of 100 to
                                     // 16384 tokens: 58.0 us at 0, 53.3 at 1, 50.2 at 2, 51.1 at 4)
