@@ -370,7 +370,8 @@ def test_several_new_tokens(sp, serve, d, heads, kv, new):
 
 
 @pytest.mark.parametrize("lens,new,heads,kv", [([20000], [1], 8, 1), ([9000, 3, 0, 700], [1, 1, 0, 1], 4, 4),
-                                               ([5000], [4], 32, 8), ([4097], [1], 32, 32)])
+                                               ([5000], [4], 32, 8), ([4097], [1], 32, 32),
+                                               ([5000], [40], 32, 8), ([3000, 90, 0], [300, 20, 0], 8, 8)])
 def test_long_contexts_are_split_and_joined(sp, serve, lens, new, heads, kv):
     g = np.random.default_rng(lens[0])
     f = Filled(serve, g, lens, new, heads, kv, 128, 64)
@@ -432,6 +433,52 @@ def test_nan_rows_reach_only_who_sees_them(sp, serve):
     w = f.want()
     assert np.isnan(w).any() and not np.isnan(w).all()
     _near(y, w, f.vmax())
+
+
+@pytest.mark.parametrize("heads,kv,new", [(8, 2, [1, 2, 1]), (8, 2, [6, 1, 8]), (4, 1, [40, 3, 90])])
+def test_queries_that_are_not_finite_or_of_far_scales(sp, serve, heads, kv, new):
+    """An infinity or NaN makes NaN of its own row alone; rows a factor of 2^40 apart do not disturb each
+    other (the queries' scaling is a power of two per row, or of the rows of a tile)."""
+    g = np.random.default_rng(21)
+    f = Filled(serve, g, [300, 40, 170], new, heads, kv, 64, 32)
+    x = synth.bf16_to_f32(f.q)
+    x[0, 1] *= np.float32(2.0 ** -20)
+    x[-1, 0] *= np.float32(2.0 ** -40)
+    x[0, 0, 3] = np.inf
+    x[1, 2, 60] = np.nan
+    x[-1, 1] = 0
+    f.q = synth.bf16_from_f32(x)
+    y = f.cache.attend(gu.bf16_to_dev(f.q), f.batch, max(new))
+    sp.check()
+    x[0, 0, 3] = x[1, 2, 60] = 0
+    f.q = synth.bf16_from_f32(x)
+    w = f.want()
+    w[0, 0] = w[1, 2] = np.nan
+    got = gu.bf16_from_dev(y)
+    assert np.isnan(got[0, 0]).all() and np.isnan(got[1, 2]).all()
+    _near(y, w, f.vmax())
+
+
+@pytest.mark.parametrize("kv,d,new", [(1, 128, 1), (2, 64, 2), (1, 128, 40), (1, 64, 300)])
+def test_flat_attention_over_a_long_context(sp, serve, kv, d, new):
+    """Weights that are nearly equal over 60000 keys: an average of many values, far below each of them."""
+    g = np.random.default_rng(22)
+    f = Filled(serve, g, [60000], [new], 4 * kv, kv, d, 128)
+    f.q = synth.bf16_from_f32((0.02 * g.standard_normal((new, 4 * kv, d))).astype(np.float32))
+    f.qd = gu.bf16_to_dev(f.q)
+    y = f.cache.attend(f.qd, f.batch, new)
+    sp.check()
+    rows = [0, new - 1]
+    f.q, f.lens, f.new = f.q[rows], [60000], [new]
+    q = synth.bf16_to_f32(f.q).astype(np.float64)
+    pg = f.table[0]
+    k, v = (ref.values(*r)[pg].transpose(0, 2, 1, 3).reshape(-1, kv, d)[:60000] for r in f.rows)
+    want = np.concatenate([ref.attend(q[i:i + 1], k[:60000 - new + r + 1], v[:60000 - new + r + 1], d ** -0.5)
+                           for i, r in enumerate(rows)])
+    got = gu.bf16_from_dev(y)[rows]
+    # means of 60000 values of size 1 about their channels' offsets: the offsets dominate
+    assert np.linalg.norm(got - want) <= 2.5e-3 * np.linalg.norm(want)
+    assert np.abs(got - want).max() <= 2.0 ** -8 * np.abs(want).max() + 1e-3
 
 
 def test_strided_queries_and_output(sp, serve):
