@@ -111,50 +111,62 @@ struct PartInfo {
   int h, q0, head0;
 };
 
-// One row of n parts, by a warp: its maximum and sum of weights (in every lane), and C of its sums.
-template <int C>
+// One row of n parts, by L lanes: its maximum and sum of weights (in each of them), and of its sums the
+// quadruples that begin at 4 (lane % L + L i).  A warp joins 32 / L rows side by side: a row's joining is a
+// chain of waits whatever its lanes, so many rows take eight lanes each (20 rows of 5 tokens over 4 heads of
+// D = 128, 16 requests: 23.9 us, by whole warps 25.8) and few rows, at most one a warp, as many as a row
+// has quadruples (one request: 12.55 us, by half warps 13.2).
+template <int Q>
 struct Row {
-  float m, sum, acc[C];
+  float m, sum;
+  float4 acc[Q];
 };
-template <int C, class Stat, class Sums>
-__device__ __forceinline__ Row<C> join(int n, Stat stat_at, Sums sums_at) {
-  const int lane = threadIdx.x & 31;
-  Row<C> r;
-  // the first 32 parts' numbers stay in registers
-  const float2 own = lane < n ? stat_at(lane) : make_float2(-INFINITY, 0.f);
+template <int Q, int L, class Stat, class Sums>
+__device__ __forceinline__ Row<Q> join(int n, Stat stat_at, Sums sums_at) {
+  constexpr int B = L == 8 ? 4 : 8;  // parts whose loads are in flight at a time
+  const int lane = threadIdx.x & 31, sub = lane & (L - 1);
+  Row<Q> r;
+  // the first L parts' numbers stay in registers
+  const float2 own = sub < n ? stat_at(sub) : make_float2(-INFINITY, 0.f);
   r.m = own.x;
-  for (int k = lane + 32; k < n; k += 32) r.m = fmaxf(r.m, stat_at(k).x);
+  for (int k = sub + L; k < n; k += L) r.m = fmaxf(r.m, stat_at(k).x);
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) r.m = fmaxf(r.m, __shfl_xor_sync(0xffffffffu, r.m, d));
+  for (int d = L / 2; d > 0; d >>= 1) r.m = fmaxf(r.m, __shfl_xor_sync(0xffffffffu, r.m, d));
   const float safe = r.m == -INFINITY ? 0.f : r.m;
   r.sum = 0.f;
 #pragma unroll
-  for (int c = 0; c < C; ++c) r.acc[c] = 0.f;
-  for (int k0 = 0; k0 < n; k0 += 32) {
+  for (int i = 0; i < Q; ++i) r.acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int most = __reduce_max_sync(0xffffffffu, n);  // (the warp's rows may belong to two segments)
+  for (int k0 = 0; k0 < most; k0 += L) {
     float f = 0.f;
-    if (k0 + lane < n) {
-      const float2 st = k0 == 0 ? own : stat_at(k0 + lane);
+    if (k0 + sub < n) {
+      const float2 st = k0 == 0 ? own : stat_at(k0 + sub);
       f = ex2(st.x - safe);
       r.sum = fmaf(st.y, f, r.sum);
     }
-    const int kn = min(32, n - k0);
-    for (int k = 0; k < kn; k += 4) {
-      Row<C> a[4];
+    const int kn = min(L, most - k0);
+    for (int k = 0; k < kn; k += B) {
+      float4 a[B][Q];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (k + i < kn) a[i] = sums_at(k0 + k + i);
+      for (int j = 0; j < B; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float fk = __shfl_sync(0xffffffffu, f, (k + i) & 31);
-        if (k + i < kn) {
+        for (int i = 0; i < Q; ++i)
+          if (k0 + k + j < n) a[j][i] = sums_at(k0 + k + j, 4 * (sub + L * i));
 #pragma unroll
-          for (int c = 0; c < C; ++c) r.acc[c] = fmaf(a[i].acc[c], fk, r.acc[c]);
+      for (int j = 0; j < B; ++j) {
+        const float fk = __shfl_sync(0xffffffffu, f, (lane & (32 - L)) + ((k + j) & (L - 1)));
+        if (k0 + k + j < n) {
+#pragma unroll
+          for (int i = 0; i < Q; ++i) {
+            r.acc[i].x = fmaf(a[j][i].x, fk, r.acc[i].x), r.acc[i].y = fmaf(a[j][i].y, fk, r.acc[i].y);
+            r.acc[i].z = fmaf(a[j][i].z, fk, r.acc[i].z), r.acc[i].w = fmaf(a[j][i].w, fk, r.acc[i].w);
+          }
         }
       }
     }
   }
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) r.sum += __shfl_xor_sync(0xffffffffu, r.sum, d);
+  for (int d = L / 2; d > 0; d >>= 1) r.sum += __shfl_xor_sync(0xffffffffu, r.sum, d);
   return r;
 }
 
@@ -678,13 +690,17 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
     if (lane == 31) s_parts = __popc(m), s_rows = rows;
   }
   __syncthreads();
-  constexpr int C = D / 32;  // channels of a lane
-  auto write_out = [&](const PartInfo& s, int r, const Row<C>& x) {
+  constexpr int L = NT == 1 ? D / 4 : 8;  // lanes of a row
+  constexpr int Q = D / 4 / L;            // quadruples of a lane
+  constexpr int A = 32 / L;               // rows of a warp
+  const int sub = lane & (L - 1), side = lane / L;
+  auto write_out = [&](const PartInfo& s, int r, const Row<Q>& x) {
     const float inv = x.sum == 0.f ? 0.f : 1.f / x.sum;
-    uint16_t* dst = q_row(s.q0, s.h, s.head0, r, p.out, p.out_stride) + lane * C;
+    uint16_t* dst = q_row(s.q0, s.h, s.head0, r, p.out, p.out_stride) + 4 * sub;
 #pragma unroll
-    for (int c = 0; c < C; c += 2)
-      *reinterpret_cast<uint32_t*>(dst + c) = pack_bf16(x.acc[c] * inv, x.acc[c + 1] * inv);
+    for (int i = 0; i < Q; ++i)
+      *reinterpret_cast<uint2*>(dst + 4 * L * i) = make_uint2(pack_bf16(x.acc[i].x * inv, x.acc[i].y * inv),
+                                                           pack_bf16(x.acc[i].z * inv, x.acc[i].w * inv));
   };
   const int parts = s_parts;
   int open[2] = {-1, -1};  // a part of the segment shared with the CTAs before, after
@@ -695,10 +711,17 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
     if (b.vis0 >= c0 && b.vis0 + b.seen > c1) open[1] = j;
   }
   const int own0 = lane < parts ? s_row0[lane] : -1;
-  for (int x = warp; x < s_rows; x += W) {
-    const unsigned m = __ballot_sync(0xffffffffu, own0 >= 0 && own0 <= x);
+  const unsigned opening = __ballot_sync(0xffffffffu, own0 >= 0);
+  for (int x0 = A * warp; x0 < s_rows; x0 += A * W) {
+    const int x = min(x0 + side, s_rows - 1);  // (a lane past the last row repeats it)
+    unsigned m = 0;                            // the parts whose segment opens at or before x
+#pragma unroll
+    for (int k = 0; k < A; ++k) {
+      const unsigned o = __ballot_sync(0xffffffffu, own0 >= 0 && own0 <= x0 + k);
+      if (k == side) m = o;
+    }
     const int i = 31 - __clz(m);  // the segment's first part
-    const unsigned after = __ballot_sync(0xffffffffu, own0 >= 0) & ~((2u << i) - 1u);
+    const unsigned after = opening & ~((2u << i) - 1u);
     const int n = (after ? __ffs(after) - 1 : parts) - i;
     const int r = x - __shfl_sync(0xffffffffu, own0, i);
     const PartInfo s = s_info[s_order[i] >> 1][s_order[i] & 1];
@@ -706,22 +729,17 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
       const int o = s_order[i + k];
       return reinterpret_cast<const float*>(smem + (o >> 1) * kWarpBytes + ((o & 1) ? 0 : kFirst)) + r * kRow;
     };
-    const Row<C> y = join<C>(
+    const Row<Q> y = join<Q, L>(
         n, [&](int k) { return *reinterpret_cast<const float2*>(at(k) + D); },
-        [&](int k) {
-          const float* src = at(k) + lane * C;
-          Row<C> a;
-#pragma unroll
-          for (int c = 0; c < C; ++c) a.acc[c] = src[c];
-          return a;
-        });
+        [&](int k, int c) { return *reinterpret_cast<const float4*>(at(k) + c); });
+    if (x0 + side >= s_rows) continue;
     if (s.vis0 >= c0 && s.vis0 + s.seen <= c1) {
       write_out(s, r, y);
     } else {
       float* part = p.part + (((int64_t)blockIdx.x * 2 + (s.vis0 < c0 ? 0 : 1)) * R + r) * kRow;
 #pragma unroll
-      for (int c = 0; c < C; ++c) __stcg(part + lane * C + c, y.acc[c]);
-      if (lane == 0) __stcg(reinterpret_cast<float2*>(part + D), make_float2(y.m, y.sum));
+      for (int c = 0; c < Q; ++c) __stcg(reinterpret_cast<float4*>(part + 4 * (sub + L * c)), y.acc[c]);
+      if (sub == 0) __stcg(reinterpret_cast<float2*>(part + D), make_float2(y.m, y.sum));
     }
   }
   // ------------------------------------------------------------------ segments shared by CTAs
@@ -754,24 +772,17 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
       ctas_of(i, f[i], e[i]);
     }
   }
-  for (int x = warp; x < s[0].rows + s[1].rows; x += W) {
+  const int all_rows = s[0].rows + s[1].rows;
+  for (int x0 = A * warp; x0 < all_rows; x0 += A * W) {
+    const int x = min(x0 + side, all_rows - 1);
     const int i = x < s[0].rows ? 0 : 1, r = x - (i ? s[0].rows : 0);
     const int first = i ? f[1] : f[0], n = (i ? e[1] : e[0]) - first + 1;
     // the segment is the first CTA's second part and the others' first
     auto at = [&](int k) { return p.part + (((int64_t)(first + k) * 2 + (k == 0 ? 1 : 0)) * R + r) * kRow; };
-    const Row<C> y = join<C>(
+    const Row<Q> y = join<Q, L>(
         n, [&](int k) { return __ldcg(reinterpret_cast<const float2*>(at(k) + D)); },
-        [&](int k) {
-          const float2* src = reinterpret_cast<const float2*>(at(k) + lane * C);
-          Row<C> a;
-#pragma unroll
-          for (int c = 0; c < C / 2; ++c) {
-            const float2 v = __ldcg(src + c);
-            a.acc[2 * c] = v.x, a.acc[2 * c + 1] = v.y;
-          }
-          return a;
-        });
-    write_out(i ? s[1] : s[0], r, y);
+        [&](int k, int c) { return __ldcg(reinterpret_cast<const float4*>(at(k) + c)); });
+    if (x0 + side < all_rows) write_out(i ? s[1] : s[0], r, y);
   }
   if (tid < 2 && s_last[tid]) atomicExch(&p.cnt[tid ? f[1] : f[0]], 0);
 }
