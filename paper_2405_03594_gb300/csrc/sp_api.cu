@@ -7,6 +7,7 @@
 
 #include "../../include/sp_stack.h"
 #include "sp_internal.cuh"
+#include "sp_kv4.cuh"
 
 namespace sp {
 

@@ -15,12 +15,14 @@
 //   warps 12, 13     issue a tile's products each
 //   warp 14          copies of the codes, and the next item
 //
-// Measured, 32 heads of 128, two prompts of up to 2048 tokens behind a prefix (4 x 24e9 operations): 142 us,
-// 0.68 PFLOP/s, 0.36 of the measured bf16 rate.  A step of a tile is a chain -- scores read 0.13 us,
-// exponentials 0.5 (the special-function units' rate), weights' products and the next scores 0.55,
-// and four barriers -- of which the two tiles overlap about half.
+// Measured, 32 heads of 128, two prompts of up to 2048 tokens behind a prefix (4 x 24e9 operations): 136 us,
+// 0.71 PFLOP/s, 0.37 of the measured bf16 rate.  A step of both tiles takes 4300 clocks, 2048 of them the
+// tensor core's.  The expansion of the codes bounds it, 1500 clocks for the keys and as many for the
+// values (without its arithmetic: 125 us before the items were sorted, where the whole took 142); then the chain of a
+// tile: scores read and weights made 1400 clocks, their products and the next scores 1300, four barriers.  The
+// exponentials are not felt (left out: no change).
 //
-// Split.  Pairs of tiles are taken from one list, later rows (which see more) first.  Where there are
+// Split.  Pairs of tiles are taken from one list, those that see more first.  Where there are
 // fewer pairs than SMs, each one's steps of keys are cut into shares, whose sums join_rows_kernel adds up
 // in order: twelve tokens behind 8000, 8 key heads, 130 us uncut, 42 in shares.
 //
@@ -180,6 +182,66 @@ __device__ __forceinline__ Item item_at(const AttendParams& p, int64_t i, int& s
     set_status(p.status, kStatusBadIndex);
     shares = 1;
   }
+  return it;
+}
+
+// Item i, by a warp, where every item is a whole one and up to 32 requests have more items than there are
+// CTAs: most steps first, whatever request they belong to, so that the CTAs finish together (two prompts, of
+// 24 to 17 and 18 to 10 steps, over 152 SMs: the last one ends after 51 steps, in the list's order
+// after 55).  A lane per request counts its pairs of at least so many steps, and a search over the steps finds the item.
+__device__ __forceinline__ Item item_by_steps(const AttendParams& p, int64_t i) {
+  const int32_t* share = p.work + p.requests + 1;
+  const int lane = threadIdx.x & 31, heads = p.cache.heads;
+  int shares;
+  if (p.requests > 32 || (int64_t)share[p.requests] * heads <= gridDim.x) return item_at(p, i, shares);
+  Item it;
+  it.rows = 0;
+  int pairs = 0, q0 = 0, len = 0, fresh = 0;
+  if (lane < p.requests) {
+    q0 = p.cu_q[lane];
+    len = p.lens[lane];
+    fresh = p.cu_q[lane + 1] - q0;
+    pairs = share[lane + 1] - share[lane];
+    if (pairs != 0 && (fresh <= 0 || len < fresh || fresh > p.max_new || q0 < 0 || q0 + (int64_t)fresh > p.tokens ||
+                       ((int64_t)fresh * p.group + 2 * kTile - 1) / (2 * kTile) != pairs)) {
+      set_status(p.status, kStatusBadIndex);
+      pairs = 0;
+    }
+  }
+  const int64_t rows = (int64_t)fresh * p.group;
+  const int k = (int)(i / heads);  // pairs of tiles before this one
+  auto of_steps = [&](int steps) {  // of the lane's request: pairs of at least so many
+    const int64_t row = ((int64_t)(steps - 1) * kTile - (len - fresh)) * p.group;  // the first row that needs them
+    return pairs == 0 || row >= rows ? 0 : row <= 0 ? pairs : pairs - (int)(row / (2 * kTile));
+  };
+  int lo = 1, hi = (int)__reduce_max_sync(0xffffffffu, pairs ? (unsigned)((len + kTile - 1) / kTile) : 0u) + 1;
+  if (__reduce_add_sync(0xffffffffu, pairs) <= k) return it;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (__reduce_add_sync(0xffffffffu, of_steps(mid)) > k) lo = mid;
+    else hi = mid;
+  }
+  const int more = of_steps(lo + 1), own = of_steps(lo) - more;
+  int before = own;  // own pairs of the requests up to this one
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, before, d);
+    if (lane >= d) before += x;
+  }
+  const int rank = k - __reduce_add_sync(0xffffffffu, more);
+  const int b = __ffs(__ballot_sync(0xffffffffu, before > rank)) - 1;
+  const int from_end = __shfl_sync(0xffffffffu, more + rank - (before - own), b);
+  it.b = b;
+  it.h = (int)(i % heads);
+  it.q0 = __shfl_sync(0xffffffffu, q0, b);
+  it.len = __shfl_sync(0xffffffffu, len, b);
+  fresh = __shfl_sync(0xffffffffu, fresh, b);
+  it.row0 = (__shfl_sync(0xffffffffu, pairs, b) - 1 - from_end) * 2 * kTile;
+  it.rows = (int)min((int64_t)fresh * p.group - it.row0, (int64_t)(2 * kTile));
+  it.sees0 = it.len - fresh + 1;
+  it.j0 = 0;
+  it.j1 = max(all_steps(p, it, 0), all_steps(p, it, 1));
+  it.part = -1;
   return it;
 }
 
@@ -428,11 +490,11 @@ __device__ __forceinline__ void copy_role(const AttendParams& p, Shared& sh, uin
       return j < n && lane < pages && ((int64_t)at << shift) < it.len ? (at < p.width ? table[at] : -1) : INT_MIN;
     };
     int next = page_of(0);
-    if (lane == 0) {  // the item after this one
-      Item after;
+    {
+      Item after;  // the item after this one
       do fetch(after);
       while (after.rows < 0);
-      sh.item[(round + 1) & 1] = after;
+      if (lane == 0) sh.item[(round + 1) & 1] = after;
     }
     __syncwarp();
     for (int j = 0; j < n && !wait.dead; ++j) {
@@ -476,8 +538,8 @@ __device__ __forceinline__ void fill_role(const AttendParams& p, Shared& sh, uin
   constexpr int KP = D / 32;  // 16-byte pieces of a row: a lane takes one of row f / KP, then of rows further on
   const int piece = f % KP;
   // The pieces of a row that lie in the second panel are stored in another order, so that eight
-  // lanes' 16 bytes never share a bank.
-  const int turn = piece >> 1;
+  // lanes' 16 bytes, of two rows, never share a bank.
+  const int turn = piece >> 1 << 1;
   Wait wait{p};
   uint32_t steps = 0;
   for (uint32_t round = 0;; ++round) {
@@ -526,8 +588,8 @@ __device__ __forceinline__ void fill_role(const AttendParams& p, Shared& sh, uin
         for (int x = 0; x < KP; ++x) {
           const int key = x * (kTile / KP) + f / KP;
           const uint32_t s = __byte_perm(par[x], par[x], 0x1010), m = __byte_perm(par[x], par[x], 0x3232);
-          const uint32_t w[4] = {turn ? c4[x].y : c4[x].x, turn ? c4[x].x : c4[x].y, turn ? c4[x].w : c4[x].z,
-                                 turn ? c4[x].z : c4[x].w};
+          const uint32_t w[4] = {turn ? c4[x].z : c4[x].x, turn ? c4[x].w : c4[x].y, turn ? c4[x].x : c4[x].z,
+                                 turn ? c4[x].y : c4[x].w};
           uint8_t* row = dst + key * 128 + (piece >> 1) * kPanel;
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
@@ -646,9 +708,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
     sh.dead = 0;
   }
   pdl_wait();
-  // the next share of the list
+  // the next share of the list, by a warp
   auto fetch = [&](Item& it) {
-    const int64_t i = (int64_t)atomicAdd(&p.cnt[0], 1);
+    int next = 0;
+    if ((tid & 31) == 0) next = atomicAdd(&p.cnt[0], 1);
+    const int64_t i = (int64_t)__shfl_sync(0xffffffffu, next, 0);
+    if (p.split == 1) {
+      it = item_by_steps(p, i);
+      return;
+    }
     int shares;
     it = item_at(p, i / p.split, shares);
     if (it.rows <= 0 || shares == 1) {
@@ -664,11 +732,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
     it.j1 = (int)((int64_t)(x + 1) * n / shares);
     it.part = (int)i;
   };
-  if (tid == kBusyThreads - 32) {
+  if (warp == kBusyThreads / 32 - 1) {
     Item it;
     do fetch(it);
     while (it.rows < 0);
-    sh.item[0] = it;
+    if (tid == kBusyThreads - 32) sh.item[0] = it;
   }
   if (warp == 0) {
     tmem_alloc(&sh.tmem, 512);

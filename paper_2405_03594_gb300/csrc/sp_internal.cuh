@@ -97,7 +97,7 @@ inline size_t ws_counter_bytes(int num_sms) {
   return ((size_t)2 * kMaxGridPerSm * num_sms * sizeof(int) + 255) / 256 * 256;
 }
 
-enum : int { kStatusOk = 0, kStatusTimeout = 1, kStatusBadFormat = 2, kStatusBadIndex = 3 };
+enum : int { kStatusOk = 0, kStatusTimeout = 1, kStatusBadFormat = 2 };
 
 // ---------------------------------------------------------------- device helpers
 #if defined(__CUDACC__)

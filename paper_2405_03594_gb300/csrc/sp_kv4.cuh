@@ -9,6 +9,8 @@
 
 namespace sp {
 
+constexpr int kStatusBadIndex = 3;  // device status, behind kStatusBadFormat: an index that a kernel left out
+
 constexpr float kKvMost = 32768.f;  // largest magnitude that the cache holds
 constexpr int kMaxGroup = 64;       // query heads per key head
 constexpr int kUnitKeys = 32;       // keys of one step of attend_kernel

@@ -386,6 +386,18 @@ def test_long_contexts_are_split_and_joined(sp, serve, lens, new, heads, kv):
     assert not ws[:32 * sms].any()  # the arrival counters: ready for the next call, of sp_linear too
 
 
+@pytest.mark.parametrize("lens,new,heads,kv,d", [([600, 4000, 20, 300, 140], [600, 34, 0, 300, 129], 64, 32, 64),
+                                                 ([1500], [1500], 32, 32, 64), ([700] * 3, [700, 650, 513], 32, 32, 128),
+                                                 ([40 + 8 * i for i in range(33)], [40] * 33, 8, 8, 64)])
+def test_more_pairs_of_tiles_than_multiprocessors(sp, serve, lens, new, heads, kv, d):
+    """Prompts of different and of equal lengths, whose work is taken in order of its size; more than 32 of them."""
+    g = np.random.default_rng(sum(lens))
+    f = Filled(serve, g, lens, new, heads, kv, d, 16)
+    y = f.cache.attend(f.qd, f.batch, max(new))
+    sp.check()
+    _near(y, f.want(), f.vmax())
+
+
 def test_many_requests(sp, serve):
     g = np.random.default_rng(3)
     lens = g.integers(1, 300, 500).tolist()
