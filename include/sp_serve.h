@@ -147,8 +147,11 @@ typedef struct sp_attend_args {
 
 /* out = softmax(scale * q . K^T) . V over the values that the cache stands for.  Of a request with
  * L tokens, a of them new, new token i sees the first L - a + i + 1.  Scores, softmax statistics and
- * sums are fp32; codes and queries enter the products exactly; one rounding to bf16 at the end.  A
- * token that sees nothing gets zeros.  Rows of `out` behind cu_q[requests] are not written.
+ * sums are fp32; queries enter the products exactly, weights rounded to fp16, cached values exactly
+ * (of a request with more than 32 query rows per key head: rounded to fp16); one rounding to bf16 at
+ * the end.  Keys whose page the table does not hold take no part and are recorded for sp_check, and a
+ * token left with none gets zeros.  Of a request whose tables do not belong to its lengths nothing is
+ * written, and it is recorded.  Rows of `out` behind cu_q[requests] are not written.
  * `workspace` as for sp_linear: sp_kv4_attend_workspace_size bytes, its first
  * SP_WORKSPACE_ZERO_BYTES zero before its first use, calls that share it ordered on one stream; one
  * buffer can serve sp_linear and this call.  Results are bitwise repeatable. */

@@ -19,7 +19,12 @@
 namespace sp {
 namespace {
 
-constexpr int kFewThreads = 128, kManyThreads = 512;  // of a row's CTA: where rows are many, few
+// Threads of a row's CTA: few where rows are many, as 16 such CTAs are resident at a time (2048 rows of 32000,
+// bf16: 23.6 us; with 12 of them, which leaves 40 registers a thread and a second wave, 26.5).  Else by the
+// 16-byte vectors that the CTA has (one row of 32000 and its best five: 6.1 us by 256 threads, 7.0 by 512; one
+// row of 131071 in fp32: 7.9 and 7.3).
+constexpr int kFewThreads = 128, kSomeThreads = 256, kManyThreads = 512;
+constexpr int64_t kManyVectors = 2048;
 constexpr int kMaxTop = 64;
 constexpr int kMaxCluster = 8;
 constexpr int kCandidates = 1024;
@@ -166,7 +171,7 @@ __device__ __forceinline__ Stat join_warp(Stat a) {
 }
 
 template <typename T, int kLpThreads>
-__global__ void __launch_bounds__(kLpThreads, 1536 / kLpThreads)
+__global__ void __launch_bounds__(kLpThreads, (kLpThreads == kFewThreads ? 2048 : 1536) / kLpThreads)
     logprobs_kernel(const __grid_constant__ LogprobParams p) {
   constexpr int kLpWarps = kLpThreads / 32;
   using V = Vec<T>;
@@ -404,7 +409,7 @@ extern "C" sp_status sp_token_logprobs(const void* logits, sp_logits_dtype dtype
   // its threads
   int cluster = 1;
   while (cluster < kMaxCluster && tokens * cluster * 2 <= 2 * sms &&
-         vocab * es / 16 >= (int64_t)cluster * 2 * (kManyThreads / 2))
+         vocab * es / 16 >= (int64_t)cluster * 2 * (kSomeThreads / 2))
     cluster *= 2;
   const bool few = tokens >= 4 * sms;
   if (tokens * cluster > ((int64_t)1 << 31) - 1) return SP_ERR_UNSUPPORTED;
@@ -420,9 +425,13 @@ extern "C" sp_status sp_token_logprobs(const void* logits, sp_logits_dtype dtype
   p.top_logp = top_logp_out;
   p.top_ids = top_ids_out;
   p.status = device_status_ptr();
-  auto kern = dtype == SP_LOGITS_BF16
-                  ? (few ? logprobs_kernel<uint16_t, kFewThreads> : logprobs_kernel<uint16_t, kManyThreads>)
-                  : (few ? logprobs_kernel<float, kFewThreads> : logprobs_kernel<float, kManyThreads>);
-  return launch_pdl(kern, dim3((unsigned)(tokens * cluster)), few ? kFewThreads : kManyThreads, 0, cluster,
+  const int threads = few ? kFewThreads : vocab * es / 16 / cluster < kManyVectors ? kSomeThreads : kManyThreads;
+  auto kern = [&](auto x) {
+    using T = decltype(x);
+    return threads == kFewThreads    ? logprobs_kernel<T, kFewThreads>
+           : threads == kSomeThreads ? logprobs_kernel<T, kSomeThreads>
+                                     : logprobs_kernel<T, kManyThreads>;
+  };
+  return launch_pdl(dtype == SP_LOGITS_BF16 ? kern(uint16_t()) : kern(float()), dim3((unsigned)(tokens * cluster)), threads, 0, cluster,
                     (cudaStream_t)stream, p);
 }

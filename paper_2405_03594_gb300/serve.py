@@ -52,9 +52,10 @@ def _heads(x: torch.Tensor, heads: int | None, dim: int, name: str) -> tuple[int
     """Checks x [tokens, heads, dim] bf16 with contiguous heads (a view of a fused row serves) and
     returns its tokens, heads and token stride."""
     shape, stride = x.shape, x.stride()
-    if x.dtype is not _BF16 or len(shape) != 3 or shape[2] != dim or (heads is not None and shape[1] != heads):
-        raise ValueError(f"{name}: bf16 [tokens, {'heads' if heads is None else heads}, {dim}] wanted, "
-                         f"got {x.dtype} {list(shape)}")
+    if (x.dtype is not _BF16 or len(shape) != 3 or shape[2] != dim or (heads is not None and shape[1] != heads)
+            or not x.is_cuda):
+        raise ValueError(f"{name}: bf16 [tokens, {'heads' if heads is None else heads}, {dim}] on a GPU wanted, "
+                         f"got {x.dtype} {list(shape)} on {x.device}")
     t, h, _ = shape
     if stride[2] != 1 or (h > 1 and stride[1] != dim):
         raise ValueError(f"{name}: the heads of a token must be contiguous")
@@ -63,24 +64,24 @@ def _heads(x: torch.Tensor, heads: int | None, dim: int, name: str) -> tuple[int
 
 def _index(x: torch.Tensor, n: int, dtype, name: str) -> int:
     """Checks a contiguous vector of n entries or more and returns its address."""
-    if x.dtype is not dtype or x.dim() != 1 or x.shape[0] < n or not x.is_contiguous():
-        raise ValueError(f"{name}: contiguous {dtype} [{n}] wanted, got {x.dtype} {list(x.shape)}")
+    if x.dtype is not dtype or x.dim() != 1 or x.shape[0] < n or not x.is_contiguous() or not x.is_cuda:
+        raise ValueError(f"{name}: contiguous {dtype} [{n}] on a GPU wanted, got {x.dtype} {list(x.shape)} on {x.device}")
     return x.data_ptr()
 
 
 def _weight(w: torch.Tensor | None, dim: int, name: str) -> int:
     if w is None:
         return 0
-    if w.dtype is not _BF16 or w.shape != (dim,) or not w.is_contiguous():
-        raise ValueError(f"{name}: contiguous bf16 [{dim}] wanted")
+    if w.dtype is not _BF16 or w.shape != (dim,) or not w.is_contiguous() or not w.is_cuda:
+        raise ValueError(f"{name}: contiguous bf16 [{dim}] on a GPU wanted")
     return w.data_ptr()
 
 
 def _output(out: torch.Tensor | None, t: int, h: int, dim: int, like: torch.Tensor, name: str) -> torch.Tensor:
     if out is None:
-        return like.new_empty((t, h, dim))
-    if out.dtype is not _BF16 or out.shape != (t, h, dim) or not out.is_contiguous():
-        raise ValueError(f"{name}: contiguous bf16 {[t, h, dim]} wanted")
+        return torch.empty((t, h, dim), dtype=_BF16, device=like.device)  # (new_empty takes 1 us longer)
+    if out.dtype is not _BF16 or out.shape != (t, h, dim) or not out.is_contiguous() or not out.is_cuda:
+        raise ValueError(f"{name}: contiguous bf16 {[t, h, dim]} on a GPU wanted")
     return out
 
 
@@ -90,8 +91,8 @@ def _run_rope(q, k, v, positions, cos_sin, q_weight, k_weight, eps, pairs, q_out
     tk, kv, k_stride = _heads(k, None, dim, "k")
     if tk != t:
         raise ValueError("q and k hold different numbers of tokens")
-    if cos_sin.dtype is not _F32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous():
-        raise ValueError("cos_sin: contiguous float32 [rows, rot] wanted")
+    if cos_sin.dtype is not _F32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous() or not cos_sin.is_cuda:
+        raise ValueError("cos_sin: contiguous float32 [rows, rot] on a GPU wanted")
     rows, rot = cos_sin.shape
     pos = _index(positions, t, _I32, "positions")
     qw, kw = _weight(q_weight, dim, "q_weight"), _weight(k_weight, dim, "k_weight")
@@ -162,19 +163,18 @@ class KvCache:
                out: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
         """Causal attention of q [T, H, D] (the step's tokens, request by request) over the cache by
         the tables of `batch`; max_new: at least the most new tokens of a request; scale: 1 / sqrt(D)
-        by default.  A token that sees nothing gets zeros; rows behind the step's last token keep what
-        `out` held."""
+        by default.  Rows behind the step's last token keep what `out` held."""
         dim = self.head_dim
         t, h, q_stride = _heads(q, batch.heads, dim, "q")
+        device = q.device
         if out is None:
-            out, out_stride = q.new_empty((t, h, dim)), h * dim
+            out, out_stride = torch.empty((t, h, dim), dtype=_BF16, device=device), h * dim
         else:
             to, _, out_stride = _heads(out, h, dim, "out")
             if to != t:
                 raise ValueError("q and out hold different numbers of tokens")
         if self.kv_heads != batch.kv_heads or self.page_size != batch.page_size:
             raise ValueError("the batch was planned for another kind of cache")
-        device = q.device
         if workspace is None:
             workspace = sp.workspace_for(self.workspace_size(), device, stream)
         _check(_attend(_pack_attend(q.data_ptr(), out.data_ptr(), q_stride, out_stride, self._address,
@@ -248,8 +248,8 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, str
     float32 [T]; with top > 0 also the `top` most likely entries: log probabilities [T, top] and ids
     (int64), by falling logit and, among equal ones, rising id."""
     dtype = logits.dtype
-    if (dtype is not _BF16 and dtype is not _F32) or logits.dim() != 2 or logits.stride(1) != 1:
-        raise ValueError("logits: bf16 or float32 [T, V] with unit column stride wanted")
+    if (dtype is not _BF16 and dtype is not _F32) or logits.dim() != 2 or logits.stride(1) != 1 or not logits.is_cuda:
+        raise ValueError("logits: bf16 or float32 [T, V] with unit column stride on a GPU wanted")
     t, v = logits.shape
     ids = _index(tokens, t, _I64, "tokens")
     device = logits.device

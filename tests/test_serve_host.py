@@ -146,6 +146,23 @@ def test_logprobs_refusals(sp):
     assert call(tokens=0) == 0
 
 
+def test_tensors_outside_a_gpu_are_refused(sp):
+    import torch
+
+    from paper_2405_03594_gb300 import serve
+
+    data = torch.zeros(4 * 2 * 16 * 72, dtype=torch.uint8)
+    c = serve.KvCache(4, 2, 64, 16, data=data)
+    q = torch.zeros((3, 4, 64), dtype=torch.bfloat16)
+    pos, slots, cs = torch.zeros(3, dtype=torch.int32), torch.zeros(3, dtype=torch.int64), torch.zeros((4, 64))
+    b = serve.Batch(c, 4, 1, 3, 1)
+    for call in (lambda: c.append(q, q[:, :2], q[:, :2], pos, slots, cs), lambda: c.read(slots), lambda: c.attend(q, b, 3),
+                 lambda: serve.qk_norm_rope(q, q[:, :2], pos, cs), lambda: b.plan(pos[:1]),
+                 lambda: serve.token_logprobs(cs, slots)):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+
+
 def test_struct_layouts(sp, tmp_path):
     """The binding's structs are the header's (gcc, no GPU)."""
     gcc = shutil.which("gcc")
