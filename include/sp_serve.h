@@ -149,9 +149,9 @@ typedef struct sp_attend_args {
  * L tokens, a of them new, new token i sees the first L - a + i + 1.  Scores, softmax statistics and
  * sums are fp32; queries enter the products exactly, weights rounded to fp16, cached values exactly
  * (of a request with more than 32 query rows per key head: rounded to fp16); one rounding to bf16 at
- * the end.  Keys whose page the table does not hold take no part and are recorded for sp_check, and a
- * token left with none gets zeros.  Of a request whose tables do not belong to its lengths nothing is
- * written, and it is recorded.  Rows of `out` behind cu_q[requests] are not written.
+ * the end.  A page that the table does not hold is not read and is recorded for sp_check; what the
+ * tokens that would see its keys get is unspecified.  Of a request whose tables do not belong to its
+ * lengths nothing is written, and it is recorded.  Rows of `out` behind cu_q[requests] are not written.
  * `workspace` as for sp_linear: sp_kv4_attend_workspace_size bytes, its first
  * SP_WORKSPACE_ZERO_BYTES zero before its first use, calls that share it ordered on one stream; one
  * buffer can serve sp_linear and this call.  Results are bitwise repeatable. */

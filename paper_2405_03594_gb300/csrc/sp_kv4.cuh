@@ -16,13 +16,14 @@ constexpr int kMaxGroup = 64;       // query heads per key head
 constexpr int kUnitKeys = 32;       // keys of one step of attend_kernel
 constexpr int kRowTile = 32;        // query rows (token, head of the group) of its widest form
 // Query rows of a request from which attend_rows_kernel takes it: every request that attend_kernel would
-// need a second row tile for.  32 heads over 8, 12 new tokens (48 rows), attend_kernel / attend_rows_kernel,
-// us: one request behind 1000 tokens 37 / 24, behind 8000 50 / 42 (130 without its steps cut into
-// shares), 16 requests 61 / 29 and 228 / 146; alone with its 12 tokens 12 / 16.
+// need a second row tile for.  32 heads over 8 of 128, 12 new tokens (48 rows), attend_kernel / attend_rows_kernel,
+// us: 16 requests behind 1000 tokens 46 / 28, behind 8000 218 / 141; one request 23 / 24 and 37 / 42 (130
+// without its steps cut into shares), alone with its 12 tokens 12 / 15: what one request loses is less than what
+// several gain, and the host, which launches both kernels or one, sees no lengths.
 constexpr int kManyRows = 33;
 constexpr int kPairRows = 256;      // query rows of one of its items
 constexpr int kSetupUnits = 2;      // what a segment costs beside its units, in units (64 requests of 100 to
-                                    // 16384 tokens: 58.0 us at 0, 53.3 at 1, 50.2 at 2, 51.1 at 4)
+                                    // 16384 tokens: 57.9 us at 0, 52.5 at 1, 49.9 at 2, 50.0 at 3, 50.6 at 4)
 
 struct Kv4 {
   uint8_t* data;
