@@ -227,6 +227,9 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
   else window();
   const int heads = p.cache.heads;
   const int64_t all = (int64_t)p.work[p.requests] * heads;
+  int others = 0;  // requests of more new tokens than the call was told of: loaded here, looked at at the end
+  if (p.alone && blockIdx.x == 0 && tid == 0)
+    asm volatile("ld.global.s32 %0, [%1];" : "=r"(others) : "l"(p.work + 2 * p.requests + 1));
   const int total = (int)min(all, (int64_t)INT_MAX);
   if (total != all && tid == 0) set_status(p.status, kStatusBadIndex);
   const int ctas = max(1, min((int)gridDim.x, total / kMinUnits));
@@ -677,6 +680,8 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
     }
   }
 
+  if (others != 0) set_status(p.status, kStatusBadIndex);
+
   // ------------------------------------------------------------------ segments shared by warps
   __syncthreads();
   if (warp == 0) {  // the parts in order, and the rows of the segments that begin among them
@@ -894,7 +899,8 @@ sp_status sp_kv4_attend(const sp_attend_args* a, void* workspace_dev, size_t wor
   p.timeout_ns = wait_timeout_ns();
   cudaStream_t s = (cudaStream_t)stream;
   const int64_t most = (int64_t)a->max_new * p.group;
-  if (most >= kManyRows) {
+  p.alone = most < kManyRows;
+  if (!p.alone) {
     const sp_status st = launch_attend_rows(p, d, s);
     if (st != SP_OK) return st;
   }

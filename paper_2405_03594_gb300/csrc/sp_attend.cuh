@@ -13,6 +13,7 @@ struct AttendParams {
   const int32_t *table, *lens, *cu_q, *work;
   int32_t requests, width, group;
   int32_t max_new;
+  int32_t alone;  // attend_kernel: no attend_rows_kernel was launched before it
   int64_t tokens;
   int32_t group_inverse;  // 2^16 / group, rounded up
   float scale_log2;

@@ -534,6 +534,12 @@ def test_rows_behind_the_last_token_and_bad_tables(sp, serve):
     with pytest.raises(sp.SpError):
         sp.check()
     assert (out[:3] == 7).all() and not (out[3:6] == 7).all()
+    many = Filled(serve, g, [50, 20], [40, 1], 2, 2, 64, 16)
+    y = torch.full_like(many.qd, 7.0)
+    many.cache.attend(many.qd, many.batch, 1, out=y)
+    with pytest.raises(sp.SpError):
+        sp.check()
+    assert (y[:40] == 7).all() and not (y[40] == 7).all()
     # lengths that the tables were not planned for
     f.batch.lens[0] = 500
     f.cache.attend(f.qd, f.batch, 3)
