@@ -6,11 +6,13 @@
 //     out          = (sum_k (e_k s_k) n + sum_k e_k m_k) / sum_k e_k,    e_k = 2^(x_k - M)
 // so both products run on the codes.  A code's four bits, wherever they lie in the low byte of a
 // 16-bit half, are an fp16 subnormal, n 2^-24 or n 2^-20, which the tensor cores multiply exactly:
-// one AND per two codes is all the expansion there is.  The queries enter as fp16 too, exactly: a
-// row is scaled by the power of two that brings its largest entry under fp16's (bf16 has fewer
-// bits).  The weights e_k s_k of the values are rounded to fp16; M is a running maximum of
-// x_k + log2(s_k), so that they stay below 2^8 and their large ones keep 11 bits whatever the scales
-// are.  M moves only when a weight would pass 2^8, so most steps rescale nothing.
+// one AND per two codes is all the expansion there is.  The queries enter as fp16 too: each row is
+// scaled by the power of two that brings its own largest entry to 2^14 ... 2^15, half of its channels
+// by 1/16 of that, which is exact (bf16 has fewer bits) but for entries below 2^-27 of the largest; those
+// round to 2^-35 of it, far below the fp32 sums' own rounding.  The weights e_k s_k of the values are
+// rounded to fp16; M is a running maximum of x_k + log2(s_k), so that they stay below 2^8 and their large
+// ones keep 11 bits whatever the scales are.  M moves only when a weight would pass 2^8, so most steps
+// rescale nothing.
 //
 // Layout.  A warp takes units of 32 keys.  Both products have the codes as the wide operand of
 // m16n8k16 (keys, then channels, along M) and up to 8 NT query rows -- the heads that share the key
@@ -396,8 +398,8 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
       // queries: fp16 operand registers, and sums over the channels
       uint32_t qf[kQShared ? 1 : NT][KW][4];
       uint64_t qsum[NT];  // of query rows 2t, 2t + 1: c sum(q)
+      uint64_t rs[NT];    // of the same: c / the row's scaling
       int limit[NT][2];   // keys that they see
-      float rs;           // c 2^24 / the queries' scaling
       {
         auto load = [&](int nt, uint4(&x)[KW]) {
           const uint16_t* src = q_row(s.q0, s.h, s.head0, nt * 8 + g, p.q, p.q_stride) + t * (D / 4);
@@ -407,28 +409,24 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
             if (nt * 8 + g < s.rows) x[i] = *(reinterpret_cast<const uint4*>(src) + i);
           }
         };
-        uint32_t big = 0;  // the largest entry's magnitude, as bf16 bits
-        uint4 x4[KW];
-#pragma unroll(kQShared ? 1 : NT)
+#pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
+          uint4 x4[KW];
           load(nt, x4);
+          // each row by its own power of two, so that no other row takes bits from it
+          uint32_t big = 0;  // the row's largest magnitude, as bf16 bits
 #pragma unroll
           for (int i = 0; i < KW; ++i) {
             const uint32_t x[4] = {x4[i].x, x4[i].y, x4[i].z, x4[i].w};
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {  // (an infinity or NaN is its own row's matter)
-              const uint32_t y = (x[j >> 1] >> (16 * (j & 1))) & 0x7fffu;
-              big = max(big, y < 0x7f80u ? y : 0u);
-            }
+            for (int j = 0; j < 4; ++j) big = max(big, max(x[j] & 0x7fffu, (x[j] >> 16) & 0x7fffu));
           }
-        }
-        // 2^(141 - e): the largest entry, of biased exponent e, comes to 2^14 ... 2^15
-        const uint32_t e = max(15u, min(254u, __reduce_max_sync(0xffffffffu, big) >> 7));
-        const float f = __uint_as_float((268u - e) << 23);
-        rs = __uint_as_float((e - 14u) << 23) * kLo * p.scale_log2;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          if (NT > 1) load(nt, x4);
+          big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
+          big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
+          // 2^(141 - e): the largest entry, of biased exponent e, comes to 2^14 ... 2^15
+          const uint32_t e = max(15u, min(254u, big >> 7));
+          const float f = __uint_as_float((268u - e) << 23);
+          const float back = __uint_as_float((e - 14u) << 23) * p.scale_log2;
           float sum = 0.f;
 #pragma unroll
           for (int i = 0; i < KW; ++i) {
@@ -453,6 +451,7 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
           sum += __shfl_xor_sync(0xffffffffu, sum, 2);
           sum *= p.scale_log2;
           qsum[nt] = two(__shfl_sync(0xffffffffu, sum, 8 * t), __shfl_sync(0xffffffffu, sum, 8 * t + 4));
+          rs[nt] = two(__shfl_sync(0xffffffffu, back, 8 * t), __shfl_sync(0xffffffffu, back, 8 * t + 4));
 #pragma unroll
           for (int c = 0; c < 2; ++c) limit[nt][c] = s.sees + token_of(s.head0 + nt * 8 + 2 * t + c);
         }
@@ -512,7 +511,7 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
           for (int j = 0; j < 2; ++j) {
             const float2 a = __half22float2(kp[16 * i + 8 * j + kg]);
             const float2 v = __half22float2(kp[kUnitKeys + 16 * i + 8 * j + kg]);
-            ks[i][j] = a.x * rs, km[i][j] = a.y;
+            ks[i][j] = a.x * kLo, km[i][j] = a.y;
             vs[i][j] = v.x, vm[i][j] = v.y;
             vl[i][j] = lg2(fmaxf(v.x, 1.f / kLo));
           }
@@ -523,7 +522,8 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
               float *y = &x[nt][i][2 * j], k2 = ks[i][j], m2 = km[i][j];
-              apart(fma2(two(y[0], y[1]), two(k2, k2), mul2(two(m2, m2), qsum[nt])), y[0], y[1]);
+              // (the row's factor last: with the key's it could leave fp32's range)
+              apart(fma2(mul2(two(y[0], y[1]), two(k2, k2)), rs[nt], mul2(two(m2, m2), qsum[nt])), y[0], y[1]);
             }
         const bool edge = (u + 1) * kUnitKeys > s.sees || ok != 3;  // some row does not see all of the unit
         if (edge) {
