@@ -50,6 +50,7 @@ constexpr int kStages = 2;
 constexpr int kMostShares = 16;
 constexpr int kShareSteps = 3;            // of keys, least of a share where an item is cut
 constexpr int kMaxDevices = 64;
+constexpr float kFarScore = 1048576.f;    // 2^20: half a unit of such a score is 2^-4
 constexpr uint32_t kPanel = kTile * 128;  // 128 rows of 64 columns
 
 template <int D>
@@ -384,7 +385,15 @@ __device__ __forceinline__ void rows_role(const AttendParams& p, Shared& sh, uin
         }
       }
       const float minus = m == -INFINITY ? 0.f : -m;
-      const uint64_t c2 = two(cr, cr), m2 = two(minus, minus);
+      float c = cr;
+      // The maximum is a rounded product, the exponents below are not: off by half a unit of the scores, all by
+      // the same, which is nothing up to here and would pass fp16 from 2^28 on.  So far away the scores are rounded first.
+      if (__any_sync(0xffffffffu, fabsf(minus) > kFarScore)) {
+        c = 1.f;
+#pragma unroll
+        for (int k = 0; k < kTile; ++k) u[k] = __float_as_uint(__uint_as_float(u[k]) * cr);
+      }
+      const uint64_t c2 = two(c, c), m2 = two(minus, minus);
       uint64_t sum[2] = {0, 0};
 #pragma unroll
       for (int c = 0; c < 4; ++c) {

@@ -24,10 +24,11 @@ def _scaled(f, rows, by):
 
 @pytest.mark.parametrize("by", [2.0 ** 16, 2.0 ** 26, 2.0 ** 30, 2.0 ** 34, 2.0 ** 40, 2.0 ** 100])
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("heads,kv,new", [(4, 1, [1, 1, 1]), (12, 1, [1, 1, 1]), (8, 2, [5, 3, 2]), (8, 2, [8, 7, 1])])
+@pytest.mark.parametrize("heads,kv,new", [(4, 1, [1, 1, 1]), (12, 1, [1, 1, 1]), (8, 2, [5, 3, 2]), (8, 2, [8, 7, 1]),
+                                          (4, 1, [40, 3, 90])])
 def test_a_row_of_large_queries_leaves_its_neighbours_alone(sp, serve, heads, kv, new, d, by):  # noqa: F811
     """One head of one token is scaled up, in every row tile that it shares: the other heads and tokens of the
-    tile keep their results (8, 16, 24, 32 rows)."""
+    tile keep their results (8, 16, 24, 32 rows, and the kernel for many)."""
     g = np.random.default_rng(heads + sum(new))
     f = Filled(serve, g, [300, 40, 170], new, heads, kv, d, 32)
     _scaled(f, [(0, heads - 1), (new[0], 0), (sum(new) - 1, heads // 2)], by)
@@ -36,7 +37,7 @@ def test_a_row_of_large_queries_leaves_its_neighbours_alone(sp, serve, heads, kv
     _near(y, f.want(), f.vmax())
 
 
-@pytest.mark.parametrize("heads,kv,new", [(4, 1, [1, 1, 1]), (8, 2, [5, 3, 2]), (8, 2, [8, 7, 1])])
+@pytest.mark.parametrize("heads,kv,new", [(4, 1, [1, 1, 1]), (8, 2, [5, 3, 2]), (8, 2, [8, 7, 1]), (4, 1, [40, 3, 90])])
 @pytest.mark.parametrize("d", [64, 128])
 def test_queries_near_the_end_of_the_range(sp, serve, heads, kv, new, d):  # noqa: F811
     """Queries of 2^118 to 2^120: their scores are still fp32 numbers."""
