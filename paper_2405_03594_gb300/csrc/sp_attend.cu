@@ -180,7 +180,9 @@ __device__ __forceinline__ Row<Q> join(int n, Stat stat_at, Sums sums_at) {
   return r;
 }
 
-template <int D, int NT>
+// kExpire: a variant for sp_test_expired_attend, whose warp p.expire_warp of CTA p.expire_cta first waits for
+// what never comes and gives up.
+template <int D, int NT, bool kExpire = false>
 __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const __grid_constant__ AttendParams p) {
   constexpr int KW = D / 32, VW = D / 64;  // words of a lane: keys, values
   constexpr int MT = D / 16;               // channel tiles
@@ -317,8 +319,8 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
         asm volatile("prefetch.global.L1 [%0];" ::"l"(q));
       }
     };
-    // copies the next unit of the range that any row sees; nothing where there is none
-    auto issue = [&] {
+    // copies the next unit of the range that any row sees (or only says which it is); nothing where there is none
+    auto issue = [&](bool copies) {
       while (pu >= ps.seen || pw >= p_end) {
         pw = max(pw, p_end);
         if (pw >= w1) return;
@@ -352,7 +354,7 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
         m.ok = shift >= 5 ? (pg0 >= 0 ? 3 : 0) : (pg0 >= 0 ? 1 : 0) | (pg1 >= 0 ? 2 : 0);
         m.opens = opens;
         if (opens) m.s = ps;
-        if (shift >= 5) {  // the unit lies in one page
+        if (copies && shift >= 5) {  // the unit lies in one page
           if (pg0 >= 0) {
             const int in = (pu * kUnitKeys) & ((1 << shift) - 1);
             mbar_arrive_expect_tx(full, kStage);
@@ -363,7 +365,7 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
           } else {
             mbar_arrive(full);
           }
-        } else {
+        } else if (copies) {
           const uint8_t* b1 = p.cache.data + ((int64_t)pg1 * heads + ps.h) * block;
           mbar_arrive_expect_tx(full, (pg0 >= 0 ? kStage / 2 : 0) + (pg1 >= 0 ? kStage / 2 : 0));
 #pragma unroll
@@ -384,14 +386,34 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
       ++pending;
     };
 #pragma unroll 1
-    for (int i = 0; i < S; ++i) issue();
+    for (int i = 0; i < S; ++i) issue(true);
     __syncwarp();
 
     // ---------------------------------------------------------------- the segments of the range
+    // the copies on their way, from stage i on, have landed
+    auto drain = [&](int i, uint32_t parity) {
+      for (int k = 0; k < pending; ++k) {
+        mbar_wait_sleep(&bar[i], parity, p.timeout_ns);
+        if (++i == S) i = 0, parity ^= 1u;
+      }
+    };
     int stage = 0;
     uint32_t phase = 0;
     bool dead = false;
-    while (pending > 0 && !dead) {
+    if constexpr (kExpire) {
+      __shared__ uint64_t s_probe;
+      if (blockIdx.x == p.expire_cta && warp == p.expire_warp) {
+        if (lane == 0) {
+          mbar_init(&s_probe, 1);
+          fence_barrier_init();
+        }
+        __syncwarp();
+        dead = !__all_sync(0xffffffffu, mbar_wait_sleep(&s_probe, 0, p.timeout_ns));
+        if (dead && lane == 0) set_status(p.status, kStatusTimeout);
+        if (dead) drain(0, 0);
+      }
+    }
+    while (pending > 0) {
       const Segment s = s_meta[warp][stage].s;
       int u = s_meta[warp][stage].u;
       const int u0 = u;
@@ -468,10 +490,11 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
         l[nt] = off[nt] = 0;
       }
 
-      for (;; ++u) {
+      for (; !dead; ++u) {
         if (!__all_sync(0xffffffffu, mbar_wait_sleep(&bar[stage], phase, p.timeout_ns))) {
           if (lane == 0) set_status(p.status, kStatusTimeout);
           dead = true;
+          drain(stage, phase);
           break;
         }
         const uint8_t* st = ring + stage * kStage;
@@ -620,7 +643,7 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
         }
         __syncwarp();  // the stage has been read
         --pending;
-        issue();
+        issue(true);
         __syncwarp();
         if (++stage == S) {
           stage = 0;
@@ -629,9 +652,21 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
         if (pending == 0 || s_meta[warp][stage].opens) break;
       }
 
+      // A warp that gave up goes on through its range without copies and sums: the CTAs that share a segment
+      // count one another, on a counter that the next call finds as this one leaves it.
+      if (dead) {
+        for (;; ++u) {
+          --pending;
+          issue(false);
+          __syncwarp();
+          if (++stage == S) stage = 0;
+          if (pending == 0 || s_meta[warp][stage].opens) break;
+        }
+      }
+
       // the segment's sums: to `out` if the warp held all of it, else to shared memory
       const bool first = u0 > 0, last = u < s.seen - 1;
-      if (!dead) {
+      if (!dead || first || last) {
         float* dst = reinterpret_cast<float*>(last ? ring : ring + kFirst);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -669,13 +704,6 @@ __global__ void __launch_bounds__(32 * warps_of(D, NT), 1) attend_kernel(const _
           }
         }
         if ((first || last) && lane == 0) s_info[warp][last ? 1 : 0] = PartInfo{s.vis0, s.seen, s.rows, s.h, s.q0, s.head0};
-      }
-    }
-    for (; dead && pending > 0; --pending) {  // the copies that are still on their way
-      mbar_wait_sleep(&bar[stage], phase, p.timeout_ns);
-      if (++stage == S) {
-        stage = 0;
-        phase ^= 1u;
       }
     }
   }
@@ -807,7 +835,7 @@ constexpr size_t smem_bytes() {
 }
 
 // CTAs of a full grid; 0 if a lookup failed.
-template <int D, int NT>
+template <int D, int NT, bool kExpire = false>
 int grid_of() {
   static std::atomic<int> kept[kMaxDevices] = {};
   int dev = -1;
@@ -818,9 +846,9 @@ int grid_of() {
   }
   return kept_or_looked_up(kept[dev], [sms] {
     int n = 0;
-    if (cudaFuncSetAttribute(attend_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    if (cudaFuncSetAttribute(attend_kernel<D, NT, kExpire>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              (int)smem_bytes<D, NT>()) != cudaSuccess ||
-        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, attend_kernel<D, NT>, 32 * warps_of(D, NT),
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, attend_kernel<D, NT, kExpire>, 32 * warps_of(D, NT),
                                                       smem_bytes<D, NT>()) !=
             cudaSuccess) {
       cudaGetLastError();
@@ -835,11 +863,12 @@ size_t workspace_bytes(int head_dim, int sms) {
                                           attend_rows_part_bytes(head_dim, sms));
 }
 
-template <int D, int NT>
+template <int D, int NT, bool kExpire = false>
 sp_status launch(AttendParams p, cudaStream_t stream) {
-  const int ctas = grid_of<D, NT>();
+  const int ctas = grid_of<D, NT, kExpire>();
   if (ctas == 0) return SP_ERR_CUDA;
-  return launch_pdl(attend_kernel<D, NT>, dim3((unsigned)ctas), 32 * warps_of(D, NT), smem_bytes<D, NT>(), 1, stream, p);
+  return launch_pdl(attend_kernel<D, NT, kExpire>, dim3((unsigned)ctas), 32 * warps_of(D, NT), smem_bytes<D, NT>(), 1, stream,
+                    p);
 }
 
 }  // namespace
@@ -847,18 +876,15 @@ sp_status launch(AttendParams p, cudaStream_t stream) {
 
 using namespace sp;
 
-extern "C" {
+namespace {
 
-sp_status sp_kv4_attend_workspace_size(int32_t head_dim, size_t* bytes) {
-  if (!bytes) return SP_ERR_INVALID_ARG;
-  if (head_dim != 64 && head_dim != 128) return SP_ERR_UNSUPPORTED;
-  const int sms = current_sms();
-  if (sms == 0) return SP_ERR_CUDA;
-  *bytes = workspace_bytes(head_dim, sms);
-  return SP_OK;
-}
+// What sp_test_expired_attend makes expire.
+struct Expire {
+  int32_t cta, warp;
+  uint64_t wait_ns;
+};
 
-sp_status sp_kv4_attend(const sp_attend_args* a, void* workspace_dev, size_t workspace_size, void* stream) {
+sp_status attend(const sp_attend_args* a, void* workspace_dev, size_t workspace_size, const Expire* expire, void* stream) {
   if (!a || !a->cache || !a->cache->data || !kv4_positive(a->cache) || a->cache->reserved != 0 || a->reserved != 0)
     return SP_ERR_INVALID_ARG;
   if (a->requests < 0 || a->width < 0 || a->tokens < 0 || a->max_new < 0 || !(a->scale - a->scale == 0.f))
@@ -899,7 +925,16 @@ sp_status sp_kv4_attend(const sp_attend_args* a, void* workspace_dev, size_t wor
   p.timeout_ns = wait_timeout_ns();
   cudaStream_t s = (cudaStream_t)stream;
   const int64_t most = (int64_t)a->max_new * p.group;
+  if (expire) {
+    p.timeout_ns = expire->wait_ns;
+    p.expire_cta = (uint32_t)expire->cta;
+    p.expire_warp = expire->warp;
+  }
   p.alone = most < kManyRows;
+  if (expire) {
+    if (d != 64 || (most > 8 && most <= 24) || !p.alone) return SP_ERR_UNSUPPORTED;
+    return most <= 8 ? launch<64, 1, true>(p, s) : launch<64, 4, true>(p, s);
+  }
   if (!p.alone) {
     const sp_status st = launch_attend_rows(p, d, s);
     if (st != SP_OK) return st;
@@ -912,6 +947,30 @@ sp_status sp_kv4_attend(const sp_attend_args* a, void* workspace_dev, size_t wor
     case 3: return d == 64 ? launch<64, 3>(p, s) : launch<128, 3>(p, s);
   }
   return d == 64 ? launch<64, 4>(p, s) : launch<128, 4>(p, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+sp_status sp_kv4_attend_workspace_size(int32_t head_dim, size_t* bytes) {
+  if (!bytes) return SP_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return SP_ERR_UNSUPPORTED;
+  const int sms = current_sms();
+  if (sms == 0) return SP_ERR_CUDA;
+  *bytes = workspace_bytes(head_dim, sms);
+  return SP_OK;
+}
+
+sp_status sp_kv4_attend(const sp_attend_args* a, void* workspace_dev, size_t workspace_size, void* stream) {
+  return attend(a, workspace_dev, workspace_size, nullptr, stream);
+}
+
+sp_status sp_test_expired_attend(const sp_attend_args* a, void* workspace_dev, size_t workspace_size, int32_t cta,
+                                 int32_t warp, uint32_t wait_ms, void* stream) {
+  if (cta < 0 || warp < 0 || wait_ms < 1 || wait_ms > 10000) return SP_ERR_INVALID_ARG;
+  const Expire e = {cta, warp, (uint64_t)wait_ms * 1000000ull};
+  return attend(a, workspace_dev, workspace_size, &e, stream);
 }
 
 }  // extern "C"

@@ -23,6 +23,8 @@ struct AttendParams {
   int* cnt;     // attend_kernel: [grid] arrivals; attend_rows_kernel: its next item, CTAs that are done
   int32_t* status;
   uint64_t timeout_ns;
+  uint32_t expire_cta;  // in the variants of sp_test_expired_attend: the warp that gives up
+  int32_t expire_warp;
 };
 
 __device__ __forceinline__ float ex2(float x) {

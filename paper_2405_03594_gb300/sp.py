@@ -32,7 +32,7 @@ EXPORTS = ["sp_compress", "sp_decompress", "sp_workspace_size", "sp_linear", "sp
            "sp_clone", "sp_free", "sp_info", "sp_copy_out", "sp_check", "sp_capture_id", "sp_status_string",
            "sp_copy_columns", "sp_residual_add", "sp_mul_halves", "sp_mul_pairs", "sp_chain_workspace_size",
            "sp_chain_run", "sp_linear_epi", "sp_kv4_bytes", "sp_kv_plan", "sp_qk_norm_rope", "sp_kv4_read",
-           "sp_kv4_attend", "sp_kv4_attend_workspace_size", "sp_token_logprobs"]
+           "sp_kv4_attend", "sp_kv4_attend_workspace_size", "sp_test_expired_attend", "sp_token_logprobs"]
 
 
 KERNELS = {0: "", 1: "linear_cc_kernel", 2: "linear_ccw_kernel", 3: "linear_tc_kernel", 4: "linear_mma_kernel",
@@ -133,6 +133,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.sp_qk_norm_rope.argtypes = [ctypes.POINTER(SpRopeArgs), P]
     lib.sp_kv4_read.argtypes = [ctypes.POINTER(SpKv4), P, I64, P, P, P]
     lib.sp_kv4_attend.argtypes = [ctypes.POINTER(SpAttendArgs), P, SZ, P]
+    lib.sp_test_expired_attend.argtypes = [ctypes.POINTER(SpAttendArgs), P, SZ, ctypes.c_int32, ctypes.c_int32,
+                                           ctypes.c_uint32, P]
     lib.sp_kv4_attend_workspace_size.argtypes = [ctypes.c_int32, ctypes.POINTER(SZ)]
     lib.sp_token_logprobs.argtypes = [P, ctypes.c_int, I64, I64, I64, P, ctypes.c_int32, P, P, P, P, P]
     lib.sp_status_string.argtypes = [ctypes.c_int]
