@@ -251,6 +251,7 @@ struct Barriers {
   uint64_t s_full[2], p_full[2], o_done[2];
   uint64_t raw_full[2], raw_empty[2];  // keys, values
   uint64_t turn[2];          // the other tile's products of its step have been issued
+  uint64_t drained[2];       // where a wait has expired: a tile's products on their way are done
 };
 
 struct Shared {
@@ -429,7 +430,9 @@ __device__ __forceinline__ void rows_role(const AttendParams& p, Shared& sh, uin
     }
     if (n > 0) wait(&sh.bar.o_done[i], (done + n - 1) & 1);
     tc_fence_after();
-    if (!wait.dead) {
+    if (wait.dead) {
+      tmem_store_wait();  // (this thread's, before the columns are given back)
+    } else {
       float a, b;
       apart(l, a, b);
       a += b;
@@ -480,7 +483,7 @@ __device__ __forceinline__ void rows_role(const AttendParams& p, Shared& sh, uin
 
 // ------------------------------------------------------------------ keys and values: copies of the codes
 // A step's codes and parameters come to shared memory as they are, by one bulk copy per page, as soon as
-// the step before is expanded.
+// the step before is expanded.  Where a wait has expired, none is on its way any more when the CTA ends.
 template <int D, class Fetch>
 __device__ __forceinline__ void copy_role(const AttendParams& p, Shared& sh, uint8_t* s_raw, Fetch fetch) {
   using L = Smem<D>;
@@ -488,7 +491,7 @@ __device__ __forceinline__ void copy_role(const AttendParams& p, Shared& sh, uin
   const int shift = p.cache.shift, heads = p.cache.heads, pages = kTile >> shift;
   const int64_t block = kv4_block_bytes<D>(shift);
   Wait wait{p};
-  uint32_t steps = 0;
+  uint32_t steps = 0, sent = 0;  // sent: copies of keys and values, one after the other
   for (uint32_t round = 0;; ++round) {
     const Item it = sh.item[round & 1];
     if (it.rows <= 0) break;
@@ -531,10 +534,15 @@ __device__ __forceinline__ void copy_role(const AttendParams& p, Shared& sh, uin
           bulk_g2s(dst + kTile * (D / 2) + ((lane * 4) << shift),
                    src + (which ? kv4_value_params<D>(shift) : kv4_key_params<D>(shift)), 4 << shift, full);
         }
+        ++sent;
       }
     }
     steps += n;
-    if (!end_item(sh, wait)) break;
+    if (!end_item(sh, wait)) {
+      for (uint32_t which = 0; which < 2 && which < sent; ++which)
+        mbar_wait_sleep(&sh.bar.raw_full[which], ((sent - 1 - which) >> 1) & 1, p.timeout_ns);
+      break;
+    }
   }
 }
 
@@ -682,7 +690,12 @@ __device__ __forceinline__ void product_role(const AttendParams& p, Shared& sh, 
     }
     steps += n_all;
     done += n;
-    if (!end_item(sh, wait)) break;
+    if (!end_item(sh, wait)) {
+      if (elect_one()) mma_commit(&sh.bar.drained[i]);
+      __syncwarp();
+      mbar_wait_sleep(&sh.bar.drained[i], 0, p.timeout_ns);
+      break;
+    }
   }
 }
 
@@ -712,6 +725,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
       mbar_init(&sh.bar.raw_full[i], 1);
       mbar_init(&sh.bar.raw_empty[i], 1);
       mbar_init(&sh.bar.turn[i], 1);
+      mbar_init(&sh.bar.drained[i], 1);
     }
     fence_barrier_init();
     sh.dead = 0;
