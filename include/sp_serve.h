@@ -159,12 +159,12 @@ typedef struct sp_attend_args {
 sp_status sp_kv4_attend(const sp_attend_args* args, void* workspace_dev, size_t workspace_bytes, void* stream);
 
 /* Failure-path test (nothing calls it in normal use).  sp_kv4_attend, with warp `warp` of CTA `cta` of its
- * kernel first waiting on a shared-memory barrier that nothing completes, and every wait bounded by
+ * kernel (of the one for many rows, where that runs) first waiting on a shared-memory barrier that nothing completes, and every wait bounded by
  * wait_ms milliseconds.  The warp gives up and records SP_ERR_TIMEOUT, as any whose wait expires; what
  * it would have added to `out` is missing there.  The launch ends by itself, and the workspace is ready
  * for the next call.  A cta or warp that the kernel does not have, or that has no keys to read, gives up
  * nothing.  wait_ms in 1..10000, cta and warp not negative (SP_ERR_INVALID_ARG otherwise); compiled for
- * head_dim 64 and up to 8, or 25 to 32, query rows of a request and key head
+ * head_dim 64 and up to 8, or 25 and more, query rows of a request and key head
  * (SP_ERR_UNSUPPORTED otherwise), as variants of the kernels of their own. */
 sp_status sp_test_expired_attend(const sp_attend_args* args, void* workspace_dev, size_t workspace_bytes, int32_t cta,
                                  int32_t warp, uint32_t wait_ms, void* stream);

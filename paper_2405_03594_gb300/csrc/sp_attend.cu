@@ -932,11 +932,11 @@ sp_status attend(const sp_attend_args* a, void* workspace_dev, size_t workspace_
   }
   p.alone = most < kManyRows;
   if (expire) {
-    if (d != 64 || (most > 8 && most <= 24) || !p.alone) return SP_ERR_UNSUPPORTED;
-    return most <= 8 ? launch<64, 1, true>(p, s) : launch<64, 4, true>(p, s);
+    if (d != 64 || (most > 8 && most <= 24)) return SP_ERR_UNSUPPORTED;
+    if (p.alone) return most <= 8 ? launch<64, 1, true>(p, s) : launch<64, 4, true>(p, s);
   }
   if (!p.alone) {
-    const sp_status st = launch_attend_rows(p, d, s);
+    const sp_status st = launch_attend_rows(p, d, expire != nullptr, s);
     if (st != SP_OK) return st;
   }
   const int64_t rows = std::min<int64_t>(most, kRowTile);

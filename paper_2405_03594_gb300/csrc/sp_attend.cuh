@@ -68,8 +68,9 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   return r;
 }
 
-// attend_rows_kernel over the requests that the plan gave to it (sp_attend_rows.cu).
-sp_status launch_attend_rows(AttendParams p, int head_dim, cudaStream_t stream);
+// attend_rows_kernel over the requests that the plan gave to it (sp_attend_rows.cu); expire: the variant of
+// sp_test_expired_attend, for head_dim 64.
+sp_status launch_attend_rows(AttendParams p, int head_dim, bool expire, cudaStream_t stream);
 size_t attend_rows_part_bytes(int head_dim, int sms);  // of the shares that it joins
 
 }  // namespace sp

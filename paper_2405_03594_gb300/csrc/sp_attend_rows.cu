@@ -251,6 +251,7 @@ struct Barriers {
   uint64_t s_full[2], p_full[2], o_done[2];
   uint64_t raw_full[2], raw_empty[2];  // keys, values
   uint64_t turn[2];          // the other tile's products of its step have been issued
+  uint64_t probe;            // kExpire: nothing arrives here
   uint64_t drained[2];       // where a wait has expired: a tile's products on their way are done
 };
 
@@ -260,7 +261,6 @@ struct Shared {
   uint32_t nan[kStages][4];  // keys of the step whose values are not finite
   Item item[2];
   unsigned pages[2];         // of the raw keys and values: the pages that exist
-  int dead;
 };
 
 // A bounded wait of a whole warp; nothing is waited for once one has expired.  (The sleeping wait is a
@@ -268,7 +268,7 @@ struct Shared {
 // cache holds beside the roles' own: 165 us against 140 for the prefill measured below.)
 struct Wait {
   const AttendParams& p;
-  bool dead = false;
+  bool dead;
   __device__ __forceinline__ void operator()(uint64_t* bar, uint32_t parity) {
     if (dead) return;
     if (!__all_sync(0xffffffffu, mbar_wait_sleep(bar, parity, p.timeout_ns))) {
@@ -278,25 +278,24 @@ struct Wait {
   }
 };
 
-// The end of an item for every warp that works on it; false once a wait has expired.
-__device__ __forceinline__ bool end_item(Shared& sh, const Wait& wait) {
-  if (wait.dead) sh.dead = 1;
+// The end of an item for every warp that works on it; false, in all of them alike, once a wait has expired.
+__device__ __forceinline__ bool end_item(const Wait& wait) {
   tc_fence_before();
-  named_bar_sync(1, kBusyThreads);
+  const bool dead = named_bar_or(1, kBusyThreads, wait.dead);
   tc_fence_after();
-  return sh.dead == 0;
+  return !dead;
 }
 
 // ------------------------------------------------------------------ rows: scores to weights, and the output
 template <int D>
-__device__ __forceinline__ void rows_role(const AttendParams& p, Shared& sh, uint8_t* s_q, uint32_t tmem) {
+__device__ __forceinline__ void rows_role(const AttendParams& p, Shared& sh, uint8_t* s_q, uint32_t tmem, bool gone) {
   using L = Smem<D>;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int i = warp >> 2;  // tile
   const int r = tid & (kTile - 1);
   const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
   const uint32_t t_s = tmem + lanes + i * kTile, t_o = tmem + lanes + 2 * kTile + i * D;
-  Wait wait{p};
+  Wait wait{p, gone};
   uint32_t steps = 0, done = 0;
   for (uint32_t round = 0;; ++round) {
     const Item& it = sh.item[round & 1];  // (in shared memory: registers are what this role is short of)
@@ -477,7 +476,7 @@ __device__ __forceinline__ void rows_role(const AttendParams& p, Shared& sh, uin
     }
     steps += max(steps_of(p, it, 0), steps_of(p, it, 1));
     done += n;
-    if (!end_item(sh, wait)) break;
+    if (!end_item(wait)) break;
   }
 }
 
@@ -485,12 +484,12 @@ __device__ __forceinline__ void rows_role(const AttendParams& p, Shared& sh, uin
 // A step's codes and parameters come to shared memory as they are, by one bulk copy per page, as soon as
 // the step before is expanded.  Where a wait has expired, none is on its way any more when the CTA ends.
 template <int D, class Fetch>
-__device__ __forceinline__ void copy_role(const AttendParams& p, Shared& sh, uint8_t* s_raw, Fetch fetch) {
+__device__ __forceinline__ void copy_role(const AttendParams& p, Shared& sh, uint8_t* s_raw, Fetch fetch, bool gone) {
   using L = Smem<D>;
   const int lane = threadIdx.x & 31;
   const int shift = p.cache.shift, heads = p.cache.heads, pages = kTile >> shift;
   const int64_t block = kv4_block_bytes<D>(shift);
-  Wait wait{p};
+  Wait wait{p, gone};
   uint32_t steps = 0, sent = 0;  // sent: copies of keys and values, one after the other
   for (uint32_t round = 0;; ++round) {
     const Item it = sh.item[round & 1];
@@ -538,7 +537,7 @@ __device__ __forceinline__ void copy_role(const AttendParams& p, Shared& sh, uin
       }
     }
     steps += n;
-    if (!end_item(sh, wait)) {
+    if (!end_item(wait)) {
       for (uint32_t which = 0; which < 2 && which < sent; ++which)
         mbar_wait_sleep(&sh.bar.raw_full[which], ((sent - 1 - which) >> 1) & 1, p.timeout_ns);
       break;
@@ -548,7 +547,8 @@ __device__ __forceinline__ void copy_role(const AttendParams& p, Shared& sh, uin
 
 // ------------------------------------------------------------------ keys and values: codes to operands
 template <int D>
-__device__ __forceinline__ void fill_role(const AttendParams& p, Shared& sh, uint8_t* s_k, uint8_t* s_v, const uint8_t* s_raw) {
+__device__ __forceinline__ void fill_role(const AttendParams& p, Shared& sh, uint8_t* s_k, uint8_t* s_v, const uint8_t* s_raw,
+                                          bool gone) {
   using L = Smem<D>;
   const int f = threadIdx.x - kRowThreads, lane = threadIdx.x & 31;
   const int shift = p.cache.shift;
@@ -557,7 +557,8 @@ __device__ __forceinline__ void fill_role(const AttendParams& p, Shared& sh, uin
   // The pieces of a row that lie in the second panel are stored in another order, so that eight
   // lanes' 16 bytes, of two rows, never share a bank.
   const int turn = piece >> 1 << 1;
-  Wait wait{p};
+  Wait wait{p, gone};
+  bool alive = true;
   uint32_t steps = 0;
   for (uint32_t round = 0;; ++round) {
     const Item& it = sh.item[round & 1];
@@ -571,64 +572,67 @@ __device__ __forceinline__ void fill_role(const AttendParams& p, Shared& sh, uin
       for (int which = 0; which < 2; ++which) {
         wait(&sh.bar.raw_full[which], (steps + j) & 1);
         wait(which ? &sh.bar.v_empty[st] : &sh.bar.k_empty[st], ph ^ 1);
-        if (wait.dead) break;
-        const uint8_t* raw = s_raw + which * L::kRaw;
-        const uint32_t* raw_par = reinterpret_cast<const uint32_t*>(raw + kTile * (D / 2));
-        uint8_t* dst = which ? s_v + st * L::kV : s_k + st * L::kQ;
-        const unsigned ok = sh.pages[which];
-        const int left = keys - j * kTile;
-        uint4 c4[KP];
-        uint32_t par[KP];
+        if (!wait.dead) {
+          const uint8_t* raw = s_raw + which * L::kRaw;
+          const uint32_t* raw_par = reinterpret_cast<const uint32_t*>(raw + kTile * (D / 2));
+          uint8_t* dst = which ? s_v + st * L::kV : s_k + st * L::kQ;
+          const unsigned ok = sh.pages[which];
+          const int left = keys - j * kTile;
+          uint4 c4[KP];
+          uint32_t par[KP];
 #pragma unroll
-        for (int x = 0; x < KP; ++x) {
-          const int key = x * (kTile / KP) + f / KP;
-          c4[x] = *reinterpret_cast<const uint4*>(raw + (x * 128 + f) * 16);
-          par[x] = raw_par[key];
-          if (key >= left || !(ok >> (key >> shift) & 1)) par[x] = 0;  // what no token was written to may hold anything
-        }
-        if (which) {
-          auto finite = [](uint32_t y) { return (y & 0x7c00u) != 0x7c00u && (y & 0x7c000000u) != 0x7c000000u; };
+          for (int x = 0; x < KP; ++x) {
+            const int key = x * (kTile / KP) + f / KP;
+            c4[x] = *reinterpret_cast<const uint4*>(raw + (x * 128 + f) * 16);
+            par[x] = raw_par[key];
+            if (key >= left || !(ok >> (key >> shift) & 1)) par[x] = 0;  // what no token was written to may hold anything
+          }
+          if (which) {
+            auto finite = [](uint32_t y) { return (y & 0x7c00u) != 0x7c00u && (y & 0x7c000000u) != 0x7c000000u; };
 #pragma unroll
-          for (int x = 0; x < KP; ++x)
-            if (!finite(par[x])) par[x] = 0;
-          if (f < 32) {
+            for (int x = 0; x < KP; ++x)
+              if (!finite(par[x])) par[x] = 0;
+            if (f < 32) {
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const int key = 32 * x + lane;
-              const bool bad = key < left && (ok >> (key >> shift) & 1) && !finite(raw_par[key]);
-              const unsigned bits = __ballot_sync(0xffffffffu, bad);
-              if (lane == 0) sh.nan[st][x] = bits;  // (read before the stage was handed back)
+              for (int x = 0; x < 4; ++x) {
+                const int key = 32 * x + lane;
+                const bool bad = key < left && (ok >> (key >> shift) & 1) && !finite(raw_par[key]);
+                const unsigned bits = __ballot_sync(0xffffffffu, bad);
+                if (lane == 0) sh.nan[st][x] = bits;  // (read before the stage was handed back)
+              }
             }
           }
-        }
 #pragma unroll
-        for (int x = 0; x < KP; ++x) {
-          const int key = x * (kTile / KP) + f / KP;
-          const uint32_t s = __byte_perm(par[x], par[x], 0x1010), m = __byte_perm(par[x], par[x], 0x3232);
-          const uint32_t w[4] = {turn ? c4[x].z : c4[x].x, turn ? c4[x].w : c4[x].y, turn ? c4[x].x : c4[x].z,
-                                 turn ? c4[x].y : c4[x].w};
-          uint8_t* row = dst + key * 128 + (piece >> 1) * kPanel;
+          for (int x = 0; x < KP; ++x) {
+            const int key = x * (kTile / KP) + f / KP;
+            const uint32_t s = __byte_perm(par[x], par[x], 0x1010), m = __byte_perm(par[x], par[x], 0x3232);
+            const uint32_t w[4] = {turn ? c4[x].z : c4[x].x, turn ? c4[x].w : c4[x].y, turn ? c4[x].x : c4[x].z,
+                                   turn ? c4[x].y : c4[x].w};
+            uint8_t* row = dst + key * 128 + (piece >> 1) * kPanel;
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const int c = (4 * (piece & 1) + y) ^ turn;  // eight channels
-            const uint32_t h = w[y] >> 8;
-            *reinterpret_cast<uint4*>(row + ((c ^ (key & 7)) << 4)) =
-                make_uint4(value_lo(w[y], s, m), value_hi(w[y], s, m), value_lo(h, s, m), value_hi(h, s, m));
+            for (int y = 0; y < 4; ++y) {
+              const int c = (4 * (piece & 1) + y) ^ turn;  // eight channels
+              const uint32_t h = w[y] >> 8;
+              *reinterpret_cast<uint4*>(row + ((c ^ (key & 7)) << 4)) =
+                  make_uint4(value_lo(w[y], s, m), value_hi(w[y], s, m), value_lo(h, s, m), value_hi(h, s, m));
+            }
           }
+          fence_proxy_async_smem();
         }
-        fence_proxy_async_smem();
-        named_bar_sync(2, 32 * kFillWarps);  // all of the raw rows have been read, all operands written
-        if (f == 0) {
+        // All of the raw rows have been read, all operands written.  (A warp whose wait expired has made none, but it
+        // comes here as often as the others, who would wait without a bound; the launch has been reported then.)
+        named_bar_sync(2, 32 * kFillWarps);
+        if (f == 0 && !wait.dead) {
           mbar_arrive(which ? &sh.bar.v_full[st] : &sh.bar.k_full[st]);
           mbar_arrive(&sh.bar.raw_empty[which]);
         }
       }
-      if (wait.dead) break;
     }
     steps += n;
-    if (!end_item(sh, wait)) break;
+    alive = end_item(wait);
+    if (!alive) break;
   }
-  if (f < 32 && !sh.dead) {  // the products' last arrivals on this CTA's barriers
+  if (f < 32 && alive) {  // the products' last arrivals on this CTA's barriers
     for (uint32_t x = steps > kStages ? steps - kStages : 0; x < steps; ++x) {
       wait(&sh.bar.k_empty[x % kStages], (x / kStages) & 1);
       wait(&sh.bar.v_empty[x % kStages], (x / kStages) & 1);
@@ -639,9 +643,9 @@ __device__ __forceinline__ void fill_role(const AttendParams& p, Shared& sh, uin
 // ------------------------------------------------------------------ the products of tile i
 template <int D>
 __device__ __forceinline__ void product_role(const AttendParams& p, Shared& sh, uint8_t* s_q, uint8_t* s_k, uint8_t* s_v,
-                                             uint32_t tmem, int i) {
+                                             uint32_t tmem, int i, bool gone) {
   using L = Smem<D>;
-  Wait wait{p};
+  Wait wait{p, gone};
   // operand descriptors; a piece further on is a larger start address, in units of 16 bytes
   const uint64_t d_q = smem_desc_sw128(smem_u32(s_q + i * L::kQ)), d_k = smem_desc_sw128(smem_u32(s_k)),
                  d_v = smem_desc_rows_along_k(smem_u32(s_v));
@@ -690,7 +694,7 @@ __device__ __forceinline__ void product_role(const AttendParams& p, Shared& sh, 
     }
     steps += n_all;
     done += n;
-    if (!end_item(sh, wait)) {
+    if (!end_item(wait)) {
       if (elect_one()) mma_commit(&sh.bar.drained[i]);
       __syncwarp();
       mbar_wait_sleep(&sh.bar.drained[i], 0, p.timeout_ns);
@@ -699,7 +703,9 @@ __device__ __forceinline__ void product_role(const AttendParams& p, Shared& sh, 
   }
 }
 
-template <int D>
+// kExpire: a variant for sp_test_expired_attend, whose warp p.expire_warp of CTA p.expire_cta first waits for what
+// never comes and gives up.
+template <int D, bool kExpire = false>
 __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_constant__ AttendParams p) {
   using L = Smem<D>;
   extern __shared__ uint8_t smem_raw[];
@@ -712,6 +718,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
   const int tid = threadIdx.x, warp = tid >> 5;
   if (tid == 0) {
     mbar_init(&sh.bar.q_full, kRowThreads / 32);
+    mbar_init(&sh.bar.probe, 1);
     for (int i = 0; i < kStages; ++i) {
       mbar_init(&sh.bar.k_full[i], 1);
       mbar_init(&sh.bar.v_full[i], 1);
@@ -728,7 +735,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
       mbar_init(&sh.bar.drained[i], 1);
     }
     fence_barrier_init();
-    sh.dead = 0;
   }
   pdl_wait();
   // the next share of the list, by a warp
@@ -769,18 +775,26 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh.tmem;
+  bool gone = false;
+  if constexpr (kExpire) {
+    if (blockIdx.x == p.expire_cta && warp == p.expire_warp && tid < kBusyThreads && sh.item[0].rows > 0) {
+      Wait wait{p, false};
+      wait(&sh.bar.probe, 0);
+      gone = wait.dead;
+    }
+  }
   // registers: 128 a thread at launch, (176 + 176 + 88 + 72) / 4 from here on
   if (warp < kRowThreads / 32) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
-    rows_role<D>(p, sh, s_q, tmem);
+    rows_role<D>(p, sh, s_q, tmem, gone);
   } else if (warp < kRowThreads / 32 + kFillWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-    fill_role<D>(p, sh, s_k, s_v, s_raw);
+    fill_role<D>(p, sh, s_k, s_v, s_raw, gone);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     const int x = warp - kRowThreads / 32 - kFillWarps;
-    if (x < 2) product_role<D>(p, sh, s_q, s_k, s_v, tmem, x);
-    if (x == 2) copy_role<D>(p, sh, s_raw, fetch);
+    if (x < 2) product_role<D>(p, sh, s_q, s_k, s_v, tmem, x, gone);
+    if (x == 2) copy_role<D>(p, sh, s_raw, fetch, gone);
   }
   tc_fence_before();
   __syncthreads();
@@ -844,7 +858,7 @@ __global__ void __launch_bounds__(128) join_rows_kernel(const __grid_constant__ 
   }
 }
 
-template <int D>
+template <int D, bool kExpire = false>
 sp_status launch(const AttendParams& p, int sms, cudaStream_t stream) {
   static std::atomic<int> set[kMaxDevices] = {};
   int dev = -1;
@@ -853,7 +867,7 @@ sp_status launch(const AttendParams& p, int sms, cudaStream_t stream) {
     return SP_ERR_CUDA;
   }
   const int ok = kept_or_looked_up(set[dev], [] {
-    if (cudaFuncSetAttribute(attend_rows_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    if (cudaFuncSetAttribute(attend_rows_kernel<D, kExpire>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              (int)Smem<D>::kTotal) != cudaSuccess) {
       cudaGetLastError();
       return 0;
@@ -861,7 +875,7 @@ sp_status launch(const AttendParams& p, int sms, cudaStream_t stream) {
     return 1;
   });
   if (!ok) return SP_ERR_CUDA;
-  const sp_status st = launch_pdl(attend_rows_kernel<D>, dim3((unsigned)sms), kThreads, Smem<D>::kTotal, 1, stream, p);
+  const sp_status st = launch_pdl(attend_rows_kernel<D, kExpire>, dim3((unsigned)sms), kThreads, Smem<D>::kTotal, 1, stream, p);
   if (st != SP_OK || p.split == 1) return st;
   return launch_pdl(join_rows_kernel<D>, dim3((unsigned)sms * 4), 128, 0, 1, stream, p);
 }
@@ -875,13 +889,14 @@ size_t attend_rows_part_bytes(int head_dim, int sms) {
 // Where there are fewer items than SMs, the steps of keys are cut into shares.  The host does not
 // see the lengths: it goes by the most items that so many tokens can make (R requests of kManyRows
 // rows or more have sum ceil(rows / 256) <= (all rows + 255 R) / 256).
-sp_status launch_attend_rows(AttendParams p, int head_dim, cudaStream_t stream) {
+sp_status launch_attend_rows(AttendParams p, int head_dim, bool expire, cudaStream_t stream) {
   const int sms = current_sms();
   if (sms == 0) return SP_ERR_CUDA;
   const int64_t rows = p.tokens * p.group, most = std::min<int64_t>(p.requests, rows / kManyRows);
   const int64_t items = (rows + (kPairRows - 1) * most) / kPairRows * p.cache.heads;
   p.parts = sms;
   p.split = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kMostShares, sms / std::max<int64_t>(items, 1)));
+  if (expire) return launch<64, true>(p, sms, stream);
   return head_dim == 64 ? launch<64>(p, sms, stream) : launch<128>(p, sms, stream);
 }
 

@@ -32,11 +32,33 @@ def body(s, name):
 
 def leaves_with_work_behind(text):
     """Whether a role leaves, once any warp has given up, without waiting for what it has issued."""
-    m = re.search(r"if\s*\(!end_item\(sh, wait\)\)\s*", text)
+    m = re.search(r"if\s*\(!end_item\(wait\)\)\s*", text)
     if text[m.end()] != "{":
         return True
     left = text[m.end():closing(text, m.end())]
     return not re.search(r"\bmbar_wait\w*\s*\(", left)
+
+
+def barriers_that_one_warp_can_miss(text):
+    """Where a warp leaves a loop with a barrier of several warps because of its own expired wait."""
+    loops = text[:text.index("end_item(")]
+    assert re.search(r"\bnamed_bar_sync\(2\b", loops)
+    return re.findall(r"\bif\s*\([^)]*\bdead\s*\)\s*\{?\s*(?:break|continue|return)", loops)
+
+
+def test_no_warp_misses_a_barrier_that_others_wait_at():
+    """A warp judges its waits alone: the one that expires and the one that completes at the same moment must
+    meet at the same barriers until the item's end, or the others wait there without a bound."""
+    s = source("sp_attend_rows.cu")
+    assert barriers_that_one_warp_can_miss(body(s, "fill_role")) == []
+    assert not re.search(r"\bsh\.dead\b", s)  # and at its end all get the same verdict, a barrier's, not a flag's
+
+
+def test_the_check_of_barriers_finds_one_that_can_be_missed():
+    loop = "{ for (int j = 0; j < n; ++j) { wait(a); %s named_bar_sync(2, 128); } alive = end_item(wait); if (!alive) break; }"
+    assert barriers_that_one_warp_can_miss(loop % "if (wait.dead) break; fill();")
+    assert barriers_that_one_warp_can_miss(loop % "if (wait.dead) { return; } fill();")
+    assert not barriers_that_one_warp_can_miss(loop % "if (!wait.dead) { fill(); }")
 
 
 def test_roles_that_issue_copies_and_products_wait_for_them_before_the_cta_ends():
@@ -48,6 +70,6 @@ def test_roles_that_issue_copies_and_products_wait_for_them_before_the_cta_ends(
 
 
 def test_the_check_of_roles_finds_one_that_leaves():
-    assert leaves_with_work_behind("{ bulk_g2s(a); if (!end_item(sh, wait)) break; }")
-    assert leaves_with_work_behind("{ if (!end_item(sh, wait)) { x = 1; break; } }")
-    assert not leaves_with_work_behind("{ if (!end_item(sh, wait)) { mbar_wait_sleep(b, 0, t); break; } }")
+    assert leaves_with_work_behind("{ bulk_g2s(a); if (!end_item(wait)) break; }")
+    assert leaves_with_work_behind("{ if (!end_item(wait)) { x = 1; break; } }")
+    assert not leaves_with_work_behind("{ if (!end_item(wait)) { mbar_wait_sleep(b, 0, t); break; } }")

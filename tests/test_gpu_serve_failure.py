@@ -59,6 +59,34 @@ def test_a_warp_that_gives_up_leaves_the_counters_as_they_were(sp, serve, lens, 
     sp.check()
 
 
+@pytest.mark.parametrize("lens,new,heads,kv,page", [([3000, 50, 400], [300, 1, 90], 8, 2, 64), ([900], [700], 32, 32, 16),
+                                                    ([5000], [40], 4, 1, 128)])
+@pytest.mark.parametrize("warp", [0, 5, 8, 10, 11, 12, 13, 14, 15])
+def test_a_role_of_the_kernel_for_many_rows_gives_up(sp, serve, lens, new, heads, kv, page, warp):  # noqa: F811
+    """Each role (rows, codes to operands, products, copies; the last warp has none): the others find their waits
+    expired in turn, the CTA ends, and the counters are at zero."""
+    import time
+
+    import torch
+
+    g = np.random.default_rng(sum(lens))
+    f = Filled(serve, g, lens, new, heads, kv, 64, page)
+    ws = torch.zeros(f.cache.workspace_size(), dtype=torch.uint8, device=gu.dev())
+    want = f.cache.attend(f.qd, f.batch, max(new), workspace=ws)
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    sp.check()
+    gave_up = 0  # (which CTAs find work is their race; of 14 shares, perhaps none of these)
+    for cta in range(0, sms, 8):
+        t0 = time.perf_counter()
+        gave_up += _expire(sp, f, max(new), ws, cta, warp)
+        assert time.perf_counter() - t0 < 2.0
+        assert not ws[:32 * sms].any(), cta
+    assert gave_up == 0 if warp == 15 else gave_up >= 1 or sum(new) == 40
+    for _ in range(2):
+        assert torch.equal(f.cache.attend(f.qd, f.batch, max(new), workspace=ws), want)
+    sp.check()
+
+
 def test_expired_attend_argument_checks(sp, serve):  # noqa: F811
     import torch
 
