@@ -297,12 +297,12 @@ __global__ void __launch_bounds__(kLpThreads, (kLpThreads == kFewThreads ? 2048 
     int n = s_count;
     if (n > kCandidates) {
       // as many equal entries: the best ones one after the other, each below the one before
-      uint64_t below = ~0ull;
+      uint64_t below = 0;
       for (int r = 0; r < p.top; ++r) {
         uint64_t best = 0;
         auto look = [&](float f, int64_t at) {
           const uint64_t k = ((uint64_t)key_of(f) << 32) | (uint32_t)~(uint32_t)at;
-          if (k < below && k > best) best = k;
+          if (k > best && (r == 0 || k < below)) best = k;  // (a NaN at index 0 is ~0)
         };
         if (any && own >= tau) {
           for (int64_t i = v0 + tid; i < v1; i += kLpThreads) {

@@ -8,6 +8,7 @@ import pytest
 
 from paper_2405_03594_gb300 import synth
 from tests import gpu_util as gu
+from tests import serve_ref as ref
 from tests.test_gpu_serve import Filled, _near, serve, sp  # noqa: F401  (fixtures)
 
 pytestmark = pytest.mark.gpu
@@ -47,3 +48,36 @@ def test_queries_near_the_end_of_the_range(sp, serve, heads, kv, new, d):  # noq
     y = f.cache.attend(f.qd, f.batch, max(new))
     sp.check()
     _near(y, f.want(), f.vmax())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("t,v", [(9, 130), (9, 1100), (9, 32000), (3, 131071), (700, 1500)])
+def test_order_of_rows_that_are_not_finite(sp, serve, dtype, t, v):  # noqa: F811
+    """All NaN (more of them than the kernel lists at a time, too), NaN at the first entries, among infinities:
+    a NaN counts as the largest, equal ones go by rising index."""
+    import torch
+
+    g = np.random.default_rng(v)
+    x = (2 * g.standard_normal((t, v))).astype(np.float32)
+    x[0] = np.nan
+    x[1, 0] = np.nan
+    x[2, : v // 2] = np.inf
+    if t > 3:
+        x[3, 3:] = np.nan
+        x[4, [0, 5, v - 1]] = np.nan
+        x[4, [1, 7]] = np.inf
+        x[5] = -np.inf
+        x[6] = np.inf
+        x[7], x[7, 0] = -np.inf, np.nan
+    xd = torch.tensor(x, device=gu.dev())
+    if dtype == "bf16":
+        xd = xd.bfloat16()
+        x = xd.float().cpu().numpy()
+    for top in (1, 20, 64):
+        ids = g.integers(0, v, t)
+        lp, en, tl, ti = serve.token_logprobs(xd, torch.tensor(ids, device=gu.dev()), top)
+        wl, we, wt, wi = ref.logprobs(x.astype(np.float64), ids, top)
+        assert np.array_equal(ti.cpu().numpy(), wi), top
+        for a, e in ((lp, wl), (en, we), (tl, wt)):
+            assert np.array_equal(np.isnan(a.cpu().numpy()), np.isnan(e))
+    sp.check()
