@@ -179,7 +179,8 @@ sp_status sp_kv4_attend_workspace_size(int32_t head_dim, size_t* bytes);
  *   logp_out   [tokens] fp32: x[id] - log(sum(exp(x)))
  *   entropy_out [tokens] fp32: -sum(p * log p)
  *   top        0..64 entries: top_logp_out fp32 and top_ids_out int64, [tokens][top], by falling
- *              logit, equal ones by rising index (a NaN counts as the largest); top <= vocab
+ *              logit, equal ones by rising index; -0 comes below +0, and a NaN counts as the largest;
+ *              top <= vocab
  * Sums are fp32 around the row's maximum.  A row of nothing but -inf has log probabilities of -inf and
  * entropy 0; one with a NaN or +inf is NaN.  One launch.  tokens == 0 returns SP_OK. */
 typedef enum sp_logits_dtype { SP_LOGITS_BF16 = 0, SP_LOGITS_F32 = 1 } sp_logits_dtype;

@@ -34,7 +34,7 @@ constexpr int kMaxCluster = 8;
 constexpr int kCandidates = 1024;
 constexpr float kLog2e = 1.4426950408889634f;
 
-// Keys in the order of the numbers, NaN above all; none is 0.
+// Keys in the order of the numbers, -0 below +0 and NaN above all; none is 0.
 __device__ __forceinline__ uint32_t key_of(float x) {
   const uint32_t u = __float_as_uint(x);
   if ((u & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;

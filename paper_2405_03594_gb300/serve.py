@@ -246,7 +246,7 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, str
     """sp_token_logprobs: of each row of logits [T, V] (bf16 or float32, rows of unit stride), the log
     probability of tokens[t] (int64; a negative one asks for nothing and gets 0) and the entropy, both
     float32 [T]; with top > 0 also the `top` most likely entries: log probabilities [T, top] and ids
-    (int64), by falling logit and, among equal ones, rising id."""
+    (int64), by falling logit (-0 below +0, a NaN above all) and, among equal ones, rising id."""
     dtype = logits.dtype
     if (dtype is not _BF16 and dtype is not _F32) or logits.dim() != 2 or logits.stride(1) != 1 or not logits.is_cuda:
         raise ValueError("logits: bf16 or float32 [T, V] with unit column stride on a GPU wanted")

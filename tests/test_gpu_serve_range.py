@@ -81,3 +81,21 @@ def test_order_of_rows_that_are_not_finite(sp, serve, dtype, t, v):  # noqa: F81
         for a, e in ((lp, wl), (en, we), (tl, wt)):
             assert np.array_equal(np.isnan(a.cpu().numpy()), np.isnan(e))
     sp.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("v", [40, 3001, 70000])
+def test_zeros_of_either_sign(sp, serve, dtype, v):  # noqa: F811
+    """-0 comes below +0, each by rising index; their log probabilities are the same."""
+    import torch
+
+    x = torch.full((3, v), -1.0)
+    x[0, : v // 2] = -0.0
+    x[0, 1:12:3] = 0.0
+    x[1] = -0.0
+    x[2] = 0.0
+    lp, _, tl, ti = serve.token_logprobs(x.to(gu.dev()).to(torch.bfloat16 if dtype == "bf16" else torch.float32),
+                                         torch.zeros(3, dtype=torch.int64, device=gu.dev()), 8)
+    sp.check()
+    assert ti.tolist() == [[1, 4, 7, 10, 0, 2, 3, 5], list(range(8)), list(range(8))]
+    assert torch.equal(tl, lp[:, None].expand(3, 8))
