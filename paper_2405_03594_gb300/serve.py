@@ -26,6 +26,7 @@ from .sp import SpAttendArgs, SpKv4, SpKvPlanArgs, SpRopeArgs, _check, _lib, _st
 PLAN_PAGES, PLAN_WIDTH, PLAN_TOKENS, PLAN_INPUT = 1, 2, 4, 8  # SP_PLAN_*
 
 _BF16, _F32, _I32, _I64 = torch.bfloat16, torch.float32, torch.int32, torch.int64
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _CODES = {ctypes.c_void_p: "P", ctypes.c_int64: "q", ctypes.c_int32: "i", ctypes.c_float: "f"}
 
 
@@ -48,13 +49,22 @@ _read = _lib["sp_kv4_read"]  # (the cache by its address)
 _read.argtypes, _read.restype = [ctypes.c_void_p, *_lib.sp_kv4_read.argtypes[1:]], ctypes.c_int
 
 
-def _heads(x: torch.Tensor, heads: int | None, dim: int, name: str) -> tuple[int, int, int]:
-    """Checks x [tokens, heads, dim] bf16 with contiguous heads (a view of a fused row serves) and
-    returns its tokens, heads and token stride."""
+def _gpu_of(x: torch.Tensor, name: str) -> int:
+    """The index of the current GPU, on which x has to be: a call's launches go there, and every other
+    address that it hands over has to be that GPU's."""
+    dev = x.get_device()
+    if dev < 0 or dev != _current_device():
+        raise ValueError(f"{name}: a tensor on the current GPU wanted, got one on {x.device}")
+    return dev
+
+
+def _heads(x: torch.Tensor, heads: int | None, dim: int, dev: int, name: str) -> tuple[int, int, int]:
+    """Checks x [tokens, heads, dim] bf16 on GPU `dev` with contiguous heads (a view of a fused row serves)
+    and returns its tokens, heads and token stride."""
     shape, stride = x.shape, x.stride()
     if (x.dtype is not _BF16 or len(shape) != 3 or shape[2] != dim or (heads is not None and shape[1] != heads)
-            or not x.is_cuda):
-        raise ValueError(f"{name}: bf16 [tokens, {'heads' if heads is None else heads}, {dim}] on a GPU wanted, "
+            or x.get_device() != dev):
+        raise ValueError(f"{name}: bf16 [tokens, {'heads' if heads is None else heads}, {dim}] on GPU {dev} wanted, "
                          f"got {x.dtype} {list(shape)} on {x.device}")
     t, h, _ = shape
     if stride[2] != 1 or (h > 1 and stride[1] != dim):
@@ -62,53 +72,55 @@ def _heads(x: torch.Tensor, heads: int | None, dim: int, name: str) -> tuple[int
     return t, h, stride[0] if t > 1 else max(stride[0], h * dim)
 
 
-def _index(x: torch.Tensor, n: int, dtype, name: str) -> int:
-    """Checks a contiguous vector of n entries or more and returns its address."""
-    if x.dtype is not dtype or x.dim() != 1 or x.shape[0] < n or not x.is_contiguous() or not x.is_cuda:
-        raise ValueError(f"{name}: contiguous {dtype} [{n}] on a GPU wanted, got {x.dtype} {list(x.shape)} on {x.device}")
+def _index(x: torch.Tensor, n: int, dtype, dev: int, name: str) -> int:
+    """Checks a contiguous vector of n entries or more on GPU `dev` and returns its address."""
+    if x.dtype is not dtype or x.dim() != 1 or x.shape[0] < n or not x.is_contiguous() or x.get_device() != dev:
+        raise ValueError(f"{name}: contiguous {dtype} [{n}] on GPU {dev} wanted, got {x.dtype} {list(x.shape)} on {x.device}")
     return x.data_ptr()
 
 
-def _weight(w: torch.Tensor | None, dim: int, name: str) -> int:
+def _weight(w: torch.Tensor | None, dim: int, dev: int, name: str) -> int:
     if w is None:
         return 0
-    if w.dtype is not _BF16 or w.shape != (dim,) or not w.is_contiguous() or not w.is_cuda:
-        raise ValueError(f"{name}: contiguous bf16 [{dim}] on a GPU wanted")
+    if w.dtype is not _BF16 or w.shape != (dim,) or not w.is_contiguous() or w.get_device() != dev:
+        raise ValueError(f"{name}: contiguous bf16 [{dim}] on GPU {dev} wanted")
     return w.data_ptr()
 
 
-def _output(out: torch.Tensor | None, t: int, h: int, dim: int, like: torch.Tensor, name: str) -> torch.Tensor:
+def _output(out: torch.Tensor | None, t: int, h: int, dim: int, like: torch.Tensor, dev: int, name: str) -> torch.Tensor:
     if out is None:
         return torch.empty((t, h, dim), dtype=_BF16, device=like.device)  # (new_empty takes 1 us longer)
-    if out.dtype is not _BF16 or out.shape != (t, h, dim) or not out.is_contiguous() or not out.is_cuda:
-        raise ValueError(f"{name}: contiguous bf16 {[t, h, dim]} on a GPU wanted")
+    if out.dtype is not _BF16 or out.shape != (t, h, dim) or not out.is_contiguous() or out.get_device() != dev:
+        raise ValueError(f"{name}: contiguous bf16 {[t, h, dim]} on GPU {dev} wanted")
     return out
 
 
 def _run_rope(q, k, v, positions, cos_sin, q_weight, k_weight, eps, pairs, q_out, k_out, cache, slots, stream):
-    dim = q.shape[-1]
-    t, h, q_stride = _heads(q, None, dim, "q")
-    tk, kv, k_stride = _heads(k, None, dim, "k")
+    dim, dev = q.shape[-1], _gpu_of(q, "q")
+    t, h, q_stride = _heads(q, None, dim, dev, "q")
+    tk, kv, k_stride = _heads(k, None, dim, dev, "k")
     if tk != t:
         raise ValueError("q and k hold different numbers of tokens")
-    if cos_sin.dtype is not _F32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous() or not cos_sin.is_cuda:
-        raise ValueError("cos_sin: contiguous float32 [rows, rot] on a GPU wanted")
+    if cos_sin.dtype is not _F32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous() or cos_sin.get_device() != dev:
+        raise ValueError(f"cos_sin: contiguous float32 [rows, rot] on GPU {dev} wanted")
     rows, rot = cos_sin.shape
-    pos = _index(positions, t, _I32, "positions")
-    qw, kw = _weight(q_weight, dim, "q_weight"), _weight(k_weight, dim, "k_weight")
-    q_out = _output(q_out, t, h, dim, q, "q_out")
+    pos = _index(positions, t, _I32, dev, "positions")
+    qw, kw = _weight(q_weight, dim, dev, "q_weight"), _weight(k_weight, dim, dev, "k_weight")
+    if cache is not None:
+        cache._check_gpu(dev)
+    q_out = _output(q_out, t, h, dim, q, dev, "q_out")
     if cache is None:
-        k_out = _output(k_out, t, kv, dim, k, "k_out")
+        k_out = _output(k_out, t, kv, dim, k, dev, "k_out")
         v_ptr = v_stride = slot = where = 0
         k_ptr = k_out.data_ptr()
     else:
-        tv, _, v_stride = _heads(v, kv, dim, "v")
+        tv, _, v_stride = _heads(v, kv, dim, dev, "v")
         if tv != t:
             raise ValueError("k and v hold different numbers of tokens")
-        slot, where, v_ptr, k_ptr = _index(slots, t, _I64, "slots"), cache._address, v.data_ptr(), 0
+        slot, where, v_ptr, k_ptr = _index(slots, t, _I64, dev, "slots"), cache._address, v.data_ptr(), 0
     _check(_rope(_pack_rope(q.data_ptr(), k.data_ptr(), v_ptr, q_stride, k_stride, v_stride, q_out.data_ptr(), k_ptr,
                             where, slot, pos, cos_sin.data_ptr(), rows, qw, kw, eps, t, h, kv, dim, rot,
-                            1 if pairs else 0), _stream(stream, q.device.index)), "sp_qk_norm_rope")
+                            1 if pairs else 0), _stream(stream, dev)), "sp_qk_norm_rope")
     return q_out, k_out
 
 
@@ -124,7 +136,7 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, cos_
 
 class KvCache:
     """Keys and values of one layer in 4 bits, in pages of `page_size` tokens (the format is in
-    include/sp_serve.h).  `data`: a uint8 buffer to use instead of a new one."""
+    include/sp_serve.h).  `data`: a uint8 buffer on the GPU of the calls to use instead of a new one."""
 
     def __init__(self, pages: int, kv_heads: int, head_dim: int, page_size: int = 64, device=None,
                  data: torch.Tensor | None = None):
@@ -140,7 +152,12 @@ class KvCache:
         self.data = data
         self._c.data = data.data_ptr()
         self._address = ctypes.addressof(self._c)
+        self._gpu = data.get_device()
         self._ws_bytes = 0
+
+    def _check_gpu(self, dev: int) -> None:
+        if self._gpu != dev:
+            raise ValueError(f"the cache's buffer is on {self.data.device}, GPU {dev} wanted")
 
     def append(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor,
                cos_sin: torch.Tensor, q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None,
@@ -151,12 +168,14 @@ class KvCache:
 
     def read(self, slots: torch.Tensor, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
         """The cached keys and values at `slots` (int64 [n]) as bf16 [n, kv_heads, head_dim]."""
-        at = _index(slots, 0, _I64, "slots")
+        dev = _gpu_of(slots, "slots")
+        at = _index(slots, 0, _I64, dev, "slots")
+        self._check_gpu(dev)
         n = slots.shape[0]
         device = slots.device
         shape = (n, self.kv_heads, self.head_dim)
         k, v = torch.empty(shape, dtype=_BF16, device=device), torch.empty(shape, dtype=_BF16, device=device)
-        _check(_read(self._address, at, n, k.data_ptr(), v.data_ptr(), _stream(stream, device.index)), "sp_kv4_read")
+        _check(_read(self._address, at, n, k.data_ptr(), v.data_ptr(), _stream(stream, dev)), "sp_kv4_read")
         return k, v
 
     def attend(self, q: torch.Tensor, batch: "Batch", max_new: int, scale: float | None = None,
@@ -164,13 +183,16 @@ class KvCache:
         """Causal attention of q [T, H, D] (the step's tokens, request by request) over the cache by
         the tables of `batch`; max_new: at least the most new tokens of a request; scale: 1 / sqrt(D)
         by default.  Rows behind the step's last token keep what `out` held."""
-        dim = self.head_dim
-        t, h, q_stride = _heads(q, batch.heads, dim, "q")
+        dim, dev = self.head_dim, _gpu_of(q, "q")
+        t, h, q_stride = _heads(q, batch.heads, dim, dev, "q")
+        self._check_gpu(dev)
+        if batch._gpu != dev:
+            raise ValueError(f"the batch's tables are not on GPU {dev}")
         device = q.device
         if out is None:
             out, out_stride = torch.empty((t, h, dim), dtype=_BF16, device=device), h * dim
         else:
-            to, _, out_stride = _heads(out, h, dim, "out")
+            to, _, out_stride = _heads(out, h, dim, dev, "out")
             if to != t:
                 raise ValueError("q and out hold different numbers of tokens")
         if self.kv_heads != batch.kv_heads or self.page_size != batch.page_size:
@@ -181,7 +203,7 @@ class KvCache:
                                     batch.table.data_ptr(), batch.lens.data_ptr(), batch.cu_q.data_ptr(),
                                     batch.work.data_ptr(), t, batch.requests, batch.width, h, max_new,
                                     1.0 / math.sqrt(dim) if scale is None else scale, 0),
-                       workspace.data_ptr(), workspace.numel(), _stream(stream, device.index)), "sp_kv4_attend")
+                       workspace.data_ptr(), workspace.numel(), _stream(stream, dev)), "sp_kv4_attend")
         return out
 
     def workspace_size(self) -> int:
@@ -209,6 +231,7 @@ class Batch:
         self.heads, self.kv_heads, self.page_size, self.pages = heads, cache.kv_heads, cache.page_size, cache.pages
         self.requests, self.tokens, self.width = requests, tokens, width
         dev = cache.data.device
+        self._gpu = cache._gpu
         i32 = dict(dtype=torch.int32, device=dev)
         self.cached = torch.zeros(requests, **i32)
         self.table = torch.full((requests, width), -1, **i32)
@@ -229,7 +252,10 @@ class Batch:
         (cached, free_count); otherwise they stay, and the step can be planned again.  allocate=False:
         `table` already holds every page of the step.  A step that does not fit leaves everything as it
         is, has no tokens, and says why in `status` (PLAN_*)."""
-        at = _index(new, self.requests, _I32, "new")
+        dev = _gpu_of(new, "new")
+        at = _index(new, self.requests, _I32, dev, "new")
+        if self._gpu != dev:
+            raise ValueError(f"the batch's tables are not on GPU {dev}")
         self.lens = self.cached if advance else self._lens
         self.next_count = self.free_count if advance else self._next_count
         _check(_plan(_pack_plan(self.cached.data_ptr(), at, self.table.data_ptr(),
@@ -238,7 +264,7 @@ class Batch:
                                 self.work.data_ptr(), self.slots.data_ptr(), self.positions.data_ptr(),
                                 self.status.data_ptr(), self.tokens, self.pages, self.requests, self.width,
                                 self.page_size, self.heads // self.kv_heads),
-                     _stream(stream, new.device.index)), "sp_kv_plan")
+                     _stream(stream, dev)), "sp_kv_plan")
         return self
 
 
@@ -248,10 +274,11 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, str
     float32 [T]; with top > 0 also the `top` most likely entries: log probabilities [T, top] and ids
     (int64), by falling logit (-0 below +0, a NaN above all) and, among equal ones, rising id."""
     dtype = logits.dtype
-    if (dtype is not _BF16 and dtype is not _F32) or logits.dim() != 2 or logits.stride(1) != 1 or not logits.is_cuda:
+    if (dtype is not _BF16 and dtype is not _F32) or logits.dim() != 2 or logits.stride(1) != 1:
         raise ValueError("logits: bf16 or float32 [T, V] with unit column stride on a GPU wanted")
     t, v = logits.shape
-    ids = _index(tokens, t, _I64, "tokens")
+    dev = _gpu_of(logits, "logits")
+    ids = _index(tokens, t, _I64, dev, "tokens")
     device = logits.device
     logp, entropy = torch.empty(t, dtype=_F32, device=device), torch.empty(t, dtype=_F32, device=device)
     tl = ti = None
@@ -259,6 +286,6 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, str
         tl, ti = torch.empty((t, top), dtype=_F32, device=device), torch.empty((t, top), dtype=_I64, device=device)
     _check(_lib.sp_token_logprobs(logits.data_ptr(), 0 if dtype is _BF16 else 1, logits.stride(0) if t > 1 else v, t, v,
                                   ids, top, logp.data_ptr(), entropy.data_ptr(), tl.data_ptr() if top else None,
-                                  ti.data_ptr() if top else None, _stream(stream, device.index)),
+                                  ti.data_ptr() if top else None, _stream(stream, dev)),
            "sp_token_logprobs")
     return (logp, entropy, tl, ti) if top else (logp, entropy)

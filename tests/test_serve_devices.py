@@ -1,0 +1,78 @@
+"""The serving calls' checks of where their tensors are: whatever hands an address to a kernel has to be on
+the GPU of the call (CPU: tensors that say they are on a GPU stand in for those that are)."""
+import pytest
+import torch
+
+from paper_2405_03594_gb300 import serve
+
+
+class OnGpu(torch.Tensor):
+    """A host tensor that says that it is on GPU 0; no call below gets as far as its address."""
+
+    is_cuda = True
+
+    def get_device(self):
+        return 0
+
+
+class Stream:
+    cuda_stream = 0
+
+
+def gpu(x):
+    return x.as_subclass(OnGpu)
+
+
+@pytest.fixture(autouse=True)
+def _current(monkeypatch):
+    if hasattr(serve, "_current_device"):
+        monkeypatch.setattr(serve, "_current_device", lambda: 0)
+
+
+def _cache(on_gpu):
+    data = torch.zeros(4 * 2 * 16 * 72, dtype=torch.uint8)
+    return serve.KvCache(4, 2, 64, 16, data=gpu(data) if on_gpu else data)
+
+
+def _tensors():
+    return dict(q=torch.zeros((3, 4, 64), dtype=torch.bfloat16), k=torch.zeros((3, 2, 64), dtype=torch.bfloat16),
+                v=torch.zeros((3, 2, 64), dtype=torch.bfloat16), positions=torch.zeros(3, dtype=torch.int32),
+                slots=torch.zeros(3, dtype=torch.int64), cos_sin=torch.zeros((4, 64)),
+                q_weight=torch.zeros(64, dtype=torch.bfloat16), k_weight=torch.zeros(64, dtype=torch.bfloat16),
+                out=torch.zeros((3, 4, 64), dtype=torch.bfloat16))
+
+
+def _refused(call, what="GPU"):
+    with pytest.raises(ValueError, match=what):
+        call()
+
+
+def test_a_cache_outside_the_calls_gpu_is_refused():
+    c, t = _cache(False), {k: gpu(x) for k, x in _tensors().items()}
+    _refused(lambda: c.append(**t, stream=Stream), "buffer")
+    _refused(lambda: c.read(t["slots"], stream=Stream), "buffer")
+    b = serve.Batch(c, 4, 1, 3, 1)
+    ws = gpu(torch.zeros(1 << 25, dtype=torch.uint8))
+    _refused(lambda: c.attend(t["q"], b, 3, out=t["out"], workspace=ws, stream=Stream), "buffer")
+    _refused(lambda: _cache(True).attend(t["q"], b, 3, out=t["out"], workspace=ws, stream=Stream), "batch")
+    _refused(lambda: b.plan(t["positions"][:1], stream=Stream), "batch")
+
+
+@pytest.mark.parametrize("name", list(_tensors()))
+def test_one_tensor_elsewhere_is_refused(name):
+    t = {k: x if k == name else gpu(x) for k, x in _tensors().items()}
+    _refused(lambda: _cache(True).append(**t, stream=Stream))
+
+
+def test_tensors_of_another_gpu_than_the_current_one_are_refused(monkeypatch):
+    monkeypatch.setattr(serve, "_current_device", lambda: 1)
+    t = {k: gpu(x) for k, x in _tensors().items()}
+    _refused(lambda: _cache(True).append(**t, stream=Stream))
+    _refused(lambda: serve.token_logprobs(t["cos_sin"], t["slots"], stream=Stream))
+    _refused(lambda: _cache(True).read(t["slots"], stream=Stream))
+
+
+def test_ids_and_logits_on_two_devices_are_refused():
+    t = _tensors()
+    _refused(lambda: serve.token_logprobs(gpu(t["cos_sin"][:3]), t["slots"], stream=Stream))
+    _refused(lambda: serve.token_logprobs(t["cos_sin"][:3], gpu(t["slots"]), stream=Stream))
