@@ -149,11 +149,16 @@ class KvCache:
         elif data.dtype != torch.uint8 or data.numel() != b.value or not data.is_contiguous():
             raise ValueError(f"data: {b.value} contiguous bytes wanted")
         self.pages, self.kv_heads, self.head_dim, self.page_size = pages, kv_heads, head_dim, page_size
-        self.data = data
+        self._data = data
         self._c.data = data.data_ptr()
         self._address = ctypes.addressof(self._c)
         self._gpu = data.get_device()
         self._ws_bytes = 0
+
+    @property
+    def data(self) -> torch.Tensor:
+        """The buffer; its address is the cache's for life."""
+        return self._data
 
     def _check_gpu(self, dev: int) -> None:
         if self._gpu != dev:
@@ -223,7 +228,28 @@ class Batch:
         free [pages] int32, free_count [1]                      stack of unused pages
         lens, cu_q, slots, positions, next_count, status        what plan() writes
 
-    A fresh batch has no tokens and every page on the stack."""
+    A fresh batch has no tokens and every page on the stack.  Another tensor of the same type on the
+    same device, no smaller, may take the place of one of these; the sizes stay what they are."""
+
+    _TABLES = {"cached": (_I32, lambda b: (b.requests,)), "table": (_I32, lambda b: (b.requests, b.width)),
+               "free": (_I32, lambda b: (b.pages,)), "free_count": (_I32, lambda b: (1,)),
+               "lens": (_I32, lambda b: (b.requests,)), "next_count": (_I32, lambda b: (1,)),
+               "cu_q": (_I32, lambda b: (b.requests + 1,)), "work": (_I32, lambda b: (3 * (b.requests + 1),)),
+               "slots": (_I64, lambda b: (b.tokens,)), "positions": (_I32, lambda b: (b.tokens,)),
+               "status": (_I32, lambda b: (1,))}
+    _SIZES = frozenset(("heads", "kv_heads", "page_size", "pages", "requests", "tokens", "width", "_gpu"))
+
+    def __setattr__(self, name, value):
+        # (the kernels go by the sizes: checked here once, so that no call has to)
+        if name in self._TABLES:
+            dtype, shape = self._TABLES[name][0], self._TABLES[name][1](self)
+            if (not isinstance(value, torch.Tensor) or value.dtype is not dtype or value.dim() != len(shape)
+                    or (value.shape[0] < shape[0] if len(shape) == 1 else tuple(value.shape) != shape)
+                    or not value.is_contiguous() or value.get_device() != self._gpu):
+                raise ValueError(f"{name}: contiguous {dtype} {list(shape)} on the batch's device wanted")
+        elif name in self._SIZES and name in self.__dict__:
+            raise AttributeError(f"{name}: a batch's sizes are those it was made with")
+        object.__setattr__(self, name, value)
 
     def __init__(self, cache: KvCache, heads: int, requests: int, tokens: int, width: int):
         if heads < 1 or heads % cache.kv_heads:
@@ -256,8 +282,9 @@ class Batch:
         at = _index(new, self.requests, _I32, dev, "new")
         if self._gpu != dev:
             raise ValueError(f"the batch's tables are not on GPU {dev}")
-        self.lens = self.cached if advance else self._lens
-        self.next_count = self.free_count if advance else self._next_count
+        own = self.__dict__  # (these tensors have been checked)
+        own["lens"] = self.cached if advance else self._lens
+        own["next_count"] = self.free_count if advance else self._next_count
         _check(_plan(_pack_plan(self.cached.data_ptr(), at, self.table.data_ptr(),
                                 self.free.data_ptr() if allocate else 0, self.free_count.data_ptr(),
                                 self.next_count.data_ptr(), self.lens.data_ptr(), self.cu_q.data_ptr(),

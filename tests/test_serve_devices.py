@@ -76,3 +76,29 @@ def test_ids_and_logits_on_two_devices_are_refused():
     t = _tensors()
     _refused(lambda: serve.token_logprobs(gpu(t["cos_sin"][:3]), t["slots"], stream=Stream))
     _refused(lambda: serve.token_logprobs(t["cos_sin"][:3], gpu(t["slots"]), stream=Stream))
+
+
+def test_a_batchs_tables_keep_their_type_and_size():
+    """A table that is exchanged for a smaller one, or one of other entries, would be read past its end."""
+    b = serve.Batch(_cache(False), 4, 3, 5, 2)
+    i32 = dict(dtype=torch.int32)
+    good = dict(cached=torch.ones(3, **i32), table=torch.ones((3, 2), **i32), free=torch.ones(4, **i32),
+                free_count=torch.ones(1, **i32), lens=torch.ones(3, **i32), next_count=torch.ones(1, **i32),
+                cu_q=torch.ones(4, **i32), work=torch.ones(12, **i32), slots=torch.ones(5, dtype=torch.int64),
+                positions=torch.ones(5, **i32), status=torch.ones(1, **i32))
+    for name, x in good.items():
+        setattr(b, name, x)
+        assert getattr(b, name) is x
+        wide = torch.ones((*x.shape[:-1], 2 * x.shape[-1]), dtype=x.dtype)
+        for bad in (x[:0], x.float(), x.to(torch.int64 if x.dtype == torch.int32 else torch.int32), gpu(x), None,
+                    *([wide[..., ::2]] if x.numel() > 1 else [])):
+            with pytest.raises(ValueError, match=name):
+                setattr(b, name, bad)
+        assert getattr(b, name) is x
+        if x.dim() == 1:
+            setattr(b, name, wide)
+    for name in ("heads", "kv_heads", "page_size", "pages", "requests", "tokens", "width"):
+        with pytest.raises(AttributeError):
+            setattr(b, name, 100)
+    with pytest.raises(AttributeError):
+        _cache(False).data = torch.zeros(5, dtype=torch.uint8)
