@@ -187,7 +187,8 @@ class KvCache:
                out: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
         """Causal attention of q [T, H, D] (the step's tokens, request by request) over the cache by
         the tables of `batch`; max_new: at least the most new tokens of a request; scale: 1 / sqrt(D)
-        by default.  Rows behind the step's last token keep what `out` held."""
+        by default.  Rows behind the step's last token keep what `out` held.  workspace: workspace_size()
+        bytes (uint8) to use instead of the stream's own, zero at first as include/sp_serve.h says."""
         dim, dev = self.head_dim, _gpu_of(q, "q")
         t, h, q_stride = _heads(q, batch.heads, dim, dev, "q")
         self._check_gpu(dev)
@@ -204,6 +205,8 @@ class KvCache:
             raise ValueError("the batch was planned for another kind of cache")
         if workspace is None:
             workspace = sp.workspace_for(self.workspace_size(), device, stream)
+        elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.get_device() != dev:
+            raise ValueError(f"workspace: contiguous bytes (uint8) on GPU {dev} wanted")
         _check(_attend(_pack_attend(q.data_ptr(), out.data_ptr(), q_stride, out_stride, self._address,
                                     batch.table.data_ptr(), batch.lens.data_ptr(), batch.cu_q.data_ptr(),
                                     batch.work.data_ptr(), t, batch.requests, batch.width, h, max_new,

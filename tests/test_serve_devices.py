@@ -102,3 +102,12 @@ def test_a_batchs_tables_keep_their_type_and_size():
             setattr(b, name, 100)
     with pytest.raises(AttributeError):
         _cache(False).data = torch.zeros(5, dtype=torch.uint8)
+
+
+def test_a_workspace_elsewhere_or_of_other_entries_is_refused():
+    c = _cache(True)
+    b, q = serve.Batch(_cache(False), 4, 1, 3, 1), gpu(_tensors()["q"])
+    b.__dict__["_gpu"] = 0  # (a batch makes its tables where the buffer is)
+    ws = torch.zeros(1 << 25, dtype=torch.uint8)
+    for bad in (ws, gpu(ws)[::2], gpu(ws.view(torch.int32))):
+        _refused(lambda: c.attend(q, b, 3, out=torch.empty_like(q), workspace=bad, stream=Stream), "workspace")
