@@ -38,8 +38,8 @@
 extern "C" {
 #endif
 
-/* A cache.  data: pages * kv_heads * page_size * (head_dim + 8) bytes.  page_size 16, 32, 64 or
- * 128, head_dim 64 or 128 (SP_ERR_UNSUPPORTED otherwise). */
+/* A cache.  data: pages * kv_heads * page_size * (head_dim + 8) bytes, fewer than 2^63.  page_size 16, 32,
+ * 64 or 128, head_dim 64 or 128 (SP_ERR_UNSUPPORTED otherwise). */
 typedef struct sp_kv4 {
   void* data;
   int64_t pages;

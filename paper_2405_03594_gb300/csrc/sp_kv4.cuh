@@ -32,9 +32,11 @@ struct Kv4 {
   int32_t heads;
 };
 
+// (the buffer's bytes, and so every slot and offset, are 63-bit numbers; of a positive cache)
 inline bool kv4_supported(const sp_kv4* c) {
   return (c->page_size == 16 || c->page_size == 32 || c->page_size == 64 || c->page_size == 128) &&
-         (c->head_dim == 64 || c->head_dim == 128);
+         (c->head_dim == 64 || c->head_dim == 128) &&
+         c->pages <= INT64_MAX / ((int64_t)c->page_size * (c->head_dim + 8)) / c->kv_heads;
 }
 inline bool kv4_positive(const sp_kv4* c) { return c->pages > 0 && c->kv_heads > 0; }
 inline int page_shift(int page_size) { return __builtin_ctz((unsigned)page_size); }

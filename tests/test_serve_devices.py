@@ -111,3 +111,22 @@ def test_a_workspace_elsewhere_or_of_other_entries_is_refused():
     ws = torch.zeros(1 << 25, dtype=torch.uint8)
     for bad in (ws, gpu(ws)[::2], gpu(ws.view(torch.int32))):
         _refused(lambda: c.attend(q, b, 3, out=torch.empty_like(q), workspace=bad, stream=Stream), "workspace")
+
+
+def test_a_cache_of_more_bytes_than_an_offset_holds_is_refused():
+    """2^52 pages of 32 heads of 128: 136 * 2^64 bytes, which a 64-bit product takes for none."""
+    import ctypes
+
+    from paper_2405_03594_gb300 import sp
+
+    b = ctypes.c_size_t()
+    for pages, heads in ((1 << 52, 32), (1 << 62, 1), ((1 << 63) - 1, 1), (1 << 33, 1 << 30)):
+        c = sp.SpKv4(1 << 20, pages, 128, heads, 128, 0)
+        assert sp._lib.sp_kv4_bytes(c, ctypes.byref(b)) == 2, pages
+        assert sp._lib.sp_kv4_read(c, 1 << 20, 1, 1 << 20, 1 << 20, None) == 2, pages
+        with pytest.raises(sp.SpError):
+            serve.KvCache(pages, heads, 128, 128, data=torch.zeros(0, dtype=torch.uint8))
+    most = ((1 << 63) - 1) // (128 * 136)
+    assert sp._lib.sp_kv4_bytes(sp.SpKv4(None, most, 128, 1, 128, 0), ctypes.byref(b)) == 0
+    assert b.value == most * 128 * 136
+    assert sp._lib.sp_kv4_bytes(sp.SpKv4(None, most + 1, 128, 1, 128, 0), ctypes.byref(b)) == 2
