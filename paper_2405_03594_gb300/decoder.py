@@ -36,7 +36,8 @@ class Decoder:
     """layers: one dict of SparseMatrix per layer, with the names of NAMES -- qkv [(H + 2 Hkv) D, d], o [d, H D],
     gate_up [2F, d] (rows interleaved: gate_j, up_j), down [d, F]; embed [V, d] bf16; head: SparseMatrix [V, d].
     Up to `requests` requests of up to `width` pages each share `pages` pages; a step has up to `tokens` new
-    tokens, and token positions up to `positions`."""
+    tokens.  The rotation's table has `positions` rows, or as many as the `width` pages of a request hold if
+    that is more, so that every token has its own."""
 
     def __init__(self, layers, embed: torch.Tensor, head: sp.SparseMatrix, heads: int, kv_heads: int, pages: int,
                  requests: int, tokens: int, width: int, page_size: int = 64, positions: int = 8192,
@@ -51,7 +52,7 @@ class Decoder:
             raise ValueError("layers: shapes that do not belong together")
         dev = embed.device
         self.norms = dict(q_weight=q_weight, k_weight=k_weight)
-        self.cos_sin = rotation_table(positions, self.dim, device=dev)
+        self.cos_sin = rotation_table(max(positions, width * page_size), self.dim, device=dev)
         self.caches = [KvCache(pages, kv_heads, self.dim, page_size, device=dev) for _ in layers]
         self.batch = Batch(self.caches[0], heads, requests, tokens, width)
         bf = dict(dtype=torch.bfloat16, device=dev)

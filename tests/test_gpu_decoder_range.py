@@ -1,0 +1,29 @@
+"""The decoder at the ends of what it was made for: positions behind the given number."""
+import pytest
+
+from tests import gpu_util as gu
+from tests.test_gpu_decoder import HEADS, KV, VOCAB, _i32, model  # noqa: F401  (fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def _decoder(model, positions, tokens=200, width=10):  # noqa: F811
+    from paper_2405_03594_gb300.decoder import Decoder
+
+    layers, _, head, _, embed = model
+    return Decoder(layers, embed, head, HEADS, KV, 40, 3, tokens, width, page_size=16, positions=positions)
+
+
+def test_positions_as_far_as_the_tables_reach(model):  # noqa: F811
+    """A request may grow to its table's pages whatever `positions` says: its later tokens turn by their own
+    angles, not by position 0's."""
+    import torch
+
+    from paper_2405_03594_gb300 import sp
+
+    a, b = _decoder(model, 160), _decoder(model, 32)
+    g = torch.Generator().manual_seed(5)
+    for new in ([90, 20, 1], [70, 1, 33], [0, 1, 1]):
+        ids = torch.randint(0, VOCAB, (sum(new),), generator=g).to(gu.dev())
+        assert torch.equal(a.step(ids, _i32(new), max(new)), b.step(ids, _i32(new), max(new)))
+        sp.check()
