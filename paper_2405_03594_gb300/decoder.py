@@ -75,6 +75,8 @@ class Decoder:
         t = ids.shape[0]
         b, h, qkv, gu, a, tmp, q, o = (self.batch, *(x[:t] for x in (self.h, self.qkv, self.gu, self.a, self.t, self.q, self.o)))
         b.plan(new, advance=True)
+        if t == 0:  # requests that end or wait
+            return self.logits[:0]
         torch.index_select(self.embed, 0, ids, out=h)
         H, G, D = self.heads, self.kv_heads, self.dim
         x = qkv.view(t, H + 2 * G, D)

@@ -1,4 +1,4 @@
-"""The decoder at the ends of what it was made for: positions behind the given number."""
+"""The decoder at the ends of what it was made for: positions behind the given number, and steps without tokens."""
 import pytest
 
 from tests import gpu_util as gu
@@ -27,3 +27,19 @@ def test_positions_as_far_as_the_tables_reach(model):  # noqa: F811
         ids = torch.randint(0, VOCAB, (sum(new),), generator=g).to(gu.dev())
         assert torch.equal(a.step(ids, _i32(new), max(new)), b.step(ids, _i32(new), max(new)))
         sp.check()
+
+
+def test_a_step_without_tokens(model):  # noqa: F811
+    import torch
+
+    from paper_2405_03594_gb300 import sp
+
+    dec = _decoder(model, 160)
+    ids = torch.arange(30, device=gu.dev())
+    dec.step(ids, _i32([20, 10, 0]), 20)
+    logits = dec.step(ids[:0], _i32([-1, 0, 0]), 1)  # the first request ends
+    sp.check()
+    assert logits.shape == (0, VOCAB) and dec.batch.cached.tolist() == [0, 10, 0] and dec.batch.free_count.item() == 39
+    nxt, logp, entropy, top_logp, top_ids = dec.greedy(ids[:0], _i32([0, 0, 0]), 1, top=3)
+    assert nxt.shape == logp.shape == entropy.shape == (0,) and top_logp.shape == top_ids.shape == (0, 3)
+    sp.check()
