@@ -69,9 +69,11 @@ class Decoder:
     def step(self, ids: torch.Tensor, new: torch.Tensor, max_new: int, record=None) -> torch.Tensor:
         """Runs the step's tokens ids (int64 [t], request by request) of requests that each get new[b] of them
         (int32 [requests]; < 0: the request has ended and gives its pages back); max_new: at least the most
-        of one request.  Returns the logits [t, V].  A step that does not fit (batch.status) writes no cache.
+        of one request.  Returns the logits [t, V].  Ids that the step cannot take are refused before anything changes.  A step that does not fit (batch.status) writes no cache.
         If `record` is a list, (h before the layer, queries, attention's output) of each layer and h before the
         head are appended to it (copies)."""
+        if ids.dim() != 1 or ids.shape[0] > self.h.shape[0] or ids.dtype not in (torch.int64, torch.int32) or ids.device != self.h.device:
+            raise ValueError(f"ids: up to {self.h.shape[0]} int64 on {self.h.device} wanted, got {ids.dtype} {list(ids.shape)} on {ids.device}")
         t = ids.shape[0]
         b, h, qkv, gu, a, tmp, q, o = (self.batch, *(x[:t] for x in (self.h, self.qkv, self.gu, self.a, self.t, self.q, self.o)))
         b.plan(new, advance=True)

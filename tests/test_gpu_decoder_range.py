@@ -1,4 +1,5 @@
-"""The decoder at the ends of what it was made for: positions behind the given number, and steps without tokens."""
+"""The decoder at the ends of what it was made for: positions behind the given number, steps without tokens, and
+more tokens than its buffers hold."""
 import pytest
 
 from tests import gpu_util as gu
@@ -43,3 +44,17 @@ def test_a_step_without_tokens(model):  # noqa: F811
     nxt, logp, entropy, top_logp, top_ids = dec.greedy(ids[:0], _i32([0, 0, 0]), 1, top=3)
     assert nxt.shape == logp.shape == entropy.shape == (0,) and top_logp.shape == top_ids.shape == (0, 3)
     sp.check()
+
+
+@pytest.mark.parametrize("what", ["count", "dtype", "dim", "device"])
+def test_ids_that_the_step_cannot_take_change_nothing(model, what):  # noqa: F811
+    import torch
+
+    dec = _decoder(model, 160, tokens=20)
+    ids = torch.zeros(12, dtype=torch.int64, device=gu.dev())
+    dec.step(ids, _i32([12, 0, 0]), 12)
+    bad = {"count": ids.repeat(2), "dtype": ids.float(), "dim": ids[None], "device": ids.cpu()}[what]
+    held = dec.h.data_ptr(), dec.h.shape
+    with pytest.raises(ValueError):
+        dec.step(bad, _i32([0, 3, 0]), 3)
+    assert dec.batch.cached.tolist() == [12, 0, 0] and (dec.h.data_ptr(), dec.h.shape) == held
