@@ -147,9 +147,10 @@ typedef struct sp_attend_args {
 
 /* out = softmax(scale * q . K^T) . V over the values that the cache stands for.  Of a request with
  * L tokens, a of them new, new token i sees the first L - a + i + 1.  Scores, softmax statistics and
- * sums are fp32; queries enter the products exactly (but for entries below 2^-27 of the largest of
- * their own row, which round to 2^-35 of it), weights rounded to fp16, cached values exactly (of a
- * request with more than 32 query rows per key head: rounded to fp16); one rounding to bf16 at
+ * sums are fp32; queries enter the products exactly (but for entries below 2^-24 of the largest of
+ * their own row, which round to 2^-32 of it), weights rounded to fp16, cached keys and values exactly (of
+ * a request with more than 32 query rows per key head: values rounded to fp16, and of a key s * n + m the
+ * part s * (n - 8), with m + 8 * s exact, so that keys far from zero keep their codes); one rounding to bf16 at
  * the end.  A page that the table does not hold is not read and is recorded for sp_check; what the
  * tokens that would see its keys get is unspecified.  Of a request whose tables do not belong to its
  * lengths nothing is written, and it is recorded.  Rows of `out` behind cu_q[requests] are not written.

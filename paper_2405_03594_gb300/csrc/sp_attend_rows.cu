@@ -13,7 +13,7 @@
 //   warps 8-11       codes to fp16 operands in shared memory: rows of keys and of values in
 //                    128-byte-swizzled panels of 64 channels
 //   warps 12, 13     issue a tile's products each
-//   warp 14          copies of the codes, and the next item
+//   warp 14          copies of the codes, the keys' sixteen more columns, and the next item
 //
 // Measured, 32 heads of 128, two prompts of up to 2048 tokens behind a prefix (4 x 24e9 operations): 136 us,
 // 0.71 PFLOP/s, 0.37 of the measured bf16 rate.  A step of both tiles takes 4300 clocks, 2048 of them the
@@ -26,8 +26,12 @@
 // fewer pairs than SMs, each one's steps of keys are cut into shares, whose sums join_rows_kernel adds up
 // in order: twelve tokens behind 8000, 8 key heads, 130 us uncut, 42 in shares.
 //
-// Numbers.  s n + m is rounded once to fp16 (the cache holds |x| <= 2^15); the queries, bf16, enter
-// exactly, each row scaled by a power of two.  The running maximum of a row moves only when
+// Numbers.  A value s n + m is rounded once to fp16 (the cache holds |x| <= 2^15), which is an eighth of what the
+// output's rounding to bf16 takes from it.  A key is not: its offset may be a thousand times its step s, and rounded with
+// it would lose the codes (keys 1000 from zero, s = 0.3: outputs off by a tenth).  So the operand is s (n - 8), and
+// sixteen more columns hold m and 8 s, which are fp16 numbers, against the queries' sum as three fp16 numbers: 33 bits
+// of it (2 % of the time: 148.9 us against 146).  The queries, bf16, enter exactly but for entries below 2^-24 of their row's
+// largest, each row scaled by a power of two that keeps its sum below 2^15.  The running maximum of a row moves only when
 // a weight would pass 2^8, so the sums in tensor memory are rarely touched by the rows' threads.  The channels
 // stand in the order in which a word's codes come out, i and i + 4 as a pair, in the queries
 // too; the output is put in order on its way out.
@@ -58,8 +62,10 @@ struct Smem {
   static constexpr uint32_t kQ = D / 64 * kPanel;              // a tile of queries, a step's keys
   static constexpr uint32_t kV = kQ;                           // a step's values
   static constexpr uint32_t kRaw = kTile * (D / 2 + 4);        // a step's codes and parameters of one of them
-  static constexpr uint32_t kBytes = 2 * kQ + kStages * (kQ + kV) + 2 * kRaw;
+  static constexpr uint32_t kMore = kTile * 32;                // sixteen more columns of either
+  static constexpr uint32_t kBytes = 2 * kQ + kStages * (kQ + kV) + 2 * kRaw + (2 + kStages) * kMore;
   static constexpr size_t kTotal = 1024 + kBytes;              // + base alignment
+  static_assert(kTotal + 1024 <= 227 * 1024, "beside them a kilobyte at most of barriers, items and the like");
 };
 
 __device__ __forceinline__ void mma_ss(uint32_t d_taddr, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
@@ -102,6 +108,19 @@ __device__ __forceinline__ uint64_t smem_desc_rows_along_k(uint32_t saddr) {
   d |= (uint64_t)1u << 46;
   d |= (uint64_t)2u << 61;
   return d;
+}
+
+// The sixteen more columns: two blocks of 8 rows by 16 bytes side by side, 128 bytes each (no swizzle).
+__device__ __forceinline__ uint64_t smem_desc_more(uint32_t saddr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr >> 4) & 0x3FFFu);
+  d |= (uint64_t)(128u >> 4) << 16;
+  d |= (uint64_t)(256u >> 4) << 32;
+  d |= (uint64_t)1u << 46;
+  return d;
+}
+__device__ __forceinline__ uint4* more_columns(uint8_t* base, int row) {  // the first eight of a row
+  return reinterpret_cast<uint4*>(base + (row >> 3) * 256 + (row & 7) * 16);
 }
 
 __device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
@@ -288,7 +307,8 @@ __device__ __forceinline__ bool end_item(const Wait& wait) {
 
 // ------------------------------------------------------------------ rows: scores to weights, and the output
 template <int D>
-__device__ __forceinline__ void rows_role(const AttendParams& p, Shared& sh, uint8_t* s_q, uint32_t tmem, bool gone) {
+__device__ __forceinline__ void rows_role(const AttendParams& p, Shared& sh, uint8_t* s_q, uint8_t* s_more, uint32_t tmem,
+                                          bool gone) {
   using L = Smem<D>;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int i = warp >> 2;  // tile
@@ -319,12 +339,13 @@ __device__ __forceinline__ void rows_role(const AttendParams& p, Shared& sh, uin
 #pragma unroll
         for (int j = 0; j < 4; ++j) big = max(big, max(x[j] & 0x7fffu, (x[j] >> 16) & 0x7fffu));
       }
-      // 2^(141 - e): the row's largest entry, of biased exponent e, comes to 2^14 ... 2^15
+      // 2^(134 - e): the row's largest entry, of biased exponent e, comes to 2^7 ... 2^8, their sum below 2^15
       const uint32_t e = max(15u, min(254u, big >> 7));
-      const float f = copysignf(__uint_as_float((268u - e) << 23), p.scale_log2);
+      const float f = copysignf(__uint_as_float((261u - e) << 23), p.scale_log2);
       // (not 0, which would make NaN of what the row does not see)
-      cr = fmaxf(__uint_as_float((e - 14u) << 23) * fabsf(p.scale_log2), 1e-37f);
+      cr = fmaxf(__uint_as_float((e - 7u) << 23) * fabsf(p.scale_log2), 1e-37f);
       uint8_t* dst = s_q + i * L::kQ + r * 128;
+      float sum[2] = {0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < D / 8; ++c) {
         const uint32_t x[4] = {u[c].x, u[c].y, u[c].z, u[c].w};
@@ -333,10 +354,15 @@ __device__ __forceinline__ void rows_role(const AttendParams& p, Shared& sh, uin
         for (int j = 0; j < 4; ++j) {
           y[2 * j] = __uint_as_float(x[j] << 16) * f;
           y[2 * j + 1] = __uint_as_float(x[j] & 0xffff0000u) * f;
+          sum[0] += y[2 * j], sum[1] += y[2 * j + 1];
         }
         *reinterpret_cast<uint4*>(dst + (c >> 3) * kPanel + (((c & 7) ^ (r & 7)) << 4)) =
             make_uint4(pack_f16(y[0], y[4]), pack_f16(y[1], y[5]), pack_f16(y[2], y[6]), pack_f16(y[3], y[7]));
       }
+      // the sum in three fp16 numbers, against the keys' minima and scales
+      const float h0 = __half2float(__float2half_rn(sum[0] + sum[1])), r1 = sum[0] + sum[1] - h0;
+      const float h1 = __half2float(__float2half_rn(r1)), h2 = r1 - h1;
+      *more_columns(s_more + i * L::kMore, r) = make_uint4(pack_f16(h0, h1), pack_f16(h2, h0), pack_f16(h1, h2), 0);
     }
     fence_proxy_async_smem();
     __syncwarp();
@@ -484,7 +510,7 @@ __device__ __forceinline__ void rows_role(const AttendParams& p, Shared& sh, uin
 // A step's codes and parameters come to shared memory as they are, by one bulk copy per page, as soon as
 // the step before is expanded.  Where a wait has expired, none is on its way any more when the CTA ends.
 template <int D, class Fetch>
-__device__ __forceinline__ void copy_role(const AttendParams& p, Shared& sh, uint8_t* s_raw, Fetch fetch, bool gone) {
+__device__ __forceinline__ void copy_role(const AttendParams& p, Shared& sh, uint8_t* s_raw, uint8_t* s_more, Fetch fetch, bool gone) {
   using L = Smem<D>;
   const int lane = threadIdx.x & 31;
   const int shift = p.cache.shift, heads = p.cache.heads, pages = kTile >> shift;
@@ -534,6 +560,27 @@ __device__ __forceinline__ void copy_role(const AttendParams& p, Shared& sh, uin
                    src + (which ? kv4_value_params<D>(shift) : kv4_key_params<D>(shift)), 4 << shift, full);
         }
         ++sent;
+      }
+      // the keys' sixteen more columns: their minima and eight times their scales, three times each
+      const int st = (steps + j) % kStages;
+      wait(&sh.bar.raw_full[0], (steps + j) & 1);
+      wait(&sh.bar.k_empty[st], (((steps + j) / kStages) & 1) ^ 1);
+      if (wait.dead) break;
+      const uint32_t* raw_par = reinterpret_cast<const uint32_t*>(s_raw + kTile * (D / 2));
+      const int left = it.len - (it.j0 + j) * kTile;
+#pragma unroll
+      for (int x = 0; x < kTile; x += 32) {
+        const int key = x + lane;
+        uint32_t y = raw_par[key];
+        if (key >= left || !(ok >> (key >> shift) & 1)) y = 0;  // what no token was written to may hold anything
+        const uint32_t s8 = hfma2(y, 0x48004800u, 0);
+        *more_columns(s_more + (2 + st) * L::kMore, key) =
+            make_uint4(__byte_perm(y, y, 0x3232), __byte_perm(y, s8, 0x5432), __byte_perm(s8, s8, 0x1010), 0);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(&sh.bar.k_full[st]);
       }
     }
     steps += n;
@@ -605,7 +652,9 @@ __device__ __forceinline__ void fill_role(const AttendParams& p, Shared& sh, uin
 #pragma unroll
           for (int x = 0; x < KP; ++x) {
             const int key = x * (kTile / KP) + f / KP;
-            const uint32_t s = __byte_perm(par[x], par[x], 0x1010), m = __byte_perm(par[x], par[x], 0x3232);
+            const uint32_t s = __byte_perm(par[x], par[x], 0x1010);
+            // (of keys s (n - 8): the rest, which may be far larger than it, is in the other columns)
+            const uint32_t m = which ? __byte_perm(par[x], par[x], 0x3232) : hfma2(s, 0xc800c800u, 0);
             const uint32_t w[4] = {turn ? c4[x].z : c4[x].x, turn ? c4[x].w : c4[x].y, turn ? c4[x].x : c4[x].z,
                                    turn ? c4[x].y : c4[x].w};
             uint8_t* row = dst + key * 128 + (piece >> 1) * kPanel;
@@ -643,12 +692,13 @@ __device__ __forceinline__ void fill_role(const AttendParams& p, Shared& sh, uin
 // ------------------------------------------------------------------ the products of tile i
 template <int D>
 __device__ __forceinline__ void product_role(const AttendParams& p, Shared& sh, uint8_t* s_q, uint8_t* s_k, uint8_t* s_v,
-                                             uint32_t tmem, int i, bool gone) {
+                                             uint8_t* s_more, uint32_t tmem, int i, bool gone) {
   using L = Smem<D>;
   Wait wait{p, gone};
   // operand descriptors; a piece further on is a larger start address, in units of 16 bytes
   const uint64_t d_q = smem_desc_sw128(smem_u32(s_q + i * L::kQ)), d_k = smem_desc_sw128(smem_u32(s_k)),
-                 d_v = smem_desc_rows_along_k(smem_u32(s_v));
+                 d_v = smem_desc_rows_along_k(smem_u32(s_v)), d_qm = smem_desc_more(smem_u32(s_more + i * L::kMore)),
+                 d_km = smem_desc_more(smem_u32(s_more + 2 * L::kMore));
   const uint32_t t_s = tmem + i * kTile, t_o = tmem + 2 * kTile + i * D;
   uint32_t steps = 0, done = 0, turns = 0;
   for (uint32_t round = 0;; ++round) {
@@ -683,6 +733,7 @@ __device__ __forceinline__ void product_role(const AttendParams& p, Shared& sh, 
             const uint64_t off = ((kk >> 2) * kPanel + (kk & 3) * 32) >> 4;
             mma_ss(t_s, d_q + off, b + off, idesc_f16(kTile, kTile), kk > 0 ? 1u : 0u);
           }
+          mma_ss(t_s, d_qm, d_km + (uint64_t)(ks * (L::kMore >> 4)), idesc_f16(kTile, kTile), 1u);
           mma_commit(&sh.bar.s_full[i]);
         }
         mbar_arrive(&sh.bar.turn[1 - i]);
@@ -714,13 +765,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
   uint8_t* s_v = smem + 2 * L::kQ;
   uint8_t* s_k = s_v + kStages * L::kV;
   uint8_t* s_raw = s_k + kStages * L::kQ;
+  uint8_t* s_more = s_raw + 2 * L::kRaw;  // of two tiles of queries, of the stages' keys
   __shared__ Shared sh;
   const int tid = threadIdx.x, warp = tid >> 5;
   if (tid == 0) {
     mbar_init(&sh.bar.q_full, kRowThreads / 32);
     mbar_init(&sh.bar.probe, 1);
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(&sh.bar.k_full[i], 1);
+      mbar_init(&sh.bar.k_full[i], 2);
       mbar_init(&sh.bar.v_full[i], 1);
       mbar_init(&sh.bar.k_empty[i], 2);
       mbar_init(&sh.bar.v_empty[i], 2);
@@ -736,6 +788,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
     }
     fence_barrier_init();
   }
+  for (uint32_t i = tid; i < (2 + kStages) * L::kMore / 16; i += kThreads)
+    reinterpret_cast<uint4*>(s_more)[i] = make_uint4(0, 0, 0, 0);  // (the second eight columns stay so)
+  fence_proxy_async_smem();
   pdl_wait();
   // the next share of the list, by a warp
   auto fetch = [&](Item& it) {
@@ -786,15 +841,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
   // registers: 128 a thread at launch, (176 + 176 + 88 + 72) / 4 from here on
   if (warp < kRowThreads / 32) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
-    rows_role<D>(p, sh, s_q, tmem, gone);
+    rows_role<D>(p, sh, s_q, s_more, tmem, gone);
   } else if (warp < kRowThreads / 32 + kFillWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     fill_role<D>(p, sh, s_k, s_v, s_raw, gone);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     const int x = warp - kRowThreads / 32 - kFillWarps;
-    if (x < 2) product_role<D>(p, sh, s_q, s_k, s_v, tmem, x, gone);
-    if (x == 2) copy_role<D>(p, sh, s_raw, fetch, gone);
+    if (x < 2) product_role<D>(p, sh, s_q, s_k, s_v, s_more, tmem, x, gone);
+    if (x == 2) copy_role<D>(p, sh, s_raw, s_more, fetch, gone);
   }
   tc_fence_before();
   __syncthreads();

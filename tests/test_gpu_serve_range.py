@@ -99,3 +99,44 @@ def test_zeros_of_either_sign(sp, serve, dtype, v):  # noqa: F811
     sp.check()
     assert ti.tolist() == [[1, 4, 7, 10, 0, 2, 3, 5], list(range(8)), list(range(8))]
     assert torch.equal(tl, lp[:, None].expand(3, 8))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads,kv,new,lens", [(8, 2, [1, 2], [700, 90]), (8, 2, [40, 3, 90], [700, 90, 100]),
+                                               (4, 4, [300], [900])])
+@pytest.mark.parametrize("offset", [50.0, 1000.0, -20000.0])
+def test_keys_far_from_zero(sp, serve, heads, kv, new, lens, d, offset):  # noqa: F811
+    """Keys whose entries all lie `offset` from zero, a thousand times their spread and more: their codes still
+    tell them apart, with few and with many query rows.  The offset is multiplied by the queries' sum in fp32: with
+    |sum(q)| < 100 and scale <= 1/8, a part of a score up to 2.5e5, rounded to 2^-24 of itself in each of three operations: at
+    most 5e-2 of a weight, and 8e-3 of the norm for such errors at random (a third of them, over equal weights' halves)."""
+    g = np.random.default_rng(int(abs(offset)))
+    f = Filled(serve, g, lens, new, heads, kv, d, 32)
+    n, s, m = f.rows[0]
+    m += np.float16(offset)
+    f.load()
+    y = f.cache.attend(f.qd, f.batch, max(new))
+    sp.check()
+    w, got = f.want(), gu.bf16_from_dev(y)
+    assert np.abs(got - w).max() <= (5e-2 if abs(offset) > 1e4 else 8e-3) * f.vmax() + 2.0 ** -8 * np.abs(w).max()
+    assert np.linalg.norm(got - w) <= (8e-3 if abs(offset) > 1e4 else 2.5e-3) * np.linalg.norm(w)
+
+
+@pytest.mark.parametrize("case", ["large_offset", "peaked", "equal", "scale"])
+def test_distributions_of_many_rows(sp, serve, case):  # noqa: F811
+    """The distributions that tests/test_gpu_serve.py has for few rows, for the kernel of many."""
+    g = np.random.default_rng(12)
+    f = Filled(serve, g, [700, 90], [70, 33], 8, 2, 128, 64, offset=50.0 if case == "large_offset" else 0.0)
+    scale = {"peaked": 4.0, "scale": -0.02}.get(case)
+    if case == "equal":
+        for n, s, m in f.rows[:1]:
+            n[:], s[~np.isnan(s)], m[~np.isnan(m)] = 3, 0.5, -1
+        f.load()
+    y = f.cache.attend(f.qd, f.batch, 70, scale=scale)
+    sp.check()
+    if case == "peaked":  # scores four times sqrt(128) as large: so are their errors
+        w = f.want(scale)
+        assert np.abs(gu.bf16_from_dev(y) - w).max() <= 0.2 * f.vmax()
+        assert np.linalg.norm(gu.bf16_from_dev(y) - w) <= 1e-2 * np.linalg.norm(w)
+    else:
+        _near(y, f.want(scale), f.vmax())
