@@ -49,12 +49,11 @@ _read = _lib["sp_kv4_read"]  # (the cache by its address)
 _read.argtypes, _read.restype = [ctypes.c_void_p, *_lib.sp_kv4_read.argtypes[1:]], ctypes.c_int
 
 
-def _gpu_of(x: torch.Tensor, name: str) -> int:
-    """The index of the current GPU, on which x has to be: a call's launches go there, and every other
-    address that it hands over has to be that GPU's."""
-    dev = x.get_device()
+def _on_current(dev: int, x: torch.Tensor, name: str) -> int:
+    """dev, where x is, which has to be the current GPU: a call's launches go there, and every other address
+    that it hands over has to be that GPU's."""
     if dev < 0 or dev != _current_device():
-        raise ValueError(f"{name}: a tensor on the current GPU wanted, got one on {x.device}")
+        raise ValueError(f"{name} on {x.device}, the current GPU wanted")
     return dev
 
 
@@ -96,7 +95,8 @@ def _output(out: torch.Tensor | None, t: int, h: int, dim: int, like: torch.Tens
 
 
 def _run_rope(q, k, v, positions, cos_sin, q_weight, k_weight, eps, pairs, q_out, k_out, cache, slots, stream):
-    dim, dev = q.shape[-1], _gpu_of(q, "q")
+    dim = q.shape[-1]
+    dev = _on_current(q.get_device(), q, "q") if cache is None else _on_current(cache._gpu, cache._data, "the cache's buffer")
     t, h, q_stride = _heads(q, None, dim, dev, "q")
     tk, kv, k_stride = _heads(k, None, dim, dev, "k")
     if tk != t:
@@ -106,8 +106,6 @@ def _run_rope(q, k, v, positions, cos_sin, q_weight, k_weight, eps, pairs, q_out
     rows, rot = cos_sin.shape
     pos = _index(positions, t, _I32, dev, "positions")
     qw, kw = _weight(q_weight, dim, dev, "q_weight"), _weight(k_weight, dim, dev, "k_weight")
-    if cache is not None:
-        cache._check_gpu(dev)
     q_out = _output(q_out, t, h, dim, q, dev, "q_out")
     if cache is None:
         k_out = _output(k_out, t, kv, dim, k, dev, "k_out")
@@ -160,10 +158,6 @@ class KvCache:
         """The buffer; its address is the cache's for life."""
         return self._data
 
-    def _check_gpu(self, dev: int) -> None:
-        if self._gpu != dev:
-            raise ValueError(f"the cache's buffer is on {self.data.device}, GPU {dev} wanted")
-
     def append(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor,
                cos_sin: torch.Tensor, q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None,
                eps: float = 1e-5, pairs: bool = False, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
@@ -173,9 +167,8 @@ class KvCache:
 
     def read(self, slots: torch.Tensor, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
         """The cached keys and values at `slots` (int64 [n]) as bf16 [n, kv_heads, head_dim]."""
-        dev = _gpu_of(slots, "slots")
+        dev = _on_current(self._gpu, self._data, "the cache's buffer")
         at = _index(slots, 0, _I64, dev, "slots")
-        self._check_gpu(dev)
         n = slots.shape[0]
         device = slots.device
         shape = (n, self.kv_heads, self.head_dim)
@@ -189,9 +182,8 @@ class KvCache:
         the tables of `batch`; max_new: at least the most new tokens of a request; scale: 1 / sqrt(D)
         by default.  Rows behind the step's last token keep what `out` held.  workspace: workspace_size()
         bytes (uint8) to use instead of the stream's own, zero at first as include/sp_serve.h says."""
-        dim, dev = self.head_dim, _gpu_of(q, "q")
+        dim, dev = self.head_dim, _on_current(self._gpu, self._data, "the cache's buffer")
         t, h, q_stride = _heads(q, batch.heads, dim, dev, "q")
-        self._check_gpu(dev)
         if batch._gpu != dev:
             raise ValueError(f"the batch's tables are not on GPU {dev}")
         device = q.device
@@ -281,10 +273,8 @@ class Batch:
         (cached, free_count); otherwise they stay, and the step can be planned again.  allocate=False:
         `table` already holds every page of the step.  A step that does not fit leaves everything as it
         is, has no tokens, and says why in `status` (PLAN_*)."""
-        dev = _gpu_of(new, "new")
+        dev = _on_current(self._gpu, self.cached, "the batch's tables")
         at = _index(new, self.requests, _I32, dev, "new")
-        if self._gpu != dev:
-            raise ValueError(f"the batch's tables are not on GPU {dev}")
         own = self.__dict__  # (these tensors have been checked)
         own["lens"] = self.cached if advance else self._lens
         own["next_count"] = self.free_count if advance else self._next_count
@@ -307,7 +297,7 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, str
     if (dtype is not _BF16 and dtype is not _F32) or logits.dim() != 2 or logits.stride(1) != 1:
         raise ValueError("logits: bf16 or float32 [T, V] with unit column stride on a GPU wanted")
     t, v = logits.shape
-    dev = _gpu_of(logits, "logits")
+    dev = _on_current(logits.get_device(), logits, "logits")
     ids = _index(tokens, t, _I64, dev, "tokens")
     device = logits.device
     logp, entropy = torch.empty(t, dtype=_F32, device=device), torch.empty(t, dtype=_F32, device=device)
