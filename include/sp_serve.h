@@ -75,7 +75,7 @@ typedef struct sp_kv_plan_args {
 
 enum {
   SP_PLAN_PAGES = 1,  /* the stack has too few pages       */
-  SP_PLAN_WIDTH = 2,  /* a request outgrows its table row  */
+  SP_PLAN_WIDTH = 2,  /* a request outgrows its table row, or all of them what sp_kv4_attend counts */
   SP_PLAN_TOKENS = 4, /* more than max_tokens new tokens   */
   SP_PLAN_INPUT = 8   /* cached or free_count out of range */
 };

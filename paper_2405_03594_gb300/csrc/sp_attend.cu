@@ -30,7 +30,7 @@
 // Measured (GPU time of one call among others).  One request behind 4096 tokens, 32 key heads of 128 (17.9 MB):
 // 12.5 us.  64 requests of 100 to 16384 tokens, 8 key heads of 128 with four query heads each (207 MB): 49.9 us,
 // 4.2 TB/s over the whole, 5.7 while it streams.  16 requests of 500 to 6000 tokens with five new ones, 8 key
-// heads of 64 with four each (21 MB): 23.9 us.  Bound by what lies around the stream: 4 us to the first
+// heads of 64 with four each (21 MB): 22.9 us.  Bound by what lies around the stream: 4 us to the first
 // copies (lengths, table and pages are loads that wait for one another), 2 to 3 to the first unit, 4 to 8 for the
 // last units and the joins; with many rows a unit (24: 840 instructions, some 80 % of the issue slots) the products
 // and softmax take longer than its bytes.

@@ -15,16 +15,19 @@
 //   warps 12, 13     issue a tile's products each
 //   warp 14          copies of the codes, the keys' sixteen more columns, and the next item
 //
-// Measured, 32 heads of 128, two prompts of up to 2048 tokens behind a prefix (4 x 24e9 operations): 136 us,
-// 0.71 PFLOP/s, 0.37 of the measured bf16 rate.  A step of both tiles takes 4300 clocks, 2048 of them the
-// tensor core's.  The expansion of the codes bounds it, 1500 clocks for the keys and as many for the
-// values (without its arithmetic: 125 us before the items were sorted, where the whole took 142); then the chain of a
-// tile: scores read and weights made 1400 clocks, their products and the next scores 1300, four barriers.  The
-// exponentials are not felt (left out: no change).
+// Measured, 32 heads of 128, two prompts of up to 2048 tokens behind a prefix (4 x 24e9 operations): 149 us,
+// 0.65 PFLOP/s, 0.34 of the measured bf16 rate; the tensor pipe is active 35 % of the time.  No part alone bounds
+// it.  With the products cut to an eighth it takes 148 us, without exponentials no less than with them, without the
+// expansion of the codes and its stores 139, without the expansion and with an eighth of the products 130 (the same
+// kernel with that part left out, wrong results).  What is left is a tile's chain in each step, whose links wait
+// for one another: scores out of tensor memory, maximum, weights and their stores, the products of the weights, the
+// next scores, four barriers.
 //
 // Split.  Pairs of tiles are taken from one list, those that see more first.  Where there are
 // fewer pairs than SMs, each one's steps of keys are cut into shares, whose sums join_rows_kernel adds up
-// in order: twelve tokens behind 8000, 8 key heads, 130 us uncut, 42 in shares.
+// in order: a chunk of 64 tokens behind 8000, 8 key heads of 128 with four query heads each, 142 us uncut, 46 in
+// shares.  The host, which sees no lengths, cuts by the most pairs that so many rows of q can make, so beside many
+// single tokens, or in a padded q, such a chunk stays uncut.
 //
 // Numbers.  A value s n + m is rounded once to fp16 (the cache holds |x| <= 2^15), which is an eighth of what the
 // output's rounding to bf16 takes from it.  A key is not: its offset may be a thousand times its step s, and rounded with

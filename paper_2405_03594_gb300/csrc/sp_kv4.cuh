@@ -17,9 +17,8 @@ constexpr int kUnitKeys = 32;       // keys of one step of attend_kernel
 constexpr int kRowTile = 32;        // query rows (token, head of the group) of its widest form
 // Query rows of a request from which attend_rows_kernel takes it: every request that attend_kernel would
 // need a second row tile for.  32 heads over 8 of 128, 12 new tokens (48 rows), attend_kernel / attend_rows_kernel,
-// us: 16 requests behind 1000 tokens 46 / 28, behind 8000 218 / 141; one request 23 / 24 and 37 / 42 (130
-// without its steps cut into shares), alone with its 12 tokens 12 / 15: what one request loses is less than what
-// several gain, and the host, which launches both kernels or one, sees no lengths.
+// us: 16 requests behind 1000 tokens 44 / 30, behind 8000 209 / 149; one request 21 / 26 and 36 / 43, alone with its 12
+// tokens 11 / 16: what one request loses is less than what several gain, and the host, which launches both kernels or one, sees no lengths.
 constexpr int kManyRows = 33;
 constexpr int kPairRows = 256;      // query rows of one of its items
 constexpr int kSetupUnits = 2;      // what a segment costs beside its units, in units (64 requests of 100 to

@@ -9,7 +9,7 @@ compressed layers runs beside them.
     logp, entropy, top, ids = token_logprobs(logits, tokens, 5)
 
 Argument marshalling only: the work is in libsp's kernels, and PyTorch holds the buffers.  No call
-synchronises, so a step can be captured in a CUDA graph.  Indices in device tensors (tables, slots,
+synchronises, so a step can be captured in a CUDA graph.  Every tensor of a call has to be on the current GPU.  Indices in device tensors (tables, slots,
 positions, token ids) are checked by the kernels, which leave bad ones out; sp.check() then raises.
 """
 from __future__ import annotations
