@@ -156,7 +156,8 @@ typedef struct sp_attend_args {
  * lengths nothing is written, and it is recorded.  Rows of `out` behind cu_q[requests] are not written.
  * `workspace` as for sp_linear: sp_kv4_attend_workspace_size bytes, its first
  * SP_WORKSPACE_ZERO_BYTES zero before its first use, calls that share it ordered on one stream; one
- * buffer can serve sp_linear and this call.  Results are bitwise repeatable. */
+ * buffer can serve sp_linear and this call.  Results are bitwise repeatable.  Of a launch that sp_check
+ * reports as SP_ERR_TIMEOUT no result is to be used; the workspace is ready for the next call. */
 sp_status sp_kv4_attend(const sp_attend_args* args, void* workspace_dev, size_t workspace_bytes, void* stream);
 
 /* Failure-path test (nothing calls it in normal use).  sp_kv4_attend, with warp `warp` of CTA `cta` of its
