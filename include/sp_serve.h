@@ -1,7 +1,7 @@
 /*
  * sp_serve.h -- what a program that serves a compressed model runs beside its linear layers
  * (libsp, GB300 / sm_103a): the tables of a paged cache, per-head norms with the position rotation,
- * attention over a cache held in 4 bits, and the probabilities of the answer.
+ * attention over a cache held in 4 bits, the probabilities of the answer, and the verification of drafted tokens.
  *
  * The paper's deployment measurements (Sec. 3.4) serve whole models; it defines none of these
  * operators, so their definitions stand here.  The conventions of sp.h hold: device pointers of
@@ -90,6 +90,30 @@ enum {
  * next_count), a negative size or a page size that is no power of two; requests == 0 or
  * max_tokens == 0 is allowed.  One launch, or two where max_tokens is large. */
 sp_status sp_kv_plan(const sp_kv_plan_args* args, void* stream);
+
+/* Tokens taken back, such as drafts that were refused. */
+typedef struct sp_kv_retract_args {
+  const int32_t* cached;     /* [requests] tokens that each request holds                            */
+  const int32_t* drop;       /* [requests] how many of its last ones go: 0..cached                   */
+  const int32_t* table;      /* [requests][width] pages of each request, in order                    */
+  int32_t* free_pages;       /* [pages] stack of unused pages, or NULL: pages stay where they are    */
+  const int32_t* free_count; /* [1] its height before                                                */
+  int32_t* next_count;       /* [1] its height after (may be free_count)                             */
+  int32_t* lens;             /* [requests] tokens after (may be `cached`)                            */
+  int32_t* status;           /* [1] 0, or SP_PLAN_INPUT                                              */
+  int64_t pages;
+  int32_t requests, width;
+  int32_t page_size;
+  int32_t reserved;          /* 0 */
+} sp_kv_retract_args;
+
+/* Shorten requests.  The pages that a request no longer needs go on the stack, in the order of the requests and
+ * of each one's table; the table's entries stay as they are, behind the length.  Lengths out of range, a
+ * drop below 0 or above the length, or more pages than there are: nothing changes, and *status says
+ * SP_PLAN_INPUT.  Unless it writes over its own inputs, the call can be repeated.  SP_ERR_INVALID_ARG for a
+ * null pointer (but free_pages, with free_count, next_count and table), a negative size, a page size that is no power
+ * of two.  requests == 0 is allowed.  One launch. */
+sp_status sp_kv_retract(const sp_kv_retract_args* args, void* stream);
 
 /* Per-head norms of queries and keys with the position rotation, in one pass; keys and values go to
  * the cache's slots in 4 bits, or the keys to a tensor. */
@@ -189,6 +213,53 @@ typedef enum sp_logits_dtype { SP_LOGITS_BF16 = 0, SP_LOGITS_F32 = 1 } sp_logits
 sp_status sp_token_logprobs(const void* logits, sp_logits_dtype dtype, int64_t stride, int64_t tokens, int64_t vocab,
                             const int64_t* ids, int32_t top, float* logp_out, float* entropy_out, float* top_logp_out,
                             int64_t* top_ids_out, void* stream);
+
+/* Probabilities from logits (of `dtype`, [tokens][vocab], `stride` elements from row to row), fp32
+ * [tokens][vocab], out_stride elements from row to row.  Row t with temperature T (temperature[t], or one_temperature
+ * where `temperature` is NULL), in fp32 with each operation rounded on its own:
+ *     z = (x - max x) * (1 / max(T, 2^-120))
+ *     p = exp(z) / sum(exp(z)) over the entries with z >= ln(min_p), 0 elsewhere
+ * that is, entries of less than min_p times the best one's probability are left out (0: none).  T <= 0: 1 for the
+ * first of the largest entries and 0 elsewhere.  A row with a NaN, with nothing but -inf, or (T > 0) with +inf, is NaN, and so
+ * is one whose temperature is a NaN; T = +inf makes all entries above -inf alike.  min_p in 0..1, vocab below 2^31
+ * (SP_ERR_UNSUPPORTED); out rows that start at multiples of 16 bytes are written fastest.  Results are
+ * bitwise repeatable.  One launch.  tokens == 0 returns SP_OK. */
+sp_status sp_token_probs(const void* logits, sp_logits_dtype dtype, int64_t stride, int64_t tokens, int64_t vocab,
+                         const float* temperature, float one_temperature, double min_p, float* out,
+                         int64_t out_stride, void* stream);
+
+/* Verification of drafted tokens: which of them the target's distribution keeps, and the token behind them. */
+typedef struct sp_verify_args {
+  const void* probs;        /* [rows][vocab] of `dtype`, the target's probabilities, `stride` from row to row */
+  const void* draft_probs;  /* [rows][vocab] of draft_dtype, draft_stride from row to row: row j is what    */
+                            /* ids[j + 1] was drawn from; rows without a draft are not read.  NULL: drafts  */
+                            /* are certain (1 for the token itself)                                         */
+  int64_t stride, draft_stride;
+  int64_t rows, vocab;
+  const int64_t* ids;       /* [rows] the step's tokens: row j of probs is the distribution behind ids[j]   */
+  const int32_t* cu_q;      /* [requests + 1] first row of each request, as sp_kv_plan writes it             */
+  const int32_t* drafts;    /* [requests] how many of its last tokens are drafts: fewer than its rows        */
+  const float* accept;      /* [rows] in [0, 1): accept[j] decides on ids[j + 1]                             */
+  const float* sample;      /* [requests] in [0, 1): draws the token behind                                  */
+  int32_t* accepted;        /* [requests] drafts kept                                                        */
+  int32_t* rejected;        /* [requests] drafts - accepted (sp_kv_retract's drop)                           */
+  int64_t* next;            /* [requests] the token behind the last one kept; -1 for a request without rows  */
+  int32_t requests;
+  int32_t dtype, draft_dtype; /* sp_logits_dtype */
+  int32_t reserved;         /* 0 */
+} sp_verify_args;
+
+/* Of a request with n drafts, whose rows end at r: draft i, the token d behind row r - 1 - n + i, is kept while
+ *     accept[row] * q[row][d] < p[row][d]     (fp32, the product rounded once)
+ * The token behind the a that are kept is drawn from row r - 1 - n + a: with weights p where a = n, and
+ * max(p - q, 0) where draft a was refused (fp32), or p if that leaves nothing.  Every weight w
+ * counts as floor(2^40 * min(max(w, 0), 1)), a NaN as 0, and the token is the first whose cumulated weight is above
+ * floor(total * u), u = sample in 24 bits (values outside [0, 1) go to its ends): whole numbers, so that the result
+ * depends on nothing but the inputs.  Probabilities need not add up to 1.  A row without any weight gives -1; a
+ * drafted token outside the vocabulary is refused; of a request whose rows and drafts do not belong together nothing is
+ * kept (0, 0, -1): all three are recorded for sp_check.  vocab up to 2^22 (SP_ERR_UNSUPPORTED).  One launch.
+ * requests == 0 returns SP_OK. */
+sp_status sp_verify_drafts(const sp_verify_args* args, void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,135 @@
+// sp_fp8.cu -- quantisation to e4m3 with a scale for each block of 128 (include/sp_fp8.h).
+//
+// A row's block is held by 16 lanes, eight entries each, a warp taking two neighbouring blocks; its largest
+// magnitude goes around by shuffles, so that x is read once and its codes and scale are written once.  A weight's
+// block of 128 x 128 is held by a CTA's registers in the same way.  Bound by the bytes.
+#include "sp_fp8.cuh"
+
+namespace sp {
+namespace {
+
+constexpr int kQuThreads = 256;
+
+// Eight entries of a row from column c on; 0 behind the end.
+template <bool WIDE>
+__device__ __forceinline__ uint4 load8(const uint16_t* row, int64_t c, int64_t k) {
+  if (WIDE && c + 8 <= k) return __ldg(reinterpret_cast<const uint4*>(row + c));
+  uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (c + i < k) w[i >> 1] |= (uint32_t)__ldg(row + c + i) << (16 * (i & 1));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ uint32_t largest_of(const uint4& u) {  // fp32 bits
+  uint32_t m = 0;
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m = max(m, max((w[i] << 16) & 0x7fffffffu, w[i] & 0x7fff0000u));
+  return m;
+}
+__device__ __forceinline__ uint2 codes_of(const uint4& u, float inv) {
+  auto lo = [](uint32_t w) { return __uint_as_float(w << 16); };
+  auto hi = [](uint32_t w) { return __uint_as_float(w & 0xffff0000u); };
+  return make_uint2(fp8_codes4(lo(u.x), hi(u.x), lo(u.y), hi(u.y), inv),
+                    fp8_codes4(lo(u.z), hi(u.z), lo(u.w), hi(u.w), inv));
+}
+
+template <bool WIDE>
+__global__ void __launch_bounds__(kQuThreads) quantize_rows_kernel(const uint16_t* __restrict__ x, int64_t x_stride,
+                                                                   int64_t m, int64_t k, uint8_t* __restrict__ codes,
+                                                                   int64_t stride, float* __restrict__ scale,
+                                                                   int64_t scale_stride) {
+  const int lane = threadIdx.x & 31;
+  const int64_t pairs = (k + 2 * kFp8Block - 1) / (2 * kFp8Block), blocks = (k + kFp8Block - 1) / kFp8Block;
+  const int64_t at = blockIdx.x * (int64_t)(kQuThreads / 32) + (threadIdx.x >> 5);
+  pdl_wait();
+  if (at >= m * pairs) return;
+  const int64_t row = at / pairs, b = at % pairs * 2 + (lane >> 4), c = b * kFp8Block + 8 * (lane & 15);
+  const uint4 u = c < k ? load8<WIDE>(x + row * x_stride, c, k) : make_uint4(0, 0, 0, 0);
+  uint32_t a = largest_of(u);
+#pragma unroll
+  for (int d = 8; d > 0; d >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, d));
+  const float s = fp8_scale(a);
+  const uint2 q = codes_of(u, __frcp_rn(s));
+  if (c < stride && b < blocks) *reinterpret_cast<uint2*>(codes + row * stride + c) = q;
+  if ((lane & 15) == 0 && b < blocks) scale[b * scale_stride + row] = s;
+}
+
+template <bool WIDE>
+__global__ void __launch_bounds__(kQuThreads) quantize_blocks_kernel(const uint16_t* __restrict__ w, int64_t w_stride,
+                                                                     int64_t n, int64_t k, uint8_t* __restrict__ codes,
+                                                                     int64_t stride, float* __restrict__ scale) {
+  __shared__ uint32_t s_most[kQuThreads / 32];
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int64_t blocks = (k + kFp8Block - 1) / kFp8Block;
+  const int64_t rb = blockIdx.x / blocks, b = blockIdx.x % blocks, c = b * kFp8Block + 8 * (lane & 15);
+  pdl_wait();
+  uint4 u[8];
+  uint32_t a = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t r = rb * kFp8Block + 16 * i + (tid >> 4);
+    u[i] = r < n && c < k ? load8<WIDE>(w + r * w_stride, c, k) : make_uint4(0, 0, 0, 0);
+    a = max(a, largest_of(u[i]));
+  }
+  a = __reduce_max_sync(0xffffffffu, a);
+  if (lane == 0) s_most[tid >> 5] = a;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kQuThreads / 32; ++i) a = max(a, s_most[i]);
+  const float s = fp8_scale(a), inv = __frcp_rn(s);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t r = rb * kFp8Block + 16 * i + (tid >> 4);
+    if (r < n && c < stride) *reinterpret_cast<uint2*>(codes + r * stride + c) = codes_of(u[i], inv);
+  }
+  if (tid == 0) scale[rb * blocks + b] = s;
+}
+
+// 16-byte loads of eight entries
+bool wide_rows(const void* x, int64_t stride) { return al16(x) && stride % 8 == 0; }
+
+bool bad_sizes(const void* x, int64_t x_stride, int64_t rows, int64_t k, const void* codes, int64_t stride, const void* scale) {
+  return rows < 0 || k < 1 || x_stride < k || stride < k || (rows > 0 && (!x || !codes || !scale));
+}
+bool off_bounds(const void* x, const void* codes, const void* scale) {
+  return reinterpret_cast<uintptr_t>(x) % 2 || !al16(codes) || reinterpret_cast<uintptr_t>(scale) % 4;
+}
+constexpr int64_t kMost = (int64_t)1 << 30;
+
+}  // namespace
+
+sp_status launch_fp8_quantize_rows(const uint16_t* x, int64_t x_stride, int64_t m, int64_t k, uint8_t* codes,
+                                   int64_t stride, float* scale, int64_t scale_stride, cudaStream_t stream) {
+  const int64_t warps = m * ((k + 2 * kFp8Block - 1) / (2 * kFp8Block)), ctas = (warps * 32 + kQuThreads - 1) / kQuThreads;
+  if (ctas > INT32_MAX) return SP_ERR_UNSUPPORTED;
+  return launch_pdl(wide_rows(x, m > 1 ? x_stride : 0) ? quantize_rows_kernel<true> : quantize_rows_kernel<false>,
+                    dim3((unsigned)ctas), kQuThreads, 0, 1, stream, x, x_stride, m, k, codes, stride, scale, scale_stride);
+}
+
+}  // namespace sp
+
+using namespace sp;
+
+extern "C" sp_status sp_fp8_quantize_rows(const void* x, int64_t x_stride, int64_t m, int64_t k, void* codes,
+                                          int64_t stride, float* scale, int64_t scale_stride, void* stream) {
+  if (bad_sizes(x, x_stride, m, k, codes, stride, scale) || scale_stride < m) return SP_ERR_INVALID_ARG;
+  if (m > kMost || k > kMost || stride % 16 || scale_stride % 4) return SP_ERR_UNSUPPORTED;
+  if (off_bounds(x, codes, scale) || !al16(scale)) return SP_ERR_ALIGNMENT;
+  if (m == 0) return SP_OK;
+  return launch_fp8_quantize_rows(static_cast<const uint16_t*>(x), x_stride, m, k, static_cast<uint8_t*>(codes), stride,
+                                  scale, scale_stride, (cudaStream_t)stream);
+}
+
+extern "C" sp_status sp_fp8_quantize_blocks(const void* w, int64_t w_stride, int64_t n, int64_t k, void* codes,
+                                            int64_t stride, float* scale, void* stream) {
+  if (bad_sizes(w, w_stride, n, k, codes, stride, scale)) return SP_ERR_INVALID_ARG;
+  if (n > kMost || k > kMost || stride % 16) return SP_ERR_UNSUPPORTED;
+  if (off_bounds(w, codes, scale)) return SP_ERR_ALIGNMENT;
+  if (n == 0) return SP_OK;
+  const int64_t ctas = ((n + kFp8Block - 1) / kFp8Block) * ((k + kFp8Block - 1) / kFp8Block);
+  if (ctas > INT32_MAX) return SP_ERR_UNSUPPORTED;
+  return launch_pdl(wide_rows(w, n > 1 ? w_stride : 0) ? quantize_blocks_kernel<true> : quantize_blocks_kernel<false>,
+                    dim3((unsigned)ctas), kQuThreads, 0, 1, (cudaStream_t)stream, static_cast<const uint16_t*>(w), w_stride, n,
+                    k, static_cast<uint8_t*>(codes), stride, scale);
+}

@@ -7,6 +7,9 @@ compressed layers runs beside them.
     q = cache.append(q, k, v, batch.positions, batch.slots, cos_sin)     norms, rotation, 4-bit write
     o = cache.attend(q, batch, max_new)                attention over the cache
     logp, entropy, top, ids = token_logprobs(logits, tokens, 5)
+    p = token_probs(logits, temperature)               and with drafted tokens among the step's
+    accepted, rejected, nxt = verify_drafts(p, ids, batch.cu_q, drafts, accept, sample, draft_probs)
+    batch.retract(rejected, advance=True)
 
 Argument marshalling only: the work is in libsp's kernels, and PyTorch holds the buffers.  No call
 synchronises, so a step can be captured in a CUDA graph.  Every tensor of a call has to be on the current GPU.  Indices in device tensors (tables, slots,
@@ -21,7 +24,7 @@ import struct
 import torch
 
 from . import sp
-from .sp import SpAttendArgs, SpKv4, SpKvPlanArgs, SpRopeArgs, _check, _lib, _stream
+from .sp import SpAttendArgs, SpKv4, SpKvPlanArgs, SpKvRetractArgs, SpRopeArgs, SpVerifyArgs, _check, _lib, _stream
 
 PLAN_PAGES, PLAN_WIDTH, PLAN_TOKENS, PLAN_INPUT = 1, 2, 4, 8  # SP_PLAN_*
 
@@ -43,6 +46,8 @@ def _packed(name: str, args):
 
 
 _pack_plan, _plan = _packed("sp_kv_plan", SpKvPlanArgs)
+_pack_retract, _retract = _packed("sp_kv_retract", SpKvRetractArgs)
+_pack_verify, _verify = _packed("sp_verify_drafts", SpVerifyArgs)
 _pack_rope, _rope = _packed("sp_qk_norm_rope", SpRopeArgs)
 _pack_attend, _attend = _packed("sp_kv4_attend", SpAttendArgs)
 _read = _lib["sp_kv4_read"]  # (the cache by its address)
@@ -288,6 +293,24 @@ class Batch:
         return self
 
 
+    def retract(self, drop: torch.Tensor, advance: bool = False, allocate: bool = True, stream=None) -> "Batch":
+        """sp_kv_retract: request b loses its last drop[b] tokens (int32 [requests], 0 to what it holds), such as
+        drafts that were refused, and the pages that held nothing else go back on the stack.  advance and allocate
+        as for plan(): the lengths and the stack's height after it are `lens` and `next_count`, or replace those
+        before it.  Slots, positions and shares of a step planned before stay as they are."""
+        dev = _on_current(self._gpu, self.cached, "the batch's tables")
+        at = _index(drop, self.requests, _I32, dev, "drop")
+        own = self.__dict__
+        own["lens"] = self.cached if advance else self._lens
+        own["next_count"] = self.free_count if advance else self._next_count
+        _check(_retract(_pack_retract(self.cached.data_ptr(), at, self.table.data_ptr(),
+                                      self.free.data_ptr() if allocate else 0, self.free_count.data_ptr(),
+                                      self.next_count.data_ptr(), self.lens.data_ptr(), self.status.data_ptr(),
+                                      self.pages, self.requests, self.width, self.page_size, 0),
+                        _stream(stream, dev)), "sp_kv_retract")
+        return self
+
+
 def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, stream=None):
     """sp_token_logprobs: of each row of logits [T, V] (bf16 or float32, rows of unit stride), the log
     probability of tokens[t] (int64; a negative one asks for nothing and gets 0) and the entropy, both
@@ -309,3 +332,70 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, str
                                   ti.data_ptr() if top else None, _stream(stream, dev)),
            "sp_token_logprobs")
     return (logp, entropy, tl, ti) if top else (logp, entropy)
+
+
+def _matrix(x: torch.Tensor, dev: int, name: str) -> int:
+    """Checks rows [T, V] of probabilities or logits and returns their type's number (SP_LOGITS_*)."""
+    dtype = x.dtype
+    if (dtype is not _BF16 and dtype is not _F32) or x.dim() != 2 or x.stride(1) != 1 or x.get_device() != dev:
+        raise ValueError(f"{name}: bf16 or float32 [T, V] with unit column stride on GPU {dev} wanted")
+    return 0 if dtype is _BF16 else 1
+
+
+def token_probs(logits: torch.Tensor, temperature=1.0, min_p: float = 0.0, out: torch.Tensor | None = None,
+                stream=None) -> torch.Tensor:
+    """sp_token_probs: probabilities, float32 [T, V], of the rows of logits [T, V] (bf16 or float32, rows of unit
+    stride).  temperature: a number, or one for each row (float32 [T]); 0 or less takes the best entry.
+    min_p: entries of less than min_p times the best one's probability are left out.  Without `out` the
+    rows start at multiples of 16 bytes: where V is no multiple of 4 the result is a view of wider rows."""
+    dev = _on_current(logits.get_device(), logits, "logits")
+    kind = _matrix(logits, dev, "logits")
+    t, v = logits.shape
+    if v < 1:
+        raise ValueError("logits: a vocabulary of one entry or more wanted")
+    if isinstance(temperature, torch.Tensor):
+        per_row, one = _index(temperature, t, _F32, dev, "temperature"), 1.0
+    else:
+        per_row, one = 0, float(temperature)
+    if out is None:
+        wide = (v + 3) // 4 * 4
+        out = torch.empty((t, wide), dtype=_F32, device=logits.device)
+        if wide != v:
+            out = out[:, :v]
+    elif _matrix(out, dev, "out") != 1 or out.shape != logits.shape:
+        raise ValueError(f"out: float32 {[t, v]} wanted")
+    _check(_lib.sp_token_probs(logits.data_ptr(), kind, logits.stride(0) if t > 1 else v, t, v, per_row, one, min_p,
+                               out.data_ptr(), out.stride(0) if t > 1 else max(out.stride(0), v), _stream(stream, dev)),
+           "sp_token_probs")
+    return out
+
+
+def verify_drafts(probs: torch.Tensor, ids: torch.Tensor, cu_q: torch.Tensor, drafts: torch.Tensor, accept: torch.Tensor,
+                  sample: torch.Tensor, draft_probs: torch.Tensor | None = None, stream=None):
+    """sp_verify_drafts: of each request's drafted tokens, the last drafts[b] (int32 [B]) of its step's tokens
+    ids[cu_q[b]:cu_q[b + 1]] (int64 [T]; int32 [B + 1]), which ones the target's probabilities (bf16 or float32 [T, V],
+    row j behind token j) keep, and the token behind those.  accept (float32 [T]): accept[j] decides on token j + 1;
+    sample (float32 [B]) draws the token behind; both uniform in [0, 1).  draft_probs [T, V]: row j is what token j + 1
+    was drawn from; None: drafts are certain.  With drafts of 0 it samples.  Returns
+    (accepted int32 [B], rejected int32 [B], next token int64 [B], -1 for a request without tokens)."""
+    dev = _on_current(probs.get_device(), probs, "probs")
+    kind = _matrix(probs, dev, "probs")
+    t, v = probs.shape
+    b = cu_q.shape[0] - 1 if cu_q.dim() == 1 else -1
+    if b < 0:
+        raise ValueError("cu_q: int32 [requests + 1] wanted")
+    draft_kind = draft_stride = draft = 0
+    if draft_probs is not None:
+        draft_kind = _matrix(draft_probs, dev, "draft_probs")
+        if draft_probs.shape != probs.shape:
+            raise ValueError(f"draft_probs: {[t, v]} wanted")
+        draft, draft_stride = draft_probs.data_ptr(), draft_probs.stride(0) if t > 1 else v
+    where = (_index(ids, t, _I64, dev, "ids"), _index(cu_q, b + 1, _I32, dev, "cu_q"), _index(drafts, b, _I32, dev, "drafts"),
+             _index(accept, t, _F32, dev, "accept"), _index(sample, b, _F32, dev, "sample"))
+    device = probs.device
+    accepted, rejected = torch.empty((2, b), dtype=_I32, device=device)
+    nxt = torch.empty(b, dtype=_I64, device=device)
+    _check(_verify(_pack_verify(probs.data_ptr(), draft, probs.stride(0) if t > 1 else v, draft_stride, t, v, *where,
+                                accepted.data_ptr(), rejected.data_ptr(), nxt.data_ptr(), b, kind, draft_kind, 0),
+                   _stream(stream, dev)), "sp_verify_drafts")
+    return accepted, rejected, nxt

@@ -25,14 +25,16 @@ STATUS = {
     5: "SP_ERR_OUT_OF_MEMORY", 6: "SP_ERR_TIMEOUT", 7: "SP_ERR_BAD_HANDLE", 8: "SP_ERR_WORKSPACE",
 }
 SP_ERR_UNSUPPORTED = 2
-# every function declared in include/sp.h, include/sp_stack.h and include/sp_serve.h
+# every function declared in include/sp.h, include/sp_stack.h, include/sp_serve.h and include/sp_fp8.h
 EXPORTS = ["sp_compress", "sp_decompress", "sp_workspace_size", "sp_linear", "sp_linear_ex", "sp_launch_count",
            "sp_kernel_family",
            "sp_linear_noalloc", "sp_test_expired_wait", "sp_masked_update", "sp_linear_w8a8", "sp_w8a8_workspace_size",
            "sp_clone", "sp_free", "sp_info", "sp_copy_out", "sp_check", "sp_capture_id", "sp_status_string",
            "sp_copy_columns", "sp_residual_add", "sp_mul_halves", "sp_mul_pairs", "sp_chain_workspace_size",
            "sp_chain_run", "sp_linear_epi", "sp_kv4_bytes", "sp_kv_plan", "sp_qk_norm_rope", "sp_kv4_read",
-           "sp_kv4_attend", "sp_kv4_attend_workspace_size", "sp_test_expired_attend", "sp_token_logprobs"]
+           "sp_kv4_attend", "sp_kv4_attend_workspace_size", "sp_test_expired_attend", "sp_token_logprobs",
+           "sp_kv_retract", "sp_token_probs", "sp_verify_drafts", "sp_fp8_quantize_rows", "sp_fp8_quantize_blocks",
+           "sp_fp8_linear", "sp_fp8_workspace_size"]
 
 
 KERNELS = {0: "", 1: "linear_cc_kernel", 2: "linear_ccw_kernel", 3: "linear_tc_kernel", 4: "linear_mma_kernel",
@@ -75,6 +77,23 @@ class SpKvPlanArgs(ctypes.Structure):
                 ("width", ctypes.c_int32), ("page_size", ctypes.c_int32), ("group", ctypes.c_int32)]
 
 
+class SpKvRetractArgs(ctypes.Structure):
+    _fields_ = [("cached", ctypes.c_void_p), ("drop", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("free_pages", ctypes.c_void_p), ("free_count", ctypes.c_void_p), ("next_count", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("status", ctypes.c_void_p), ("pages", ctypes.c_int64),
+                ("requests", ctypes.c_int32), ("width", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class SpVerifyArgs(ctypes.Structure):
+    _fields_ = [("probs", ctypes.c_void_p), ("draft_probs", ctypes.c_void_p), ("stride", ctypes.c_int64),
+                ("draft_stride", ctypes.c_int64), ("rows", ctypes.c_int64), ("vocab", ctypes.c_int64),
+                ("ids", ctypes.c_void_p), ("cu_q", ctypes.c_void_p), ("drafts", ctypes.c_void_p),
+                ("accept", ctypes.c_void_p), ("sample", ctypes.c_void_p), ("accepted", ctypes.c_void_p),
+                ("rejected", ctypes.c_void_p), ("next", ctypes.c_void_p), ("requests", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("draft_dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 class SpRopeArgs(ctypes.Structure):
     _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
                 ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("q_out", ctypes.c_void_p),
@@ -92,6 +111,13 @@ class SpAttendArgs(ctypes.Structure):
                 ("tokens", ctypes.c_int64), ("requests", ctypes.c_int32), ("width", ctypes.c_int32),
                 ("heads", ctypes.c_int32), ("max_new", ctypes.c_int32), ("scale", ctypes.c_float),
                 ("reserved", ctypes.c_int32)]
+
+
+class SpFp8LinearArgs(ctypes.Structure):
+    _fields_ = [("w", ctypes.c_void_p), ("w_scale", ctypes.c_void_p), ("x", ctypes.c_void_p), ("xq", ctypes.c_void_p),
+                ("x_scale", ctypes.c_void_p), ("y", ctypes.c_void_p), ("w_stride", ctypes.c_int64),
+                ("x_stride", ctypes.c_int64), ("xq_stride", ctypes.c_int64), ("x_scale_stride", ctypes.c_int64),
+                ("y_stride", ctypes.c_int64), ("m", ctypes.c_int64), ("n", ctypes.c_int64), ("k", ctypes.c_int64)]
 
 
 ALLOC_FN = ctypes.CFUNCTYPE(ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p)
@@ -137,6 +163,13 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                                            ctypes.c_uint32, P]
     lib.sp_kv4_attend_workspace_size.argtypes = [ctypes.c_int32, ctypes.POINTER(SZ)]
     lib.sp_token_logprobs.argtypes = [P, ctypes.c_int, I64, I64, I64, P, ctypes.c_int32, P, P, P, P, P]
+    lib.sp_kv_retract.argtypes = [ctypes.POINTER(SpKvRetractArgs), P]
+    lib.sp_token_probs.argtypes = [P, ctypes.c_int, I64, I64, I64, P, ctypes.c_float, ctypes.c_double, P, I64, P]
+    lib.sp_verify_drafts.argtypes = [ctypes.POINTER(SpVerifyArgs), P]
+    lib.sp_fp8_quantize_rows.argtypes = [P, I64, I64, I64, P, I64, P, I64, P]
+    lib.sp_fp8_quantize_blocks.argtypes = [P, I64, I64, I64, P, I64, P, P]
+    lib.sp_fp8_linear.argtypes = [ctypes.POINTER(SpFp8LinearArgs), P, SZ, P]
+    lib.sp_fp8_workspace_size.argtypes = [I64, I64, I64, ctypes.POINTER(SZ)]
     lib.sp_status_string.argtypes = [ctypes.c_int]
     lib.sp_status_string.restype = ctypes.c_char_p
     for name in EXPORTS:
