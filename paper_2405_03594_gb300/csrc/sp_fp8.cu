@@ -10,30 +10,6 @@ namespace {
 
 constexpr int kQuThreads = 256;
 
-// Eight entries of a row from column c on; 0 behind the end.
-template <bool WIDE>
-__device__ __forceinline__ uint4 load8(const uint16_t* row, int64_t c, int64_t k) {
-  if (WIDE && c + 8 <= k) return __ldg(reinterpret_cast<const uint4*>(row + c));
-  uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (c + i < k) w[i >> 1] |= (uint32_t)__ldg(row + c + i) << (16 * (i & 1));
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ uint32_t largest_of(const uint4& u) {  // fp32 bits
-  uint32_t m = 0;
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) m = max(m, max((w[i] << 16) & 0x7fffffffu, w[i] & 0x7fff0000u));
-  return m;
-}
-__device__ __forceinline__ uint2 codes_of(const uint4& u, float inv) {
-  auto lo = [](uint32_t w) { return __uint_as_float(w << 16); };
-  auto hi = [](uint32_t w) { return __uint_as_float(w & 0xffff0000u); };
-  return make_uint2(fp8_codes4(lo(u.x), hi(u.x), lo(u.y), hi(u.y), inv),
-                    fp8_codes4(lo(u.z), hi(u.z), lo(u.w), hi(u.w), inv));
-}
-
 template <bool WIDE>
 __global__ void __launch_bounds__(kQuThreads) quantize_rows_kernel(const uint16_t* __restrict__ x, int64_t x_stride,
                                                                    int64_t m, int64_t k, uint8_t* __restrict__ codes,

@@ -24,7 +24,6 @@ __device__ __forceinline__ uint32_t fp8_codes4(float a, float b, float c, float 
   return (uint32_t)fp8_codes(__fmul_rn(a, inv), __fmul_rn(b, inv)) |
          ((uint32_t)fp8_codes(__fmul_rn(c, inv), __fmul_rn(d, inv)) << 16);
 }
-__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
 // Instruction descriptor, kind::f8f6f4: D fp32, A and B e4m3, both K-major, M = m, N = n.
 __host__ __device__ constexpr uint32_t idesc_e4m3(int m, int n) {
@@ -58,6 +57,37 @@ __device__ __forceinline__ void tmem_load16(uint32_t taddr, uint32_t (&v)[16]) {
         "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
       : "r"(taddr)
       : "memory");
+}
+
+// Eight entries of a row from column c on; 0 behind the end.
+template <bool WIDE>
+__device__ __forceinline__ uint4 load8(const uint16_t* row, int64_t c, int64_t k) {
+  if (WIDE && c + 8 <= k) return __ldg(reinterpret_cast<const uint4*>(row + c));
+  uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (c + i < k) w[i >> 1] |= (uint32_t)__ldg(row + c + i) << (16 * (i & 1));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ uint32_t largest_of(const uint4& u) {  // fp32 bits
+  uint32_t m = 0;
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m = max(m, max((w[i] << 16) & 0x7fffffffu, w[i] & 0x7fff0000u));
+  return m;
+}
+__device__ __forceinline__ uint2 codes_of(const uint4& u, float inv) {
+  auto lo = [](uint32_t w) { return __uint_as_float(w << 16); };
+  auto hi = [](uint32_t w) { return __uint_as_float(w & 0xffff0000u); };
+  return make_uint2(fp8_codes4(lo(u.x), hi(u.x), lo(u.y), hi(u.y), inv),
+                    fp8_codes4(lo(u.z), hi(u.z), lo(u.w), hi(u.w), inv));
+}
+
+// A tile asked into L2: a hint that may come before what it reads is ordered behind an earlier launch.
+__device__ __forceinline__ void tma_prefetch_2d(const CUtensorMap* map, int c0, int c1) {
+  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(c0),
+               "r"(c1)
+               : "memory");
 }
 
 // Bounded wait as mbar_wait, for waits that end within a microsecond: it looks at the barrier many times before it
@@ -99,6 +129,11 @@ __device__ __forceinline__ void fma2_behind(float& c0, float& c1, uint32_t a0, u
       : "f"(__uint_as_float(a0)), "f"(__uint_as_float(a1)), "f"(s));
 }
 
+// c += a * s for two numbers each, behind the wait.
+__device__ __forceinline__ void add_behind(uint64_t& c, uint32_t a0, uint32_t a1, uint64_t s) {
+  asm volatile("{\n\t.reg .b64 a;\n\tmov.b64 a, {%1, %2};\n\tfma.rn.f32x2 %0, a, %3, %0;\n\t}" : "+l"(c) : "r"(a0), "r"(a1), "l"(s));
+}
+
 // A warpgroup's registers per thread, of those that the block was launched with.
 template <int R>
 __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
@@ -111,6 +146,26 @@ struct Fp8Rows {
   const float* scale;
   int64_t stride, scale_stride;
 };
+
+// fp8_few_kernel: up to kFewTokens rows.
+constexpr int kFewTokens = 64;
+inline int few_box(int64_t m) { return m <= 16 ? 16 : m <= 32 ? 32 : 64; }  // rows of x in a tile, of map_x's box
+// CTAs that share a tile: as many as the SMs hold at once, `ctas` each, with two blocks each at least.
+inline int few_cluster(int64_t n, int64_t blocks, int ctas, int sms) {
+  const int64_t tiles = (n + kFp8Block - 1) / kFp8Block;
+  int c = 1;
+  while (c < 8 && tiles * c * 2 <= (int64_t)ctas * sms && blocks >= 4 * c) c *= 2;
+  return c;
+}
+// Whether that kernel quantises x itself, which every tile then does again (rows: NULL; no workspace): up to eight rows, and up
+// to ten pairs of rows of a block for each of its four warps. Measured, us, so / by a launch before: 8 x 4096 x 4096 (four) 7.5 / 9.0,
+// 8 x 22016 x 4096 (32) 27.0 / 19.7; 1 x 32000 x 4096 (eight) 22.3 / 24.6.
+inline bool few_fused(int64_t m, int64_t n, int64_t k, int sms) {
+  const int64_t blocks = (k + kFp8Block - 1) / kFp8Block, c = few_cluster(n, blocks, 2, sms);
+  return m <= 8 && (m + 1) / 2 * ((blocks + c - 1) / c) <= 40;
+}
+sp_status launch_fp8_few(const sp_fp8_linear_args& a, const Fp8Rows* rows, const CUtensorMap& map_w, const CUtensorMap& map_x,
+                         int sms, cudaStream_t stream);
 
 sp_status launch_fp8_quantize_rows(const uint16_t* x, int64_t x_stride, int64_t m, int64_t k, uint8_t* codes,
                                    int64_t stride, float* scale, int64_t scale_stride, cudaStream_t stream);

@@ -566,7 +566,7 @@ Workspace workspace_for(int64_t m, int64_t k, int sms) {
   w.codes = ws_counter_bytes(sms);
   w.scale = w.codes + round256((size_t)m * code_stride(k));
   w.part = w.scale + round256((size_t)((k + kFp8Block - 1) / kFp8Block) * scale_stride(m) * 4);
-  w.bytes = w.part + (size_t)2 * sms * tokens_of(m) * kTileN * 4;
+  w.bytes = w.part + (m <= kFewTokens ? 0 : (size_t)2 * sms * tokens_of(m) * kTileN * 4);
   return w;
 }
 
@@ -678,7 +678,7 @@ extern "C" sp_status sp_fp8_workspace_size(int64_t m, int64_t n, int64_t k, size
   if (m > kMost || n > kMost || k > kMost) return SP_ERR_UNSUPPORTED;
   const int sms = current_sms();
   if (sms == 0) return SP_ERR_CUDA;
-  *bytes = m == 0 ? 0 : workspace_for(m, k, sms).bytes;
+  *bytes = m == 0 || few_fused(m, n, k, sms) ? 0 : workspace_for(m, k, sms).bytes;
   return SP_OK;
 }
 
@@ -696,13 +696,18 @@ extern "C" sp_status sp_fp8_linear(const sp_fp8_linear_args* a, void* ws, size_t
   if (a->m == 0) return SP_OK;
   const int sms = current_sms();
   if (sms == 0) return SP_ERR_CUDA;
-  const Workspace w = workspace_for(a->m, a->k, sms);
-  if (!ws || ws_bytes < w.bytes) return SP_ERR_WORKSPACE;
-  uint8_t* base = static_cast<uint8_t*>(ws);
   cudaStream_t stream = (cudaStream_t)stream_;
   PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
   sp_status st = tensor_map_encoder(&encode);
   if (st != SP_OK) return st;
+  CUtensorMap map_w, map_x;
+  if (a->x && few_fused(a->m, a->n, a->k, sms)) {
+    st = code_map(&map_w, encode, a->w, a->n, a->k, a->w_stride, kTileN);
+    return st != SP_OK ? st : launch_fp8_few(*a, nullptr, map_w, map_w, sms, stream);
+  }
+  const Workspace w = workspace_for(a->m, a->k, sms);
+  if ((a->x || a->m > kFewTokens) && (!ws || ws_bytes < w.bytes)) return SP_ERR_WORKSPACE;
+  uint8_t* base = static_cast<uint8_t*>(ws);
 
   Fp8Rows rows = {static_cast<const uint8_t*>(a->xq), a->x_scale, a->xq_stride, a->x_scale_stride};
   if (a->x) {
@@ -711,8 +716,13 @@ extern "C" sp_status sp_fp8_linear(const sp_fp8_linear_args* a, void* ws, size_t
                                   reinterpret_cast<float*>(base + w.scale), rows.scale_stride, stream);
     if (st != SP_OK) return st;
   }
+  if (a->m <= kFewTokens) {
+    if ((st = code_map(&map_w, encode, a->w, a->n, a->k, a->w_stride, kTileN)) != SP_OK ||
+        (st = code_map(&map_x, encode, rows.codes, a->m, a->k, rows.stride, few_box(a->m))) != SP_OK)
+      return st;
+    return launch_fp8_few(*a, &rows, map_w, map_x, sms, stream);
+  }
   const int mt = tokens_of(a->m), nt = pair_columns(a->m, a->n, (a->k + kFp8Block - 1) / kFp8Block, sms);
-  CUtensorMap map_w, map_x;
   if ((st = code_map(&map_w, encode, a->w, a->n, a->k, a->w_stride, nt ? nt / 2 : kTileN)) != SP_OK ||
       (st = code_map(&map_x, encode, rows.codes, a->m, a->k, rows.stride, nt ? 128 : mt)) != SP_OK)
     return st;

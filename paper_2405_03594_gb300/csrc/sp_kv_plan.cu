@@ -336,12 +336,21 @@ __global__ void __launch_bounds__(kPlanThreads) retract_kernel(const __grid_cons
       }
       __syncthreads();
       const int at = s_base + s_warp[warp] + s - n;
-      // page j of those that b gives back, from table entry after + j
-      for (unsigned todo = __ballot_sync(0xffffffffu, n > 0); todo; todo &= todo - 1) {
+      // page j of those that b gives back, from table entry after + j: a few by the request's lane, all asked for before the
+      // first is written (by the warp, one request after the other: 1000 requests 13.1 us), many by the warp
+      const int64_t from = b * a.width + r.after, to = height + at;
+      int few[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < n && n <= 4) few[j] = a.table[from + j];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < n && n <= 4) a.free_pages[to + j] = few[j];
+      for (unsigned todo = __ballot_sync(0xffffffffu, n > 4); todo; todo &= todo - 1) {
         const int src = __ffs(todo) - 1;
-        const int m = __shfl_sync(0xffffffffu, n, src), to = __shfl_sync(0xffffffffu, at, src);
-        const int64_t from = __shfl_sync(0xffffffffu, b * a.width + r.after, src);
-        for (int j = lane; j < m; j += 32) a.free_pages[height + to + j] = a.table[from + j];
+        const int m = __shfl_sync(0xffffffffu, n, src);
+        const int64_t f = __shfl_sync(0xffffffffu, from, src), o = __shfl_sync(0xffffffffu, to, src);
+        for (int j = lane; j < m; j += 32) a.free_pages[o + j] = a.table[f + j];
       }
       __syncthreads();
       if (tid == kPlanThreads - 1) s_base = at + n;

@@ -17,6 +17,7 @@ namespace {
 constexpr int kVeThreads = 512;
 constexpr int kVeWarps = kVeThreads / 32;
 constexpr int kVeCluster = 8;
+constexpr int kBatch = 4;  // quads of a lane under way at a time
 constexpr int64_t kVeMostVocab = (int64_t)1 << 22;  // sums of weights of up to 2^40 stay below 2^63
 
 struct VerifyParams {
@@ -39,31 +40,50 @@ template <>
 __device__ __forceinline__ float number<uint16_t>(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 
 template <typename T>
-__device__ __forceinline__ void load4(const T* x, int64_t i, float (&v)[4]);
+__device__ __forceinline__ void load4(const T* x, int i, float (&v)[4]);
 template <>
-__device__ __forceinline__ void load4<float>(const float* x, int64_t i, float (&v)[4]) {
+__device__ __forceinline__ void load4<float>(const float* x, int i, float (&v)[4]) {
   const float4 u = __ldg(reinterpret_cast<const float4*>(x + i));
   v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w;
 }
 template <>
-__device__ __forceinline__ void load4<uint16_t>(const uint16_t* x, int64_t i, float (&v)[4]) {
+__device__ __forceinline__ void load4<uint16_t>(const uint16_t* x, int i, float (&v)[4]) {
   const uint2 u = __ldg(reinterpret_cast<const uint2*>(x + i));
   v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xffff0000u);
   v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xffff0000u);
 }
 
-__device__ __forceinline__ uint64_t weight(float w) {  // (a NaN counts as 0)
-  return (uint64_t)__float2ull_rz(__saturatef(w) * 1099511627776.f);
+// floor(2^40 w), w limited to [0, 1] (a NaN counts as 0), in two parts: floor(2^17 w) are the last bits of 64 + w rounded towards zero,
+// and what is left of w, below 2^-17, gives floor(2^40 rest) as those of 2^-17 + rest. A conversion to 64 bits takes the SM
+// several times as long: 256 rows of 32000 24.2 us so, 29.7 at first.
+struct Parts {
+  uint32_t hi, lo;  // sums of the parts' bits, with what belongs to 64 and 2^-17 (modulo 2^32)
+  __device__ __forceinline__ void add(float w) {
+    w = __saturatef(w);
+    const float t = __fadd_rz(w, 64.f);
+    hi += __float_as_uint(t);
+    lo += __float_as_uint(__fadd_rz(__fsub_rn(w, __fsub_rn(t, 64.f)), 0x1p-17f));
+  }
+  // the sum of n weights, n up to 511
+  __device__ __forceinline__ uint64_t sum(uint32_t n) const {
+    return ((uint64_t)(hi - n * 0x42800000u) << 23) + (lo - n * 0x37000000u);
+  }
+};
+__device__ __forceinline__ uint64_t weight(float w) {
+  Parts p = {0, 0};
+  p.add(w);
+  return p.sum(1);
 }
 
 template <typename T, typename Q>
 struct Rows {
   const T* p;
   const Q* q;    // or NULL
-  int64_t not_this, vocab;
+  int not_this, vocab;
   bool wide;     // both rows start at a vector's boundary
+  __device__ __forceinline__ float left(int i, float a, float b) const { return __fsub_rn(a, i == not_this ? 1.f : b); }
   // entries i .. i + 3 of the row (0 behind the end)
-  __device__ __forceinline__ void get(int64_t i, uint64_t (&w)[4]) const {
+  __device__ __forceinline__ void get(int i, uint64_t (&w)[4]) const {
     float a[4], b[4] = {0.f, 0.f, 0.f, 0.f};
     if (wide && i + 4 <= vocab) {
       load4(p, i, a);
@@ -71,15 +91,56 @@ struct Rows {
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        a[j] = i + j < vocab ? number(p[i + j]) : 0.f;
-        if (q && i + j < vocab) b[j] = number(q[i + j]);
+        a[j] = i + j < vocab ? number(__ldg(p + i + j)) : 0.f;
+        if (q && i + j < vocab) b[j] = number(__ldg(q + i + j));
       }
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (i + j == not_this) b[j] = 1.f;
-      w[j] = weight(__fsub_rn(a[j], b[j]));
+    for (int j = 0; j < 4; ++j) w[j] = weight(left(i + j, a[j], b[j]));
+  }
+  // this lane's share of the sum over the quads [q0, q1), which the warp takes together: by quads, or, where rows start
+  // anywhere, by single entries side by side (in quads of single loads four lanes' sectors would be asked for four times)
+  __device__ __forceinline__ uint64_t sum(int q0, int q1, int lane) const {
+    uint64_t s = 0;
+    if (wide) {
+      const int end = min(q1, vocab / 4);  // whole quads
+      for (int i = q0 + lane; i < end; i += 32 * kBatch) {
+        float a[kBatch][4], b[kBatch][4];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) a[k][j] = b[k][j] = 0.f;
+          if (i + 32 * k < end) {
+            load4(p, 4 * (i + 32 * k), a[k]);
+            if (q) load4(q, 4 * (i + 32 * k), b[k]);
+          }
+        }
+        Parts sums = {0, 0};  // (entries behind the end are 0)
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sums.add(left(4 * (i + 32 * k) + j, a[k][j], b[k][j]));
+        s += sums.sum(4 * kBatch);
+      }
+      for (int i = 4 * max(end, q0) + lane; i < min(4 * q1, vocab); i += 32)
+        s += weight(left(i, number(__ldg(p + i)), q ? number(__ldg(q + i)) : 0.f));
+    } else {
+      const int end = min(4 * q1, vocab);
+      constexpr int N = 4 * kBatch;
+      for (int i = 4 * q0 + lane; i < end; i += 32 * N) {
+        float a[N], b[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          a[k] = i + 32 * k < end ? number(__ldg(p + i + 32 * k)) : 0.f;
+          b[k] = q && i + 32 * k < end ? number(__ldg(q + i + 32 * k)) : 0.f;
+        }
+        Parts sums = {0, 0};
+#pragma unroll
+        for (int k = 0; k < N; ++k) sums.add(left(i + 32 * k, a[k], b[k]));
+        s += sums.sum(N);
+      }
     }
+    return s;
   }
 };
 
@@ -93,7 +154,9 @@ template <typename T, typename Q>
 __global__ void __launch_bounds__(kVeThreads, 2) verify_kernel(const __grid_constant__ VerifyParams p) {
   __shared__ uint64_t s_warp[kVeWarps];
   __shared__ uint64_t s_total[2];  // this CTA's, of either try
-  __shared__ int s_accepted, s_bad;
+  __shared__ int s_accepted, s_bad, s_owner;
+  __shared__ int s_range[2];
+  __shared__ uint64_t s_before;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = p.cluster > 1 ? (int)cluster_rank() : 0;
   const int64_t b = blockIdx.x / p.cluster;
@@ -139,28 +202,25 @@ __global__ void __launch_bounds__(kVeThreads, 2) verify_kernel(const __grid_cons
   __syncthreads();
   const int64_t a = s_accepted, row = first + a;
   const bool less = a < n;
+  int not_this = -1;  // (an index outside the vocabulary is none of its entries)
+  if (less && !draft) {
+    const int64_t id = p.ids[row + 1];
+    not_this = id >= 0 && id < p.vocab ? (int)id : -1;
+  }
   Rows<T, Q> rows;
   rows.p = probs + row * p.stride;
-  rows.vocab = p.vocab;
+  rows.vocab = (int)p.vocab;
   const uint32_t u24 = (uint32_t)(fminf(fmaxf(p.sample[b], 0.f), 0.99999994f) * 16777216.f);
-  const int64_t quads = (p.vocab + 3) / 4;
-  const int64_t parts = (int64_t)p.cluster * kVeWarps, part = (int64_t)rank * kVeWarps + warp;
-  const int64_t q0 = quads * part / parts, q1 = quads * (part + 1) / parts;
+  const int quads = (int)((p.vocab + 3) / 4), parts = p.cluster * kVeWarps, part = rank * kVeWarps + warp;
+  const int q0 = quads * part / parts, q1 = quads * (part + 1) / parts;  // (quads up to 2^20, parts up to 2^7)
 
   uint64_t total = 0, before = 0, own = 0;
   for (int attempt = 0; attempt < 2; ++attempt) {
     rows.q = less && draft && attempt == 0 ? draft + row * p.draft_stride : nullptr;
-    rows.not_this = less && !draft && attempt == 0 ? p.ids[row + 1] : -1;
+    rows.not_this = less && !draft && attempt == 0 ? not_this : -1;
     rows.wide = (reinterpret_cast<uintptr_t>(rows.p) % (4 * sizeof(T)) == 0) &&
                 (reinterpret_cast<uintptr_t>(rows.q) % (4 * sizeof(Q)) == 0);
-    uint64_t s = 0;
-#pragma unroll 4
-    for (int64_t i = q0 + lane; i < q1; i += 32) {
-      uint64_t w[4];
-      rows.get(4 * i, w);
-      s += w[0] + w[1] + w[2] + w[3];
-    }
-    own = warp_sum(s);
+    own = warp_sum(rows.sum(q0, q1, lane));
     if (lane == 0) s_warp[warp] = own;
     __syncthreads();
     before = total = 0;  // weights before the warp's stretch, and all
@@ -185,29 +245,53 @@ __global__ void __launch_bounds__(kVeThreads, 2) verify_kernel(const __grid_cons
   }
   // floor(total * u): total < 2^63, u in 24 bits
   const uint64_t t = __umul64hi(total, (uint64_t)u24 << 40);
-  if (total > 0 && t >= before && t - before < own) {  // one warp of the cluster
-    uint64_t sum = before;
-    for (int64_t i = q0; i < q1; i += 32) {
-      uint64_t w[4] = {0, 0, 0, 0};
-      if (i + lane < q1) rows.get(4 * (i + lane), w);
-      uint64_t incl = w[0] + w[1] + w[2] + w[3];
-      const uint64_t mine = incl;
+  // the warp in whose stretch it falls; all warps of its CTA then share that stretch, until a warp looks at it whole
+  if (tid == 0) s_owner = -1;
+  __syncthreads();
+  if (lane == 0 && total > 0 && t >= before && t - before < own) {
+    s_owner = warp;
+    s_range[0] = q0, s_range[1] = q1, s_before = before;
+  }
+  __syncthreads();
+  if (s_owner >= 0) {
+    int f0 = s_range[0], f1 = s_range[1];
+    uint64_t up = s_before;  // weights before f0: t is at least this
+    while (f1 - f0 > 32 * kBatch) {
+      const int n = f1 - f0;
+      const uint64_t part_sum = warp_sum(rows.sum(f0 + n * warp / kVeWarps, f0 + n * (warp + 1) / kVeWarps, lane));
+      if (lane == 0) s_warp[warp] = part_sum;
+      __syncthreads();
+      int w = 0;
+      while (w < kVeWarps - 1 && t - up >= s_warp[w]) up += s_warp[w++];
+      f1 = f0 + n * (w + 1) / kVeWarps;
+      f0 += n * w / kVeWarps;
+      __syncthreads();
+    }
+    if (warp == 0) {  // kBatch quads in a row of each lane
+      uint64_t w[kBatch][4], mine = 0;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int i = f0 + kBatch * lane + k;
+        w[k][0] = w[k][1] = w[k][2] = w[k][3] = 0;
+        if (i < f1) rows.get(4 * i, w[k]);
+        mine += w[k][0] + w[k][1] + w[k][2] + w[k][3];
+      }
+      uint64_t incl = mine;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
         const uint64_t v = __shfl_up_sync(0xffffffffu, incl, d);
         if (lane >= d) incl += v;
       }
-      const uint64_t end = sum + __shfl_sync(0xffffffffu, incl, 31);
-      if (t < end) {
-        uint64_t at = sum + incl - mine;
-        if (t >= at && t - at < mine) {
-          int j = 0;
-          while (j < 3 && t - at >= w[j]) at += w[j++];
-          p.next[b] = 4 * (i + lane) + j;
+      uint64_t at = up + incl - mine;
+      if (t >= at && t - at < mine) {
+        int found = -1;
+#pragma unroll
+        for (int k = 0; k < 4 * kBatch; ++k) {
+          if (found < 0 && t - at < w[k / 4][k % 4]) found = k;
+          at += w[k / 4][k % 4];
         }
-        break;
+        p.next[b] = 4 * (f0 + kBatch * lane) + found;
       }
-      sum = end;
     }
   }
   if (rank == 0 && tid == 0) {

@@ -146,10 +146,16 @@ class Fp8Matrix:
             out_stride = _rows(out, self.n, dev, "out")
             if out.shape[0] != m:
                 raise ValueError("x and out hold different numbers of rows")
+        ws = nbytes = 0
         if workspace is None:
-            workspace = sp.workspace_for(self.workspace_size(m), device, stream)
+            nbytes = self.workspace_size(m)
+            if nbytes:
+                workspace = sp.workspace_for(nbytes, device, stream)
+                ws, nbytes = workspace.data_ptr(), workspace.numel()
         elif workspace.dtype is not _U8 or not workspace.is_contiguous() or workspace.get_device() != dev:
             raise ValueError(f"workspace: contiguous bytes (uint8) on GPU {dev} wanted")
+        else:
+            ws, nbytes = workspace.data_ptr(), workspace.numel()
         _check(_linear(_pack_linear(*self._where, *rows, out.data_ptr(), self._stride, *strides, out_stride, m, self.n, self.k),
-                       workspace.data_ptr(), workspace.numel(), _stream(stream, dev)), "sp_fp8_linear")
+                       ws, nbytes, _stream(stream, dev)), "sp_fp8_linear")
         return out

@@ -393,7 +393,7 @@ def verify_drafts(probs: torch.Tensor, ids: torch.Tensor, cu_q: torch.Tensor, dr
     where = (_index(ids, t, _I64, dev, "ids"), _index(cu_q, b + 1, _I32, dev, "cu_q"), _index(drafts, b, _I32, dev, "drafts"),
              _index(accept, t, _F32, dev, "accept"), _index(sample, b, _F32, dev, "sample"))
     device = probs.device
-    accepted, rejected = torch.empty((2, b), dtype=_I32, device=device)
+    accepted, rejected = torch.empty(b, dtype=_I32, device=device), torch.empty(b, dtype=_I32, device=device)
     nxt = torch.empty(b, dtype=_I64, device=device)
     _check(_verify(_pack_verify(probs.data_ptr(), draft, probs.stride(0) if t > 1 else v, draft_stride, t, v, *where,
                                 accepted.data_ptr(), rejected.data_ptr(), nxt.data_ptr(), b, kind, draft_kind, 0),

@@ -242,9 +242,9 @@ def test_linear_past_32_bits(sp, fp8):
 # ------------------------------------------------------------------ streams, graphs, workspaces
 def test_linear_on_another_stream_and_with_a_given_workspace(sp, fp8):
     g = _gen(5)
-    x, w = _x(40, 700, g), fp8.Fp8Matrix.from_dense(_w(900, 700, g))
+    x, w = _x(90, 700, g), fp8.Fp8Matrix.from_dense(_w(900, 700, g))
     y = w.linear(x)
-    ws = torch.zeros(w.workspace_size(40), dtype=torch.uint8, device="cuda")
+    ws = torch.zeros(w.workspace_size(90), dtype=torch.uint8, device="cuda")
     assert torch.equal(w.linear(x, workspace=ws), y)
     with pytest.raises(sp.SpError, match="WORKSPACE"):
         w.linear(x, workspace=ws[:-256])
