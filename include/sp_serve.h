@@ -100,7 +100,7 @@ typedef struct sp_kv_retract_args {
   const int32_t* free_count; /* [1] its height before                                                */
   int32_t* next_count;       /* [1] its height after (may be free_count)                             */
   int32_t* lens;             /* [requests] tokens after (may be `cached`)                            */
-  int32_t* status;           /* [1] 0, or SP_PLAN_INPUT                                              */
+  int32_t* status;           /* [1] gets SP_PLAN_INPUT added where it cannot be done                 */
   int64_t pages;
   int32_t requests, width;
   int32_t page_size;
@@ -109,8 +109,8 @@ typedef struct sp_kv_retract_args {
 
 /* Shorten requests.  The pages that a request no longer needs go on the stack, in the order of the requests and
  * of each one's table; the table's entries stay as they are, behind the length.  Lengths out of range, a
- * drop below 0 or above the length, or more pages than there are: nothing changes, and *status says
- * SP_PLAN_INPUT.  Unless it writes over its own inputs, the call can be repeated.  SP_ERR_INVALID_ARG for a
+ * drop below 0 or above the length, or more pages than there are: nothing changes, and SP_PLAN_INPUT is added to
+ * *status, which else stays what the step's plan made it.  Unless it writes over its own inputs, the call can be repeated.  SP_ERR_INVALID_ARG for a
  * null pointer (but free_pages, with free_count, next_count and table), a negative size, a page size that is no power
  * of two.  requests == 0 is allowed.  One launch. */
 sp_status sp_kv_retract(const sp_kv_retract_args* args, void* stream);
@@ -222,8 +222,8 @@ sp_status sp_token_logprobs(const void* logits, sp_logits_dtype dtype, int64_t s
  * that is, entries of less than min_p times the best one's probability are left out (0: none).  T <= 0: 1 for the
  * first of the largest entries and 0 elsewhere.  A row with a NaN, with nothing but -inf, or (T > 0) with +inf, is NaN, and so
  * is one whose temperature is a NaN; T = +inf makes all entries above -inf alike.  min_p in 0..1, vocab below 2^31
- * (SP_ERR_UNSUPPORTED); out rows that start at multiples of 16 bytes are written fastest.  Results are
- * bitwise repeatable.  One launch.  tokens == 0 returns SP_OK. */
+ * (SP_ERR_UNSUPPORTED); rows of both that lie at the same distance from 16-byte boundaries, counted in entries, are written
+ * fastest, as contiguous rows do.  Results are bitwise repeatable.  One launch.  tokens == 0 returns SP_OK. */
 sp_status sp_token_probs(const void* logits, sp_logits_dtype dtype, int64_t stride, int64_t tokens, int64_t vocab,
                          const float* temperature, float one_temperature, double min_p, float* out,
                          int64_t out_stride, void* stream);
@@ -257,7 +257,7 @@ typedef struct sp_verify_args {
  * floor(total * u), u = sample in 24 bits (values outside [0, 1) go to its ends): whole numbers, so that the result
  * depends on nothing but the inputs.  Probabilities need not add up to 1.  A row without any weight gives -1; a
  * drafted token outside the vocabulary is refused; of a request whose rows and drafts do not belong together nothing is
- * kept (0, 0, -1): all three are recorded for sp_check.  vocab up to 2^22 (SP_ERR_UNSUPPORTED).  One launch.
+ * kept (0, 0, -1): all three are recorded for sp_check.  A request without rows gets (0, 0, -1).  vocab up to 2^22 (SP_ERR_UNSUPPORTED).  One launch.
  * requests == 0 returns SP_OK. */
 sp_status sp_verify_drafts(const sp_verify_args* args, void* stream);
 

@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(kPlanThreads) retract_kernel(const __grid_cons
   const int64_t top = height + (int64_t)s_pages;
   const bool bad = s_bad || (release && top > a.pages);
   if (tid == 0) {
-    *a.status = bad ? SP_PLAN_INPUT : 0;
+    if (bad) *a.status |= SP_PLAN_INPUT;  // (what the step's plan said stays)
     if (release) *a.next_count = (int32_t)(bad ? height : top);
   }
   if (release && !bad && top > height) {

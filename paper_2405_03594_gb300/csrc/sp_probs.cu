@@ -1,12 +1,12 @@
 // sp_probs.cu -- probabilities from logits, with a temperature for each row (include/sp_serve.h):
 //     z = (x - max x) / T,   p = exp(z) / sum(exp(z)) over the entries with z >= ln(min_p).
 //
-// A row is read once: its 16-byte pieces stay in the threads' registers (eight each) while the row's
+// A row is read once: its 16-byte pieces stay in the threads' registers while the row's
 // maximum and then its sum go around, within the CTA and, where rows are few or long, among the CTAs of a
 // cluster.  Pieces beyond what the registers hold are read again, from L2.  The bound is the
-// row's bytes in and out.  A piece is eight entries (bf16) or four (fp32) counted from the row's first, so
-// that the output's vectors are aligned whatever the logits' rows are; a piece that straddles a
-// 16-byte boundary of the logits is put together from two loads.
+// row's bytes in and out.  Pieces begin at the row's first 16-byte boundary; the entries before it and behind the last piece
+// go to rank 0's first threads.  Rows of logits and of probabilities that lie as densely have their boundaries at the same
+// entries, so that the pieces of both are aligned.
 #include <cmath>
 
 #include "sp_attend.cuh"
@@ -14,9 +14,7 @@
 namespace sp {
 namespace {
 
-constexpr int kPrThreads = 512;
-constexpr int kPrWarps = kPrThreads / 32;
-constexpr int kKept = 8;  // pieces that a thread keeps
+constexpr int kPrThreads = 256;  // (512 with as many pieces each: 320 rows of 131071 82.8 us, so 81.2)
 constexpr int kPrCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -28,7 +26,6 @@ struct ProbsParams {
   int64_t stride, vocab, out_stride;
   float* out;
   int32_t cluster;
-  int32_t out_aligned;  // rows of `out` start at multiples of 16 bytes
 };
 
 template <typename T>
@@ -36,25 +33,24 @@ struct Piece;
 template <>
 struct Piece<uint16_t> {
   static constexpr int N = 8;
-  static __device__ __forceinline__ float at(const uint4& u, int i) {
-    const uint32_t w = i < 2 ? u.x : i < 4 ? u.y : i < 6 ? u.z : u.w;
-    return __uint_as_float((i & 1) ? w & 0xffff0000u : w << 16);
-  }
-  static __device__ __forceinline__ float one(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+  static constexpr int kKept = 4;  // pieces that a thread keeps, as logits
   static constexpr uint32_t kNothing = 0xff80ff80u;  // -inf
-  static __device__ __forceinline__ void put(uint32_t (&w)[4], int i, uint16_t v) {
-    w[i >> 1] = (i & 1) ? (w[i >> 1] & 0xffffu) | ((uint32_t)v << 16) : (w[i >> 1] & 0xffff0000u) | v;
+  static __device__ __forceinline__ float one(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+  static __device__ __forceinline__ void get(const uint4& u, float (&v)[8]) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
   }
 };
 template <>
 struct Piece<float> {
   static constexpr int N = 4;
-  static __device__ __forceinline__ float at(const uint4& u, int i) {
-    return __uint_as_float(i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w);
-  }
-  static __device__ __forceinline__ float one(float v) { return v; }
+  static constexpr int kKept = 8;  // as logits, then as exponentials
   static constexpr uint32_t kNothing = 0xff800000u;
-  static __device__ __forceinline__ void put(uint32_t (&w)[4], int i, float v) { w[i] = __float_as_uint(v); }
+  static __device__ __forceinline__ float one(float v) { return v; }
+  static __device__ __forceinline__ void get(const uint4& u, float (&v)[4]) {
+    v[0] = __uint_as_float(u.x), v[1] = __uint_as_float(u.y), v[2] = __uint_as_float(u.z), v[3] = __uint_as_float(u.w);
+  }
 };
 
 __device__ __forceinline__ float max_nan(float a, float b) {
@@ -63,54 +59,26 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 
-// Piece c of the row x of `vocab` entries; entries behind the end are -inf.
-template <typename T>
-__device__ __forceinline__ uint4 load_piece(const T* x, int64_t vocab, int64_t c) {
-  constexpr int N = Piece<T>::N;
-  const T* at = x + c * N;
-  const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(at) & 15u);
-  const T* lo = reinterpret_cast<const T*>(reinterpret_cast<uintptr_t>(at) - off);
-  // every byte of what is loaded belongs to the row
-  if (off == 0 && (c + 1) * N <= vocab) return __ldcs(reinterpret_cast<const uint4*>(at));
-  if (off != 0 && lo >= x && lo + 2 * N <= x + vocab) {
-    const uint4 a = __ldg(reinterpret_cast<const uint4*>(lo)), b = __ldg(reinterpret_cast<const uint4*>(lo) + 1);
-    const uint32_t sh = (off & 3u) * 8u;
-    uint32_t w[5];
-    const uint32_t s = off >> 2;
-    w[0] = s == 0 ? a.x : s == 1 ? a.y : s == 2 ? a.z : a.w;
-    w[1] = s == 0 ? a.y : s == 1 ? a.z : s == 2 ? a.w : b.x;
-    w[2] = s == 0 ? a.z : s == 1 ? a.w : s == 2 ? b.x : b.y;
-    w[3] = s == 0 ? a.w : s == 1 ? b.x : s == 2 ? b.y : b.z;
-    w[4] = s == 0 ? b.x : s == 1 ? b.y : s == 2 ? b.z : b.w;
-    return make_uint4(__funnelshift_r(w[0], w[1], sh), __funnelshift_r(w[1], w[2], sh),
-                      __funnelshift_r(w[2], w[3], sh), __funnelshift_r(w[3], w[4], sh));
-  }
-  uint32_t w[4] = {Piece<T>::kNothing, Piece<T>::kNothing, Piece<T>::kNothing, Piece<T>::kNothing};
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (c * N + i < vocab) Piece<T>::put(w, i, at[i]);
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
 struct PrShared {
-  float warp[kPrWarps];
-  int64_t warp_at[kPrWarps];
+  float warp[kPrThreads / 32];
+  uint32_t warp_at[kPrThreads / 32];
   float cta[2];  // this CTA's maximum, its sum
-  int64_t cta_at;
+  uint32_t cta_at;
 };
 
 // The row's value of `v` by f, in every thread: warps, the CTA, the cluster's CTAs in order.
 template <typename F>
 __device__ __forceinline__ float over_row(float v, PrShared& sh, int which, int cluster, F f) {
+  constexpr int W = kPrThreads / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) v = f(v, __shfl_xor_sync(0xffffffffu, v, d));
   __syncthreads();  // (the array's last readers)
   if (lane == 0) sh.warp[warp] = v;
   __syncthreads();
-  v = sh.warp[lane & (kPrWarps - 1)];
+  v = sh.warp[lane & (W - 1)];
 #pragma unroll
-  for (int d = kPrWarps / 2; d > 0; d >>= 1) v = f(v, __shfl_xor_sync(0xffffffffu, v, d));
+  for (int d = W / 2; d > 0; d >>= 1) v = f(v, __shfl_xor_sync(0xffffffffu, v, d));
   if (cluster > 1) {
     if (threadIdx.x == 0) sh.cta[which] = v;
     cluster_sync_all();
@@ -122,8 +90,8 @@ __device__ __forceinline__ float over_row(float v, PrShared& sh, int which, int 
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kPrThreads, 2) probs_kernel(const __grid_constant__ ProbsParams p) {
-  constexpr int N = Piece<T>::N;
+__global__ void __launch_bounds__(kPrThreads, 4) probs_kernel(const __grid_constant__ ProbsParams p) {
+  constexpr int N = Piece<T>::N, kKept = Piece<T>::kKept, W = kPrThreads / 32;
   __shared__ PrShared sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = p.cluster > 1 ? (int)cluster_rank() : 0;
@@ -132,102 +100,153 @@ __global__ void __launch_bounds__(kPrThreads, 2) probs_kernel(const __grid_const
   const T* x = static_cast<const T*>(p.logits) + row * p.stride;
   float* out = p.out + row * p.out_stride;
   const float t = p.temperature ? p.temperature[row] : p.one_temperature;
-  const int64_t pieces = (p.vocab + N - 1) / N;
-  const int64_t c0 = pieces * rank / p.cluster, c1 = pieces * (rank + 1) / p.cluster;
+  // entries before the first 16-byte boundary, whole pieces, entries behind the last
+  const int vocab = (int)p.vocab;
+  const int head = min((int)(((16 - (reinterpret_cast<uintptr_t>(x) & 15u)) & 15u) / sizeof(T)), vocab);
+  const int pieces = (vocab - head) / N, tail = head + pieces * N;
+  const int c0 = (int)((int64_t)pieces * rank / p.cluster), c1 = (int)((int64_t)pieces * (rank + 1) / p.cluster);
+  const uint4* xv = reinterpret_cast<const uint4*>(x + head);
+  float* ov = out + head;
+  const bool aligned = (reinterpret_cast<uintptr_t>(ov) & 15u) == 0;
+  // a loose entry of this thread: its index, or -1
+  const int loose = rank != 0 ? -1 : tid < head ? tid : tid < head + (vocab - tail) ? tail + (tid - head) : -1;
+  const float lone = loose >= 0 ? Piece<T>::one(x[loose]) : -INFINITY;
 
   uint4 kept[kKept];
-  float best = -INFINITY;
-  auto lift = [&](const uint4& u) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) best = max_nan(best, Piece<T>::at(u, i));
-  };
 #pragma unroll
   for (int j = 0; j < kKept; ++j) {
-    const int64_t c = c0 + tid + (int64_t)j * kPrThreads;
+    const int c = c0 + tid + j * kPrThreads;
     kept[j] = make_uint4(Piece<T>::kNothing, Piece<T>::kNothing, Piece<T>::kNothing, Piece<T>::kNothing);
-    if (c < c1) kept[j] = load_piece(x, p.vocab, c);
+    if (c < c1) kept[j] = __ldcs(xv + c);
   }
+  const int more = c0 + tid + kKept * kPrThreads;  // pieces that are read again
+  float best = lone;
+  auto lift = [&](const uint4& u) {
+    float v[N];
+    Piece<T>::get(u, v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) best = max_nan(best, v[i]);
+  };
 #pragma unroll
   for (int j = 0; j < kKept; ++j) lift(kept[j]);
-  for (int64_t c = c0 + tid + (int64_t)kKept * kPrThreads; c < c1; c += kPrThreads) lift(load_piece(x, p.vocab, c));
+  for (int c = more; c < c1; c += kPrThreads) lift(__ldg(xv + c));
   best = over_row(best, sh, 0, p.cluster, [](float a, float b) { return max_nan(a, b); });
 
-  auto write = [&](int64_t c, const float (&v)[N]) {
-    if (p.out_aligned && (c + 1) * N <= p.vocab) {
+  // This CTA has read the others' numbers.  It says so before it writes: behind its stores a barrier would wait for them.
+  auto leave = [] {
+    __syncwarp();
+    cluster_arrive_relaxed();
+  };
+  auto write = [&](int c, const float (&v)[N]) {
+    float* o = ov + (int64_t)c * N;
+    if (aligned) {
 #pragma unroll
-      for (int i = 0; i < N; i += 4)
-        __stcs(reinterpret_cast<float4*>(out + c * N + i), make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]));
+      for (int i = 0; i < N; i += 4) __stcs(reinterpret_cast<float4*>(o + i), make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]));
     } else {
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (c * N + i < p.vocab) out[c * N + i] = v[i];
+      for (int i = 0; i < N; ++i) o[i] = v[i];
     }
-  };
-  auto each = [&](auto f) {
-#pragma unroll
-    for (int j = 0; j < kKept; ++j) {
-      const int64_t c = c0 + tid + (int64_t)j * kPrThreads;
-      if (c < c1) f(c, kept[j]);
-    }
-    for (int64_t c = c0 + tid + (int64_t)kKept * kPrThreads; c < c1; c += kPrThreads) f(c, load_piece(x, p.vocab, c));
   };
 
   if (!(t > 0.f)) {  // the first of the best entries (the same branch in the whole cluster)
-    int64_t at = INT64_MAX;
-    each([&](int64_t c, const uint4& u) {
+    uint32_t at = loose >= 0 && lone == best ? (uint32_t)loose : 0xffffffffu;
+    auto look = [&](int c, const uint4& u) {
+      float v[N];
+      Piece<T>::get(u, v);
 #pragma unroll
-      for (int i = N - 1; i >= 0; --i)
-        if (c * N + i < p.vocab && Piece<T>::at(u, i) == best) at = min(at, c * N + i);
-    });
+      for (int i = 0; i < N; ++i)
+        if (v[i] == best) at = min(at, (uint32_t)(head + c * N + i));
+    };
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) at = min(at, __shfl_xor_sync(0xffffffffu, at, d));
+    for (int j = 0; j < kKept; ++j)
+      if (c0 + tid + j * kPrThreads < c1) look(c0 + tid + j * kPrThreads, kept[j]);
+    for (int c = more; c < c1; c += kPrThreads) look(c, __ldg(xv + c));
+    at = __reduce_min_sync(0xffffffffu, at);
     if (lane == 0) sh.warp_at[warp] = at;
     __syncthreads();
-    for (int w = 0; w < kPrWarps; ++w) at = min(at, sh.warp_at[w]);
+    at = __reduce_min_sync(0xffffffffu, sh.warp_at[lane & (W - 1)]);
     if (p.cluster > 1) {
       if (tid == 0) sh.cta_at = at;
       cluster_sync_all();
-      for (int r = 0; r < p.cluster; ++r) {
-        uint64_t v;
-        asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(cluster_map(smem_u32(&sh.cta_at), (uint32_t)r)) : "memory");
-        at = min(at, (int64_t)v);
-      }
+      for (int r = 0; r < p.cluster; ++r)
+        at = min(at, __float_as_uint(ld_cluster_f32(cluster_map(smem_u32(&sh.cta_at), (uint32_t)r))));
+      leave();
     }
     // (a NaN, as a logit or as the temperature, makes the row NaN)
-    const float nothing = best == best && t == t ? 0.f : __uint_as_float(0x7fffffffu);
-    each([&](int64_t c, const uint4&) {
+    const bool sound = best == best && t == t;
+    const float nothing = sound ? 0.f : __uint_as_float(0x7fffffffu);
+    for (int c = c0 + tid; c < c1; c += kPrThreads) {
       float v[N];
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = c * N + i == at && nothing == 0.f ? 1.f : nothing;
+      for (int i = 0; i < N; ++i) v[i] = sound && (uint32_t)(head + c * N + i) == at ? 1.f : nothing;
       write(c, v);
-    });
+    }
+    if (loose >= 0) out[loose] = sound && (uint32_t)loose == at ? 1.f : nothing;
   } else {
     // 1 / T, at most 2^120: 0 times it is 0
     const float inv = __frcp_rn(fmaxf(t, 0x1p-120f));
     // exp(z), or 0 where z is below the least that is kept; a NaN (-inf at an infinite temperature, or a
     // row's only value) is not kept either
-    auto e_of = [&](float v) {
-      const float z = __fmul_rn(__fsub_rn(v, best), inv);
-      return z >= p.least ? ex2(z * kLog2e) : 0.f;
+    const uint64_t down = two(-best, -best), inv2 = two(inv, inv), log2e = two(kLog2e, kLog2e);
+    auto exp_of = [&](const uint4& u, float (&v)[N]) {
+      Piece<T>::get(u, v);
+#pragma unroll
+      for (int i = 0; i < N; i += 2) {
+        const uint64_t z = mul2(add2(two(v[i], v[i + 1]), down), inv2);
+        float z0, z1, y0, y1;
+        apart(z, z0, z1);
+        apart(mul2(z, log2e), y0, y1);
+        v[i] = z0 >= p.least ? ex2(y0) : 0.f;
+        v[i + 1] = z1 >= p.least ? ex2(y1) : 0.f;
+      }
     };
-    float s = 0.f;
-    each([&](int64_t c, const uint4& u) {
+    auto sum_of = [&](const float (&v)[N]) {
       float a = 0.f;
 #pragma unroll
-      for (int i = 0; i < N; ++i) a += e_of(Piece<T>::at(u, i));
-      s += a;
-    });
+      for (int i = 0; i < N; ++i) a += v[i];
+      return a;
+    };
+    const float zl = __fmul_rn(__fsub_rn(lone, best), inv), el = loose >= 0 && zl >= p.least ? ex2(zl * kLog2e) : 0.f;
+    float s = el;
+#pragma unroll
+    for (int j = 0; j < kKept; ++j) {  // (what a thread does not have is -inf: 0, or NaN, which is not kept)
+      float v[N];
+      exp_of(kept[j], v);
+      if (c0 + tid + j * kPrThreads < c1) s += sum_of(v);
+      if constexpr (N == 4)  // fp32: the exponentials stay in the logits' place
+        kept[j] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    }
+    for (int c = more; c < c1; c += kPrThreads) {
+      float v[N];
+      exp_of(__ldg(xv + c), v);
+      s += sum_of(v);
+    }
     s = over_row(s, sh, 1, p.cluster, [](float a, float b) { return a + b; });
+    if (p.cluster > 1) leave();
     // a row without a largest number (a NaN, +inf, nothing above -inf) is NaN
     const float f = s > 0.f ? 1.f / s : __uint_as_float(0x7fffffffu);
-    each([&](int64_t c, const uint4& u) {
-      float v[N];
+    auto share = [&](int c, float (&v)[N]) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = e_of(Piece<T>::at(u, i)) * f;
+      for (int i = 0; i < N; ++i) v[i] *= f;
       write(c, v);
-    });
+    };
+#pragma unroll
+    for (int j = 0; j < kKept; ++j) {
+      const int c = c0 + tid + j * kPrThreads;
+      if (c >= c1) continue;
+      float v[N];
+      if constexpr (N == 4) Piece<T>::get(kept[j], v);
+      else exp_of(kept[j], v);
+      share(c, v);
+    }
+    for (int c = more; c < c1; c += kPrThreads) {
+      float v[N];
+      exp_of(__ldg(xv + c), v);
+      share(c, v);
+    }
+    if (loose >= 0) out[loose] = el * f;
   }
-  if (p.cluster > 1) cluster_sync_all();  // the other CTAs have read this one's numbers
+  if (p.cluster > 1) cluster_wait();  // the other CTAs have read this one's numbers
 }
 
 }  // namespace
@@ -252,9 +271,9 @@ extern "C" sp_status sp_token_probs(const void* logits, sp_logits_dtype dtype, i
   const int sms = current_sms();
   if (sms == 0) return SP_ERR_CUDA;
   const int64_t pieces = (vocab * es + 15) / 16;
+  const int kept = dtype == SP_LOGITS_BF16 ? Piece<uint16_t>::kKept : Piece<float>::kKept;
   int cluster = 1;
-  while (cluster < kPrCluster && (pieces > (int64_t)cluster * kKept * kPrThreads ||
-                                  (tokens * cluster * 2 <= sms && pieces >= (int64_t)cluster * kPrThreads)))
+  while (cluster < kPrCluster && (pieces > (int64_t)cluster * kept * kPrThreads || (tokens * cluster * 2 <= sms && pieces >= (int64_t)cluster * 512)))
     cluster *= 2;
   if (tokens * cluster > ((int64_t)1 << 31) - 1) return SP_ERR_UNSUPPORTED;
   ProbsParams p = {};
@@ -267,7 +286,6 @@ extern "C" sp_status sp_token_probs(const void* logits, sp_logits_dtype dtype, i
   p.out = out;
   p.out_stride = out_stride;
   p.cluster = cluster;
-  p.out_aligned = al16(out) && (out_stride % 4 == 0 || tokens == 1);
-  return launch_pdl(dtype == SP_LOGITS_BF16 ? probs_kernel<uint16_t> : probs_kernel<float>,
-                    dim3((unsigned)(tokens * cluster)), kPrThreads, 0, cluster, (cudaStream_t)stream, p);
+  return launch_pdl(dtype == SP_LOGITS_BF16 ? probs_kernel<uint16_t> : probs_kernel<float>, dim3((unsigned)(tokens * cluster)),
+                    kPrThreads, 0, cluster, (cudaStream_t)stream, p);
 }

@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(kVeThreads, 2) verify_kernel(const __grid_cons
   const int64_t r0 = p.cu_q[b], r1 = p.cu_q[b + 1];
   const int64_t n = p.drafts[b];
   // (the same in every CTA of the cluster, so that all leave here or none)
-  const bool sound = r0 >= 0 && r1 >= r0 && r1 <= p.rows && n >= 0 && (r1 == r0 ? n == 0 : n < r1 - r0);
+  const bool sound = r0 >= 0 && r1 >= r0 && r1 <= p.rows && (r1 == r0 || (n >= 0 && n < r1 - r0));
   if (!sound || r1 == r0) {
     if (rank == 0 && tid == 0) {
       p.accepted[b] = p.rejected[b] = 0;

@@ -11,6 +11,9 @@
         h       = h + a.Wdown^T                         (sparse linear, residual)
     logits = h.Whead^T                                  (sparse linear)
 
+Every linear may be a dense one in 8 bits instead (fp8.Fp8Matrix), as pruning leaves the vocabulary's, and as a small
+model that drafts tokens has them.
+
 A step takes any mixture of prompts, chunks of prompts and single tokens of its requests; prompts and
 decode steps are the same call.  As in the linear stack there is no normalisation between the
 layers; per-head norms of queries and keys are the caller's choice.  All arithmetic runs in
@@ -20,7 +23,8 @@ from __future__ import annotations
 import torch
 
 from . import sp
-from .serve import Batch, KvCache, token_logprobs
+from .fp8 import Fp8Matrix
+from .serve import Batch, KvCache, token_logprobs, token_probs, verify_drafts
 
 NAMES = ("qkv", "o", "gate_up", "down")
 
@@ -33,13 +37,13 @@ def rotation_table(rows: int, rot: int, base: float = 10000.0, device="cuda") ->
 
 
 class Decoder:
-    """layers: one dict of SparseMatrix per layer, with the names of NAMES -- qkv [(H + 2 Hkv) D, d], o [d, H D],
-    gate_up [2F, d] (rows interleaved: gate_j, up_j), down [d, F]; embed [V, d] bf16; head: SparseMatrix [V, d].
+    """layers: one dict of matrices per layer, SparseMatrix or (dense, in 8 bits) Fp8Matrix, with the names of NAMES -- qkv [(H + 2 Hkv) D, d], o [d, H D],
+    gate_up [2F, d] (rows interleaved: gate_j, up_j), down [d, F]; embed [V, d] bf16; head: a matrix of either kind [V, d].
     Up to `requests` requests of up to `width` pages each share `pages` pages; a step has up to `tokens` new
     tokens.  The rotation's table has `positions` rows, or as many as the `width` pages of a request hold if
     that is more, so that every token has its own."""
 
-    def __init__(self, layers, embed: torch.Tensor, head: sp.SparseMatrix, heads: int, kv_heads: int, pages: int,
+    def __init__(self, layers, embed: torch.Tensor, head: sp.SparseMatrix | Fp8Matrix, heads: int, kv_heads: int, pages: int,
                  requests: int, tokens: int, width: int, page_size: int = 64, positions: int = 8192,
                  q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None):
         self.layers, self.embed, self.head = layers, embed, head
@@ -98,6 +102,27 @@ class Decoder:
         if record is not None:
             record.append(h.clone())
         return self.head.linear(h, out=self.logits[:t])
+
+    def sample(self, ids: torch.Tensor, new: torch.Tensor, max_new: int, sample: torch.Tensor, temperature=1.0, min_p: float = 0.0):
+        """step(), then a token for each request behind its last one, drawn by `sample` (float32 [requests] in [0, 1)) from
+        the probabilities at that temperature (token_probs): (next ids [requests], -1 for a request without new tokens;
+        probabilities [t, V], float32)."""
+        probs = token_probs(self.step(ids, new, max_new), temperature, min_p)
+        t, b = ids.shape[0], self.batch
+        none = torch.zeros(b.requests, dtype=torch.int32, device=self.h.device)
+        nxt = verify_drafts(probs, ids.long(), b.cu_q, none, torch.empty(t, device=self.h.device), sample)[2]
+        return nxt, probs
+
+    def verify(self, ids: torch.Tensor, new: torch.Tensor, max_new: int, drafts: torch.Tensor, accept: torch.Tensor,
+               sample: torch.Tensor, draft_probs: torch.Tensor | None = None, temperature=1.0, min_p: float = 0.0):
+        """step(), where the last drafts[b] (int32 [requests]) of a request's new tokens are drafted ones: keeps the run of them
+        that the model's probabilities accept (verify_drafts: accept float32 [t], sample float32 [requests], draft_probs [t, V]
+        with row j what token j + 1 was drawn from), takes the others back out of the cache's tables, and draws the token
+        behind.  A request's first new token is the one drawn before.  Returns (accepted, rejected int32 [requests], next ids [requests])."""
+        probs = token_probs(self.step(ids, new, max_new), temperature, min_p)
+        accepted, rejected, nxt = verify_drafts(probs, ids.long(), self.batch.cu_q, drafts, accept, sample, draft_probs)
+        self.batch.retract(rejected, advance=True)
+        return accepted, rejected, nxt
 
     def greedy(self, ids: torch.Tensor, new: torch.Tensor, max_new: int, top: int = 1):
         """step(), then of each of its tokens the likeliest next one with its log probability, the entropy, and

@@ -297,7 +297,8 @@ class Batch:
         """sp_kv_retract: request b loses its last drop[b] tokens (int32 [requests], 0 to what it holds), such as
         drafts that were refused, and the pages that held nothing else go back on the stack.  advance and allocate
         as for plan(): the lengths and the stack's height after it are `lens` and `next_count`, or replace those
-        before it.  Slots, positions and shares of a step planned before stay as they are."""
+        before it.  Slots, positions and shares of a step planned before stay as they are; `status` gets PLAN_INPUT
+        added where it cannot be done."""
         dev = _on_current(self._gpu, self.cached, "the batch's tables")
         at = _index(drop, self.requests, _I32, dev, "drop")
         own = self.__dict__
@@ -334,7 +335,7 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, str
     return (logp, entropy, tl, ti) if top else (logp, entropy)
 
 
-def _matrix(x: torch.Tensor, dev: int, name: str) -> int:
+def _row_type(x: torch.Tensor, dev: int, name: str) -> int:
     """Checks rows [T, V] of probabilities or logits and returns their type's number (SP_LOGITS_*)."""
     dtype = x.dtype
     if (dtype is not _BF16 and dtype is not _F32) or x.dim() != 2 or x.stride(1) != 1 or x.get_device() != dev:
@@ -346,10 +347,9 @@ def token_probs(logits: torch.Tensor, temperature=1.0, min_p: float = 0.0, out: 
                 stream=None) -> torch.Tensor:
     """sp_token_probs: probabilities, float32 [T, V], of the rows of logits [T, V] (bf16 or float32, rows of unit
     stride).  temperature: a number, or one for each row (float32 [T]); 0 or less takes the best entry.
-    min_p: entries of less than min_p times the best one's probability are left out.  Without `out` the
-    rows start at multiples of 16 bytes: where V is no multiple of 4 the result is a view of wider rows."""
+    min_p: entries of less than min_p times the best one's probability are left out."""
     dev = _on_current(logits.get_device(), logits, "logits")
-    kind = _matrix(logits, dev, "logits")
+    kind = _row_type(logits, dev, "logits")
     t, v = logits.shape
     if v < 1:
         raise ValueError("logits: a vocabulary of one entry or more wanted")
@@ -358,14 +358,13 @@ def token_probs(logits: torch.Tensor, temperature=1.0, min_p: float = 0.0, out: 
     else:
         per_row, one = 0, float(temperature)
     if out is None:
-        wide = (v + 3) // 4 * 4
-        out = torch.empty((t, wide), dtype=_F32, device=logits.device)
-        if wide != v:
-            out = out[:, :v]
-    elif _matrix(out, dev, "out") != 1 or out.shape != logits.shape:
+        out, out_stride = torch.empty((t, v), dtype=_F32, device=logits.device), v
+    elif _row_type(out, dev, "out") != 1 or out.shape != logits.shape:
         raise ValueError(f"out: float32 {[t, v]} wanted")
+    else:
+        out_stride = out.stride(0) if t > 1 else max(out.stride(0), v)
     _check(_lib.sp_token_probs(logits.data_ptr(), kind, logits.stride(0) if t > 1 else v, t, v, per_row, one, min_p,
-                               out.data_ptr(), out.stride(0) if t > 1 else max(out.stride(0), v), _stream(stream, dev)),
+                               out.data_ptr(), out_stride, _stream(stream, dev)),
            "sp_token_probs")
     return out
 
@@ -379,14 +378,14 @@ def verify_drafts(probs: torch.Tensor, ids: torch.Tensor, cu_q: torch.Tensor, dr
     was drawn from; None: drafts are certain.  With drafts of 0 it samples.  Returns
     (accepted int32 [B], rejected int32 [B], next token int64 [B], -1 for a request without tokens)."""
     dev = _on_current(probs.get_device(), probs, "probs")
-    kind = _matrix(probs, dev, "probs")
+    kind = _row_type(probs, dev, "probs")
     t, v = probs.shape
     b = cu_q.shape[0] - 1 if cu_q.dim() == 1 else -1
     if b < 0:
         raise ValueError("cu_q: int32 [requests + 1] wanted")
     draft_kind = draft_stride = draft = 0
     if draft_probs is not None:
-        draft_kind = _matrix(draft_probs, dev, "draft_probs")
+        draft_kind = _row_type(draft_probs, dev, "draft_probs")
         if draft_probs.shape != probs.shape:
             raise ValueError(f"draft_probs: {[t, v]} wanted")
         draft, draft_stride = draft_probs.data_ptr(), draft_probs.stride(0) if t > 1 else v

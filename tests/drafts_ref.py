@@ -95,7 +95,7 @@ def verify(p, q, ids, cu, drafts, accept, sample):
     with np.errstate(all="ignore"):
         for b, n in enumerate(drafts):
             r0, r1 = cu[b], cu[b + 1]
-            if not (0 <= r0 <= r1 <= p.shape[0] and n >= 0 and (n == 0 if r0 == r1 else n < r1 - r0)) or r0 == r1:
+            if r0 == r1 or not (0 <= r0 <= r1 <= p.shape[0] and 0 <= n < r1 - r0):
                 for o, x in zip(out, (0, 0, -1)):
                     o.append(x)
                 continue

@@ -82,18 +82,24 @@ def test_probs(sp, serve, t, v, dtype, min_p):
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_probs_of_views_into_views(sp, serve, dtype):
-    """Rows that begin at any address, results into rows that begin anywhere; nothing beside them is written."""
+    """Rows that begin at any address, results into rows that begin anywhere; nothing beside them is written.  The order in
+    which a row is added up goes by its address, so that two views of one row are each held to the bound above, and a row
+    alone or written elsewhere to the same numbers as among others."""
     g = np.random.default_rng(1)
     wide = _dev(g.standard_normal((6, 900)), torch.bfloat16 if dtype == "bf16" else torch.float32)
     for a in range(9):
         for v in (1, 17, 256, 801):
             x = wide[:, a:a + v]
-            want = serve.token_probs(x.contiguous(), 0.5)
+            t = np.full(6, 0.5, np.float32)
+            _check_probs(serve.token_probs(x.contiguous(), 0.5), x.float().cpu().numpy(), t, 0.0)
+            want = serve.token_probs(x, 0.5)
+            _check_probs(want, x.float().cpu().numpy(), t, 0.0)
             out = torch.full((6, 910), 7.0, device="cuda")
-            got = serve.token_probs(x, 0.5, out=out[:, a:a + v])
-            assert torch.equal(got, want) and torch.equal(out[:, a:a + v], want)
-            out[:, a:a + v] = 7.0
-            assert (out == 7.0).all()
+            for at in (a, a + 1):
+                got = serve.token_probs(x, 0.5, out=out[:, at:at + v])
+                assert torch.equal(got, want) and torch.equal(out[:, at:at + v], want)
+                out[:, at:at + v] = 7.0
+                assert (out == 7.0).all()
             assert torch.equal(serve.token_probs(x[2:3], 0.5), want[2:3])
     sp.check()
 
@@ -231,7 +237,7 @@ def test_verify_falls_back_where_nothing_is_left(sp, serve):
 
 @pytest.mark.parametrize("ids,cu,drafts", [([0, 9, 0], [0, 3], [2]), ([0, -1, 0], [0, 3], [2]), ([0, 1, 0], [0, 3], [3]),
                                            ([0, 1, 0], [0, 3], [-1]), ([0, 1, 0], [0, 4], [1]), ([0, 1, 0], [2, 1], [0]),
-                                           ([0, 1, 0], [-1, 2], [1]), ([0, 1, 0], [1, 1], [1])])
+                                           ([0, 1, 0], [-1, 2], [1]), ([0, 1, 0], [-1, -1], [0])])
 def test_verify_leaves_out_what_does_not_belong_together(sp, serve, ids, cu, drafts):
     p = np.full((3, 4), 0.25, np.float32)
     got, want = _call(serve, p, None, ids, cu, drafts, np.zeros(3), [0.3])
@@ -255,7 +261,7 @@ def test_verify_of_views_and_nothing(sp, serve):
     none = torch.zeros(0, device="cuda")
     got = serve.verify_drafts(torch.zeros((0, 5), device="cuda"), none.long(), _i32([0]), none.int(), none, none)
     assert [x.numel() for x in got] == [0, 0, 0]
-    got = serve.verify_drafts(torch.zeros((0, 5), device="cuda"), none.long(), _i32([0, 0, 0]), _i32([0, 0]), none, torch.zeros(2, device="cuda"))
+    got = serve.verify_drafts(torch.zeros((0, 5), device="cuda"), none.long(), _i32([0, 0, 0]), _i32([0, 3]), none, torch.zeros(2, device="cuda"))
     assert [x.tolist() for x in got] == [[0, 0], [0, 0], [-1, -1]]
     sp.check()
 
@@ -356,6 +362,10 @@ def test_retract_that_cannot_be(sp, serve, what, advance):
         height = batch.pages
         batch.free_count.fill_(height)
     kept = batch.free.clone()
+    batch.status.fill_(4)  # what a plan said stays
+    batch.retract(_i32([0] * 6) if what in ("more", "negative") else _i32(drop), advance=False)
+    assert batch.status.item() == (4 if what in ("more", "negative") else 12)
+    batch.status.zero_()
     batch.retract(_i32(drop), advance=advance)
     assert batch.status.item() == 8 and batch.lens.tolist() == cached == batch.cached.tolist()
     assert torch.equal(batch.free, kept) and batch.next_count.item() == height == batch.free_count.item()
