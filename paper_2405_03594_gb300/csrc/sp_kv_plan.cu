@@ -9,7 +9,8 @@
 // first token writes it to the table.  A warp looks for the request of its first token among 32
 // shares at a time, and then among 32 requests, so that a search is few loads.
 //
-// Tokens that a step's verification refused give their pages back by a kernel of the same kind.
+// Tokens that a step's verification refused give their pages back by a kernel of the same kind: 64 requests 2.6 us, 1000 requests with
+// up to three pages each 4.5 us.
 //
 // Measured: 64 requests with a token each 4.5 us; 1000 requests with up to 256 new tokens each, some of them ended,
 // 13.2 us: the one CTA's loads and scans, which wait for one another, then the slots' grid.

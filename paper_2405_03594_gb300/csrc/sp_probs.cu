@@ -7,6 +7,10 @@
 // row's bytes in and out.  Pieces begin at the row's first 16-byte boundary; the entries before it and behind the last piece
 // go to rank 0's first threads.  Rows of logits and of probabilities that lie as densely have their boundaries at the same
 // entries, so that the pieces of both are aligned.
+//
+// Measured: 320 rows of 131071, fp32 (168 MB in, 168 out) 82 us, 4.1 TB/s: a row's exchanges, during which its CTAs neither load nor
+// write, and half of it read again (clusters of four 85 us, of two 120). Five rows of 32000, bf16, 4.5 us. The first form, which put
+// misaligned pieces together from two loads and worked out the exponentials twice, took 130 and 7.2.
 #include <cmath>
 
 #include "sp_attend.cuh"
@@ -135,7 +139,7 @@ __global__ void __launch_bounds__(kPrThreads, 4) probs_kernel(const __grid_const
   // This CTA has read the others' numbers.  It says so before it writes: behind its stores a barrier would wait for them.
   auto leave = [] {
     __syncwarp();
-    cluster_arrive_relaxed();
+    cluster_arrive_release();
   };
   auto write = [&](int c, const float (&v)[N]) {
     float* o = ov + (int64_t)c * N;

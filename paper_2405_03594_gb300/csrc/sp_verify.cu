@@ -8,7 +8,12 @@
 //
 // A request has a CTA, or a cluster where requests are few.  It looks at its drafts (a few loads that wait for one
 // another), then reads one row of p and one of q: every warp adds up a stretch of its own, the totals go
-// around, and the warp in whose stretch the drawn number falls goes over it again for the entry.
+// around, and the CTA in one of whose stretches the drawn number falls shares that one out among its warps until one looks at it
+// whole.
+//
+// Measured: one request with four drafts over 32000 entries 5.1 us; 64 requests over 131071 (34 MB of p, fp32, and 17 of q, bf16) 18 us, of which
+// the rows' bytes take 7.4: the loads before them that wait for one another (3 us), the launch, the totals' way around and
+// the search are the rest. 256 rows of 32000 without drafts (33 MB) 11.0 us.
 #include <type_traits>
 
 #include "sp_kv4.cuh"
@@ -187,6 +192,7 @@ __global__ void __launch_bounds__(kVeThreads, 2) verify_kernel(const __grid_cons
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = p.cluster > 1 ? (int)cluster_rank() : 0;
   const int64_t b = blockIdx.x / p.cluster;
+  pdl_launch_dependents();
   pdl_wait();
   const int64_t r0 = p.cu_q[b], r1 = p.cu_q[b + 1];
   const int64_t n = p.drafts[b];
