@@ -133,10 +133,9 @@ __global__ void __launch_bounds__(FewPlan<MT, FUSED>::kThreads, FewPlan<MT, FUSE
           ph ^= 1u;
         }
       }
-      if (dead) {  // the copies under way, before the CTA's memory goes
-        set_status(p.status, kStatusTimeout);
-        for (int i = max(0, issued - S); i < issued; ++i) mbar_wait(&w_full[i % S], (uint32_t)((i / S) & 1), p.timeout_ns);
-      }
+      if (dead) set_status(p.status, kStatusTimeout);
+      // the last copies, before the CTA's memory goes: whoever waited for them may have given up
+      for (int i = max(0, issued - S); i < issued; ++i) mbar_wait(&w_full[i % S], (uint32_t)((i / S) & 1), p.timeout_ns);
     }
   } else if (warp == 5) {
     // ------------------------------------------------------------ products

@@ -302,13 +302,17 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
         } else {
           __syncwarp();
           const int rows = (int)imin64(32, p.m - m0);
-          for (int r = 0; r < rows; ++r) {
-            uint16_t* yp = p.y + (m0 + r) * p.y_stride + n0 + c;
+          uint16_t* yp = p.y + m0 * p.y_stride + n0 + c + lane;
+#pragma unroll 1
+          for (int r0 = 0; r0 < rows; r0 += 8) {
 #pragma unroll
-            for (int k = 0; k < 64; k += 32) {
-              const int j = (k + lane) >> 3;
-              const uint16_t u = *reinterpret_cast<const uint16_t*>(st + r * 128 + ((j ^ (r & 7)) << 4) + ((lane & 7) << 1));
-              if (n0 + c + k + lane < p.n) yp[k + lane] = u;
+            for (int r = r0; r < r0 + 8; ++r) {
+#pragma unroll
+              for (int k = 0; k < 64; k += 32) {
+                const int j = (k + lane) >> 3;
+                const uint16_t u = *reinterpret_cast<const uint16_t*>(st + r * 128 + ((j ^ (r & 7)) << 4) + ((lane & 7) << 1));
+                if (r < rows && n0 + c + k + lane < p.n) yp[r * p.y_stride + k] = u;
+              }
             }
           }
           __syncwarp();
