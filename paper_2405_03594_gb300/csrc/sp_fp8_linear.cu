@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
     const uint32_t lane_base = ((uint32_t)(q * 32) << 16) + (uint32_t)(part * C);
     const uint32_t d_empty0 = cluster_map(smem_u32(d_empty), 0);
     uint8_t* staging = ring + P::kStages * P::kStage + (warp - 4) * 2 * kStageBytes;
-    int s = 0;
+    int s = 0, turn = 0;
     uint32_t ph = 0;
     bool dead = false, ready = false;
     pdl_wait();  // the scales and y belong to the stream order
@@ -286,7 +286,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
       // 64 columns of the warp's 32 rows, by way of shared memory: 16-byte piece j of row r lies at j ^ (r & 7), so that neither the
       // writes nor the copies out meet in a bank
       auto store = [&](int c, const float* v) {
-        uint8_t* st = staging + (c / 64 & 1) * kStageBytes;
+        uint8_t* st = staging + turn * kStageBytes;
+        turn ^= 1;  // (the two buffers in turn, over all tiles: the copy before the last one is waited for)
         if (p.y_tma && lane == 0) bulk_wait_read<1>();  // the copy that last read it is done
         __syncwarp();
 #pragma unroll

@@ -107,7 +107,7 @@ struct Rows {
     return 0.f;
   }
   __device__ __forceinline__ float left(int i, float a, float b) const {
-    if constexpr (!kDraft) return i == not_this ? 0.f : a;  // (a - 1, or less than nothing)
+    if constexpr (!kDraft) return i == not_this ? __fsub_rn(a, 1.f) : a;
     return __fsub_rn(a, b);
   }
   __device__ __forceinline__ float left_at(int i) const { return i >= 0 && i < vocab ? left(i, number(__ldg(p + i)), draft(i)) : 0.f; }

@@ -311,3 +311,48 @@ def test_workspace_is_shared_with_the_other_linears(sp, fp8):
         for _ in range(3):
             assert torch.equal(h.linear(x, workspace=ws), a) and torch.equal(w.linear(x, workspace=ws), b)
     sp.check()
+
+
+def test_linears_on_two_streams_at_once(sp, fp8):
+    """Calls of every kind that overlap: each stream has its own workspace, and the rows' codes may be shared."""
+    g = _gen(11)
+    w = fp8.Fp8Matrix.from_dense(_w(2100, 1500, g))
+    xs = [_x(m, 1500, g) for m in (1, 8, 40, 100, 600, 100, 3)]
+    qs = [fp8.quantize_rows(x) for x in xs]
+    want = [w.linear(x) for x in xs]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[] for _ in streams]
+    for _ in range(5):
+        for st, out in zip(streams, got):
+            with torch.cuda.stream(st):
+                out += [w.linear(x) for x in xs] + [w.linear(q) for q in qs]
+    torch.cuda.synchronize()
+    for out in got:
+        for i, y in enumerate(out):
+            assert torch.equal(y, want[i % 7]), i
+    sp.check()
+
+
+def test_tiles_that_are_shared_in_graphs_that_share_nothing(sp, fp8):
+    """A batch whose tiles are shared by pairs, captured twice and replayed on two streams at once."""
+    g = _gen(12)
+    w = fp8.Fp8Matrix.from_dense(_w(1000, 9000, g))
+    xs = [_x(150, 9000, g) for _ in range(2)]
+    want = [w.linear(x) for x in xs]
+    graphs, outs = [], []
+    for x in xs:
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            outs.append(w.linear(x))
+        graphs.append(gr)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for st, gr in zip(streams, graphs):
+            with torch.cuda.stream(st):
+                gr.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    _check(outs[0], fp8.quantize_rows(xs[0]), w)
+    sp.check()
