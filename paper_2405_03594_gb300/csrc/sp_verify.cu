@@ -11,9 +11,9 @@
 // around, and the CTA in one of whose stretches the drawn number falls shares that one out among its warps until one looks at it
 // whole.
 //
-// Measured: one request with four drafts over 32000 entries 5.1 us; 64 requests over 131071 (34 MB of p, fp32, and 17 of q, bf16) 18 us, of which
-// the rows' bytes take 7.4: the loads before them that wait for one another (3 us), the launch, the totals' way around and
-// the search are the rest. 256 rows of 32000 without drafts (33 MB) 11.0 us.
+// Measured: one request with four drafts over 32000 entries 4.6 us; 64 requests over 131071 (34 MB of p, fp32, and 17 of q, bf16) 17.4 us, of
+// which the rows take 11.6 (4.3 TB/s: four batches of loads a thread, one after the other), the search for the entry 1.7, the launch and the
+// loads before the rows 4; 256 rows of 32000 without drafts (33 MB) 11.4 us, the rows 5.6 of them.
 #include <type_traits>
 
 #include "sp_kv4.cuh"
@@ -21,7 +21,7 @@
 namespace sp {
 namespace {
 
-constexpr int kVeThreads = 512;
+constexpr int kVeThreads = 256;
 constexpr int kVeWarps = kVeThreads / 32;
 constexpr int kVeCluster = 8;
 constexpr int64_t kVeMostVocab = (int64_t)1 << 22;  // sums of weights of up to 2^40 stay below 2^63
@@ -181,7 +181,7 @@ __device__ __forceinline__ uint64_t warp_sum(uint64_t v) {
 }
 
 template <typename T, typename Q>
-__global__ void __launch_bounds__(kVeThreads, 2) verify_kernel(const __grid_constant__ VerifyParams p) {
+__global__ void __launch_bounds__(kVeThreads, 4) verify_kernel(const __grid_constant__ VerifyParams p) {
   constexpr bool kDraft = Rows<T, Q>::kDraft;
   constexpr int kBatch = Rows<T, Q>::kBatch;
   __shared__ uint64_t s_warp[kVeWarps];
@@ -361,7 +361,8 @@ extern "C" sp_status sp_verify_drafts(const sp_verify_args* a, void* stream) {
   const int sms = current_sms();
   if (sms == 0) return SP_ERR_CUDA;
   int cluster = 1;
-  while (cluster < kVeCluster && (int64_t)a->requests * cluster * 2 <= 2 * sms && a->vocab >= (int64_t)cluster * 2 * 4 * kVeThreads)
+  // (four CTAs to an SM, a few quads for each thread; 512 threads, two to an SM: one request 5.1 us for 4.6, 64 requests 18.1 for 17.4)
+  while (cluster < kVeCluster && (int64_t)a->requests * cluster * 2 <= 4 * sms && a->vocab >= (int64_t)cluster * 2 * 4 * kVeThreads)
     cluster *= 2;
   if ((int64_t)a->requests * cluster > ((int64_t)1 << 31) - 1) return SP_ERR_UNSUPPORTED;
   VerifyParams p = {};
