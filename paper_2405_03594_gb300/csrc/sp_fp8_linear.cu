@@ -37,8 +37,10 @@ constexpr int kPairThreads = 128 + 32 * kPairEpi;
 
 template <int NT>  // rows of W in a tile
 struct PairPlan {
-  static constexpr int kAccs = NT == 256 ? 2 : 4;    // sums of blocks in tensor memory at a time
-  static constexpr uint32_t kTmem = NT * kAccs;
+  static constexpr int kColumns = NT * 4 / kPairEpi;              // of a warp
+  static constexpr int kOut = kColumns % 64 == 0 ? 64 : 32;       // of them go out at a time
+  static constexpr int kAccs = NT == 128 ? 4 : 2;    // sums of blocks in tensor memory at a time
+  static constexpr uint32_t kTmem = 512;
   static constexpr uint32_t kStage = kXBytes + NT / 2 * 128;
   static constexpr uint32_t kStaging = kPairEpi * 2 * kStageBytes;
   static constexpr int kFit = (int)((227 * 1024 - 1024 - kCtl - kStaging) / kStage);
@@ -195,7 +197,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
   } else {
     // ------------------------------------------------------------ epilogue: thread = token, some of the columns
     registers_up<232>();
-    constexpr int C = NT * 4 / kPairEpi;
+    constexpr int C = P::kColumns, O = P::kOut;
+    constexpr bool kTwo = NT == 192;  // a warp's columns may lie in two of W's blocks (32 of them never do)
     const int q = warp & 3, part = (warp - 4) >> 2;
     const uint32_t lane_base = ((uint32_t)(q * 32) << 16) + (uint32_t)(part * C);
     const uint32_t d_empty0 = cluster_map(smem_u32(d_empty), 0);
@@ -205,12 +208,13 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
     bool dead = false, ready = false;
     pdl_wait();  // the scales and y belong to the stream order
     // the scales of four blocks are asked for while the four before them are worked on
-    const float *px = nullptr, *pw = nullptr;
-    float xs[4], ws[4];
+    const float *px = nullptr, *pw = nullptr, *pw2 = nullptr;
+    float xs[4], ws[4], ws2[4];
     int b1 = 0;
     auto ask = [&](int b, int j) {
       const int64_t c = min(b + j, b1 - 1);
       xs[j] = __ldg(px + c * p.x_scale_stride), ws[j] = __ldg(pw + c);
+      if constexpr (kTwo) ws2[j] = __ldg(pw2 + c);
     };
     auto ask_first = [&](int64_t i) {  // of item i
       const PairItem it = item_at<SPLIT>(p, i);
@@ -219,6 +223,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
       const bool there = token < p.m && n0 < p.n;
       px = p.x_scale + (there ? token : 0);
       pw = p.w_scale + (there ? n0 / kFp8Block * p.blocks : 0);
+      if constexpr (kTwo) pw2 = p.w_scale + (there ? imin64(n0 + C - 1, p.n - 1) / kFp8Block * p.blocks : 0);
 #pragma unroll
       for (int j = 0; j < 4; ++j) ask(it.b0, j);
     };
@@ -229,7 +234,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
       float acc[C];
 #pragma unroll
       for (int j = 0; j < C; ++j) acc[j] = 0.f;
-      auto block = [&](float sc) {
+      const int turn_at = kTwo ? (int)(kFp8Block - n0 % kFp8Block) : C;  // the first column of the second block
+      auto block = [&](float sc1, float sc2) {
         if (!__all_sync(0xffffffffu, ready)) {
           // (behind a wait that has expired nothing waits, and what is read is worth nothing)
           if (!dead && !__all_sync(0xffffffffu, mbar_wait_short(&done[s], ph, p.timeout_ns))) {
@@ -259,9 +265,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
             }
             ready = mbar_test(&done[s], ph);
           }
+          const float sc = kTwo && c >= turn_at ? sc2 : sc1;
 #pragma unroll
           for (int j = 0; j < 32; j += 2) {
-            if constexpr (NT == 128) {
+            if constexpr (NT != 256) {
               fma2_behind(acc[c + j], acc[c + j + 1], d[now][j], d[now][j + 1], sc);
             } else {
               fma_behind(acc[c + j], d[now][j], sc);
@@ -272,27 +279,30 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
       };
 #pragma unroll 1
       for (int b = it.b0; b < it.b1; b += 4) {
-        float sc[4];
+        float sc[4], sc2[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           sc[j] = xs[j] * ws[j];
+          sc2[j] = kTwo ? xs[j] * ws2[j] : 0.f;
           ask(b + 4, j);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (b + j < it.b1) block(sc[j]);
+          if (b + j < it.b1) block(sc[j], sc2[j]);
       }
       if (i + pairs < p.items) ask_first(i + pairs);
-      // 64 columns of the warp's 32 rows, by way of shared memory: 16-byte piece j of row r lies at j ^ (r & 7), so that neither the
-      // writes nor the copies out meet in a bank
+      // O columns of the warp's 32 rows, by way of shared memory, laid out as TMA swizzles them, so that neither the writes nor the
+      // copies out meet in a bank: 16-byte piece j of a row r of 128 bytes lies at j ^ (r & 7), of 64 bytes at j ^ (r / 2 & 3)
+      constexpr int kPieces = O / 8;
+      auto place = [&](int r, int j) { return r * (2 * O) + ((O == 64 ? j ^ (r & 7) : j ^ (r >> 1 & 3)) << 4); };
       auto store = [&](int c, const float* v) {
         uint8_t* st = staging + turn * kStageBytes;
         turn ^= 1;  // (the two buffers in turn, over all tiles: the copy before the last one is waited for)
         if (p.y_tma && lane == 0) bulk_wait_read<1>();  // the copy that last read it is done
         __syncwarp();
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          *reinterpret_cast<uint4*>(st + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+        for (int j = 0; j < kPieces; ++j)
+          *reinterpret_cast<uint4*>(st + place(lane, j)) =
               make_uint4(pack_bf16(v[8 * j], v[8 * j + 1]), pack_bf16(v[8 * j + 2], v[8 * j + 3]),
                          pack_bf16(v[8 * j + 4], v[8 * j + 5]), pack_bf16(v[8 * j + 6], v[8 * j + 7]));
         if (p.y_tma) {
@@ -309,9 +319,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
 #pragma unroll
             for (int r = r0; r < r0 + 8; ++r) {
 #pragma unroll
-              for (int k = 0; k < 64; k += 32) {
-                const int j = (k + lane) >> 3;
-                const uint16_t u = *reinterpret_cast<const uint16_t*>(st + r * 128 + ((j ^ (r & 7)) << 4) + ((lane & 7) << 1));
+              for (int k = 0; k < O; k += 32) {
+                const uint16_t u = *reinterpret_cast<const uint16_t*>(st + place(r, (k + lane) >> 3) + ((lane & 7) << 1));
                 if (r < rows && n0 + c + k + lane < p.n) yp[r * p.y_stride + k] = u;
               }
             }
@@ -321,7 +330,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
       };
       if (!SPLIT) {
 #pragma unroll
-        for (int c = 0; c < C; c += 64) store(c, acc + c);
+        for (int c = 0; c < C; c += O) store(c, acc + c);
       } else {
         const int64_t rest = i / p.split;
         auto share = [&](int64_t k) { return p.part + ((k * 2 + rank) * NT + part * C) * 128 + q * 32 + lane; };
@@ -337,17 +346,17 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
         if (last) {  // of the tile's shares to arrive: it adds up all of them, in order
           __threadfence();
 #pragma unroll 1
-          for (int c = 0; c < C; c += 64) {
-            float v[64];
+          for (int c = 0; c < C; c += O) {
+            float v[O];
 #pragma unroll
-            for (int j = 0; j < 64; ++j) v[j] = 0.f;
+            for (int j = 0; j < O; ++j) v[j] = 0.f;
             for (int k = 0; k < p.split; ++k) {
               const float* src = share(rest * p.split + k) + c * 128;
-              float u[64];
+              float u[O];
 #pragma unroll
-              for (int j = 0; j < 64; ++j) u[j] = __ldcg(src + j * 128);
+              for (int j = 0; j < O; ++j) u[j] = __ldcg(src + j * 128);
 #pragma unroll
-              for (int j = 0; j < 64; ++j) v[j] += u[j];
+              for (int j = 0; j < O; ++j) v[j] += u[j];
             }
             store(c, v);
           }
@@ -397,18 +406,18 @@ sp_status code_map(CUtensorMap* map, PFN_cuTensorMapEncodeTiled_v12000 encode, c
              : SP_ERR_CUDA;
 }
 
-// The work of fp8_pair_kernel on `pairs` pairs, and its time in clocks: 890 for a block of 256 columns and 570 for one of 128,
+// The work of fp8_pair_kernel on `pairs` pairs, and its time in clocks: 890 for a block of 256 columns, 750 for one of 192 and 570 for one of 128,
 // and some 3500 around a tile. Where tiles are fewer than the pairs they are shared by the blocks of their columns, at 4000
 // and some for each share, if that is less. Measured, us, with shares / without: 128 x 4096 x 11008 (NT = 128, two) 26.5 / 38.3; tiles left
-// by whole waves in a launch of shares behind them: 512 x 12288 x 4096 52 / 38, so those are not shared. The two widths, 128 / 256, us:
-// 128 x 4096 x 4096 16.8 / 22.7, 256 x 22016 x 4096 41.1 / 39.9, 4096 x 22016 x 4096 362 / 300.
+// by whole waves in a launch of shares behind them: 512 x 12288 x 4096 52 / 38, so those are not shared. The three widths, 128 / 192 / 256, us:
+// 100 x 3000 x 4096 15.3 / 19.6 / 21.8, 512 x 12288 x 4096 40.2 / 35.2 / 37.3, 4096 x 22016 x 4096 368 / 366 / 299.
 struct PairWork {
   int64_t tiles;
   int split;
   double clocks;
 };
 PairWork pair_work(int nt, int64_t m, int64_t n, int64_t blocks, int64_t pairs) {
-  const double block = nt == 256 ? 890 : 570, share = nt == 256 ? 2500 : 1000;
+  const double block = nt == 256 ? 890 : nt == 192 ? 750 : 570, share = nt == 128 ? 1000 : 2500;
   PairWork w = {(m + kPairTokens - 1) / kPairTokens * ((n + nt - 1) / nt), 1, 0};
   double best = block * blocks;
   for (int s = 2; s <= pairs / w.tiles && s <= blocks / 4; ++s) {
@@ -473,9 +482,9 @@ sp_status launch_pair(const sp_fp8_linear_args& a, const Fp8Rows& rows, void* ws
   p.y_tma = al16(a.y) && a.y_stride % 8 == 0;
   if (p.y_tma) {
     const cuuint64_t dim[2] = {(cuuint64_t)a.n, (cuuint64_t)a.m}, strides[1] = {(cuuint64_t)a.y_stride * 2};
-    const cuuint32_t box[2] = {64, 32}, estride[2] = {1, 1};
+    const cuuint32_t box[2] = {(cuuint32_t)PairPlan<NT>::kOut, 32}, estride[2] = {1, 1};
     if (encode(&map_y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, a.y, dim, strides, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+               PairPlan<NT>::kOut == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
       return SP_ERR_CUDA;
   }
   p.status = device_status_ptr();
@@ -537,7 +546,9 @@ extern "C" sp_status sp_fp8_linear(const sp_fp8_linear_args* a, void* ws, size_t
   // rows of W in a tile: where the time is less
   const int64_t blocks = (a->k + kFp8Block - 1) / kFp8Block;
   float* part = reinterpret_cast<float*>(base + w.part);
-  return pair_work(256, a->m, a->n, blocks, sms / 2).clocks <= pair_work(128, a->m, a->n, blocks, sms / 2).clocks
-             ? launch_pair<256>(*a, rows, ws, part, sms, encode, stream)
-             : launch_pair<128>(*a, rows, ws, part, sms, encode, stream);
+  auto clocks = [&](int nt) { return pair_work(nt, a->m, a->n, blocks, sms / 2).clocks; };
+  const int nt = clocks(256) <= clocks(192) && clocks(256) <= clocks(128) ? 256 : clocks(192) <= clocks(128) ? 192 : 128;
+  return nt == 256   ? launch_pair<256>(*a, rows, ws, part, sms, encode, stream)
+         : nt == 192 ? launch_pair<192>(*a, rows, ws, part, sms, encode, stream)
+                     : launch_pair<128>(*a, rows, ws, part, sms, encode, stream);
 }

@@ -127,7 +127,8 @@ def test_quantisation_of_views(sp, fp8):
 SIZES = [(1, 1, 1), (1, 128, 128), (1, 4096, 4096), (2, 130, 5), (3, 127, 129), (8, 5000, 300), (15, 256, 2049), (16, 300, 384),
          (17, 129, 257), (31, 1000, 1000), (33, 127, 1000), (48, 2000, 513), (64, 1000, 640), (65, 129, 129), (100, 70, 4000),
          (127, 333, 100), (128, 1024, 1024), (129, 257, 385), (200, 3000, 128), (256, 512, 2048), (257, 700, 1111), (299, 5003, 1999),
-         (511, 1100, 700), (600, 4096, 2000), (1000, 900, 11008), (1025, 130, 600), (2049, 2100, 130)]
+         (511, 1100, 700), (600, 4096, 2000), (1000, 900, 11008), (1025, 130, 600), (2049, 2100, 130),
+         (512, 12288, 256), (300, 12301, 390), (1030, 7000, 129), (70, 30000, 640)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
