@@ -150,18 +150,24 @@ struct Fp8Rows {
 // fp8_few_kernel: up to kFewTokens rows.
 constexpr int kFewTokens = 64;
 inline int few_box(int64_t m) { return m <= 16 ? 16 : m <= 32 ? 32 : 64; }  // rows of x in a tile, of map_x's box
-// CTAs that share a tile: as many as the SMs hold at once, `ctas` each, with two blocks each at least.
-inline int few_cluster(int64_t n, int64_t blocks, int ctas, int sms) {
+constexpr int kFewCtas = 2;  // of its CTAs on an SM
+// CTAs that share a tile: as many as the SMs hold at once, with two blocks each at least. Tiles of 64 tokens keep an SM busy alone, and take
+// two CTAs to one only for short stretches. Measured, us: 1 x 4096 x 4096 with eight 5.9, with four 6.3; 64 x 4096 x 4096 with eight 11.2, four
+// (an SM each) 12.8; 64 x 12288 x 4096 with one 17.9, two 20.6, three 21.8; 24 x 5120 x 5120 with four 10.8, with seven, for which there is less
+// room than eight CTAs' worth, 14.5.
+inline int few_cluster(int64_t m, int64_t n, int64_t blocks, int sms) {
   const int64_t tiles = (n + kFp8Block - 1) / kFp8Block;
   int c = 1;
-  while (c < 8 && tiles * c * 2 <= (int64_t)ctas * sms && blocks >= 4 * c) c *= 2;
+  while (c < 8 && tiles * c * 2 <= (int64_t)kFewCtas * sms && blocks >= 4 * c &&
+         (m <= 32 || tiles * c * 2 <= sms || blocks <= 24 * c))
+    c *= 2;
   return c;
 }
 // Whether that kernel quantises x itself, which every tile then does again (rows: NULL; no workspace): up to eight rows, and up
 // to ten pairs of rows of a block for each of its four warps. Measured, us, so / by a launch before: 8 x 4096 x 4096 (four) 7.5 / 9.0,
 // 8 x 22016 x 4096 (32) 27.0 / 19.7; 1 x 32000 x 4096 (eight) 22.3 / 24.6.
 inline bool few_fused(int64_t m, int64_t n, int64_t k, int sms) {
-  const int64_t blocks = (k + kFp8Block - 1) / kFp8Block, c = few_cluster(n, blocks, 2, sms);
+  const int64_t blocks = (k + kFp8Block - 1) / kFp8Block, c = few_cluster(m, n, blocks, sms);
   return m <= 8 && (m + 1) / 2 * ((blocks + c - 1) / c) <= 40;
 }
 sp_status launch_fp8_few(const sp_fp8_linear_args& a, const Fp8Rows* rows, const CUtensorMap& map_w, const CUtensorMap& map_x,

@@ -2,7 +2,7 @@
 //
 // Bound by reading W once. A tile is 128 rows of W (the lanes of tensor memory) by MT tokens (its columns), so that
 // W is the tensor cores' first operand and few tokens waste no time there. The blocks of a tile's rows are shared by the
-// CTAs of a cluster, as many as fill the machine; each holds a hundred kilobytes of W in flight, two of them on an SM, and
+// CTAs of a cluster, as many as fill the machine; each holds up to ninety kilobytes of W in flight, two of them on an SM, and
 // their sums meet through the cluster's shared memory, in order. Nothing goes through global memory but
 // W, x and y:
 //   producer    W's tiles by TMA into a ring, asked into L2 before the launch before this one has ended; of quantised x its
@@ -14,7 +14,7 @@
 //   epilogue    four warps, thread = row of W: the block's sums times sx * sw, added up in registers
 //
 // Measured, us and W's rate: 1 x 4096 x 4096 5.9 (2.8 TB/s: the launch, the first blocks' way in, the cluster's two barriers), 1 x 32000 x 4096
-// 22.3 (5.9 TB/s), 16 x 32000 x 4096 23.8 with the launch that quantises (131.2 MB from memory), 64 x 32000 x 4096 34.6. With partial sums
+// 22.3 (5.9 TB/s), 16 x 32000 x 4096 23.8 with the launch that quantises (131.2 MB from memory), 64 x 32000 x 4096 26.9 (33.4 with one CTA of eight stages to an SM). With partial sums
 // through the workspace and x quantised by a launch before, the first two took 13.7 and 28.
 #include <cuda.h>
 #include <cudaTypedefs.h>
@@ -29,16 +29,15 @@ namespace {
 constexpr int kTileN = 128;
 constexpr uint32_t kWBytes = kTileN * 128;
 // warps: epilogue 0-3, producer 4, products 5, quantisers 6-9
-constexpr int kMostStages = 8;
+constexpr int kMostStages = 5;
 constexpr int kFewCluster = 8;  // (few_cluster)
 constexpr uint32_t kCtl = 512;
 
 template <int MT, bool FUSED>
 struct FewPlan {
   static constexpr int kThreads = FUSED ? 320 : 192;
-  static constexpr int kCtas = MT <= 32 ? 2 : 1;  // on an SM
-  static constexpr int kStages = MT <= 32 ? 5 : 8;
-  static constexpr uint32_t kTmem = MT == 16 ? 128 : MT == 32 ? 256 : 512;
+  static constexpr int kStages = MT <= 32 ? 5 : 4;
+  static constexpr uint32_t kTmem = MT == 16 ? 128 : 256;
   static constexpr uint32_t kStage = kWBytes + MT * 128;
   static constexpr uint32_t kScales = (kStages * MT * 4 + 511) / 512 * 512;
   static constexpr uint32_t kSmem = 1024 + kCtl + kScales + 512 + kStages * kStage;  // (1024: alignment)
@@ -58,7 +57,7 @@ struct FewParams {
 };
 
 template <int MT, bool FUSED>
-__global__ void __launch_bounds__(FewPlan<MT, FUSED>::kThreads, FewPlan<MT, FUSED>::kCtas)
+__global__ void __launch_bounds__(FewPlan<MT, FUSED>::kThreads, kFewCtas)
     fp8_few_kernel(const __grid_constant__ FewParams p, const __grid_constant__ CUtensorMap tmap_w,
                    const __grid_constant__ CUtensorMap tmap_x) {
   using P = FewPlan<MT, FUSED>;
@@ -316,7 +315,7 @@ sp_status launch(FewParams p, const CUtensorMap& map_w, const CUtensorMap& map_x
     return SP_ERR_CUDA;
   }
   const int64_t tiles = (p.n + kTileN - 1) / kTileN;
-  p.cluster = few_cluster(p.n, p.blocks, P::kCtas, sms);
+  p.cluster = few_cluster(p.m, p.n, p.blocks, sms);
   if (tiles * p.cluster > INT32_MAX) return SP_ERR_UNSUPPORTED;
   return launch_pdl(fp8_few_kernel<MT, FUSED>, dim3((unsigned)(tiles * p.cluster)), P::kThreads, P::kSmem, p.cluster, stream, p,
                     map_w, map_x);
