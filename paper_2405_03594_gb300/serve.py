@@ -347,7 +347,7 @@ def token_probs(logits: torch.Tensor, temperature=1.0, min_p: float = 0.0, out: 
                 stream=None) -> torch.Tensor:
     """sp_token_probs: probabilities, float32 [T, V], of the rows of logits [T, V] (bf16 or float32, rows of unit
     stride).  temperature: a number, or one for each row (float32 [T]); 0 or less takes the best entry.
-    min_p: entries of less than min_p times the best one's probability are left out."""
+    min_p: entries of less than min_p times the best one's probability are left out.  out must not overlap logits."""
     dev = _on_current(logits.get_device(), logits, "logits")
     kind = _row_type(logits, dev, "logits")
     t, v = logits.shape
