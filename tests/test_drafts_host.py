@@ -46,11 +46,12 @@ def test_retract_refusals(sp):
 
 
 def test_probs_refusals(sp):
-    def call(logits=FAKE, dtype=0, stride=100, tokens=2, vocab=100, temperature=None, one=1.0, min_p=0.0, out=FAKE, out_stride=100):
+    def call(logits=FAKE, dtype=0, stride=100, tokens=2, vocab=100, temperature=None, one=1.0, min_p=0.0, out=2 * FAKE, out_stride=100):
         return sp._lib.sp_token_probs(logits, dtype, stride, tokens, vocab, temperature, one, min_p, out, out_stride, None)
 
     for kw in (dict(dtype=2), dict(tokens=-1), dict(vocab=0), dict(stride=99), dict(out_stride=99), dict(min_p=-0.1),
-               dict(min_p=1.1), dict(min_p=math.nan), dict(one=math.nan), dict(logits=None), dict(out=None)):
+               dict(min_p=1.1), dict(min_p=math.nan), dict(one=math.nan), dict(logits=None), dict(out=None),
+               dict(out=FAKE), dict(out=FAKE + 396), dict(out=FAKE - 796), dict(dtype=1, out=FAKE + 796)):
         assert call(**kw) == 1, kw
     assert call(vocab=1 << 31, stride=1 << 31, out_stride=1 << 31) == 2
     for kw in (dict(logits=FAKE + 1), dict(logits=FAKE + 2, dtype=1), dict(out=FAKE + 2), dict(temperature=FAKE + 2)):
