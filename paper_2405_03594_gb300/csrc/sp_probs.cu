@@ -177,8 +177,8 @@ __global__ void __launch_bounds__(kPrThreads, 4) probs_kernel(const __grid_const
         at = min(at, __float_as_uint(ld_cluster_f32(cluster_map(smem_u32(&sh.cta_at), (uint32_t)r))));
       leave();
     }
-    // (a NaN, as a logit or as the temperature, makes the row NaN)
-    const bool sound = best == best && t == t;
+    // (a NaN, as a logit or as the temperature, makes the row NaN, and so does nothing above -inf: there is no best entry)
+    const bool sound = best > -INFINITY && t == t;
     const float nothing = sound ? 0.f : __uint_as_float(0x7fffffffu);
     for (int c = c0 + tid; c < c1; c += kPrThreads) {
       float v[N];

@@ -57,6 +57,8 @@ def probs(x, temperature, min_p):
             t, best = f32(temperature[r]), x[r].max()
             if np.isnan(t) or np.isnan(best):
                 out[r] = np.nan
+            elif best == -np.inf:  # nothing is open
+                out[r] = np.nan
             elif not t > 0:
                 out[r, np.argmax(x[r])] = 1
             else:
