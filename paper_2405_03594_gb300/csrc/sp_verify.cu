@@ -356,8 +356,13 @@ extern "C" sp_status sp_verify_drafts(const sp_verify_args* a, void* stream) {
   if (!a->cu_q || !a->drafts || !a->sample || !a->accepted || !a->rejected || !a->next ||
       (a->rows > 0 && (!a->probs || !a->ids || !a->accept)))
     return SP_ERR_INVALID_ARG;
-  auto off = [](const void* p, int32_t dtype) { return reinterpret_cast<uintptr_t>(p) % (dtype == SP_LOGITS_BF16 ? 2 : 4) != 0; };
-  if (off(a->probs, a->dtype) || off(a->draft_probs, a->draft_dtype)) return SP_ERR_ALIGNMENT;
+  auto off = [](const void* p, int size) { return reinterpret_cast<uintptr_t>(p) % size != 0; };
+  if (off(a->probs, a->dtype == SP_LOGITS_BF16 ? 2 : 4) || off(a->draft_probs, a->draft_dtype == SP_LOGITS_BF16 ? 2 : 4))
+    return SP_ERR_ALIGNMENT;
+  if (off(a->ids, 8) || off(a->next, 8)) return SP_ERR_ALIGNMENT;
+  for (const void* p : {(const void*)a->cu_q, (const void*)a->drafts, (const void*)a->accept, (const void*)a->sample,
+                        (const void*)a->accepted, (const void*)a->rejected})
+    if (off(p, 4)) return SP_ERR_ALIGNMENT;
   const int sms = current_sms();
   if (sms == 0) return SP_ERR_CUDA;
   int cluster = 1;
