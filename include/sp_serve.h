@@ -112,7 +112,7 @@ typedef struct sp_kv_retract_args {
  * drop below 0 or above the length, or more pages than there are: nothing changes, and SP_PLAN_INPUT is added to
  * *status, which else stays what the step's plan made it.  Unless it writes over its own inputs, the call can be repeated.  SP_ERR_INVALID_ARG for a
  * null pointer (but free_pages, with free_count, next_count and table), a negative size, a page size that is no power
- * of two.  requests == 0 is allowed.  One launch. */
+ * of two; SP_ERR_ALIGNMENT for an address off 4 bytes.  requests == 0 is allowed.  One launch. */
 sp_status sp_kv_retract(const sp_kv_retract_args* args, void* stream);
 
 /* Per-head norms of queries and keys with the position rotation, in one pass; keys and values go to

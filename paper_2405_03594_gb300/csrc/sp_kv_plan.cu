@@ -378,6 +378,9 @@ extern "C" sp_status sp_kv_retract(const sp_kv_retract_args* a, void* stream) {
   if (!a->status || (a->requests > 0 && (!a->cached || !a->drop || !a->lens))) return SP_ERR_INVALID_ARG;
   if (a->free_pages && (!a->free_count || !a->next_count || (a->requests > 0 && !a->table))) return SP_ERR_INVALID_ARG;
   if (a->pages > INT_MAX || a->requests > INT_MAX / 4) return SP_ERR_UNSUPPORTED;
+  auto off = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 != 0; };
+  if (off(a->cached) || off(a->drop) || off(a->lens) || off(a->status)) return SP_ERR_ALIGNMENT;
+  if (a->free_pages && (off(a->free_pages) || off(a->free_count) || off(a->next_count) || off(a->table))) return SP_ERR_ALIGNMENT;
   return launch_pdl(retract_kernel, dim3(1), kPlanThreads, 0, 1, (cudaStream_t)stream, *a, page_shift(a->page_size));
 }
 

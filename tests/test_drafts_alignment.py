@@ -31,3 +31,15 @@ def test_verification_refuses_addresses_off_their_entries(sp, name):
             assert sp._lib.sp_verify_drafts(a, None) == 3, (off, rows)
             a.requests = 0
             assert sp._lib.sp_verify_drafts(a, None) == 0
+
+
+RETRACT = ("cached", "drop", "table", "free_pages", "free_count", "next_count", "lens", "status")
+
+
+@pytest.mark.parametrize("name", RETRACT)
+@pytest.mark.parametrize("requests", [2, 0])
+def test_taking_tokens_back_refuses_addresses_off_their_entries(sp, name, requests):
+    for off in (1, 2, 3):
+        a = _filled(sp.SpKvRetractArgs(), RETRACT, pages=4, requests=requests, width=2, page_size=16)
+        setattr(a, name, FAKE + off)
+        assert sp._lib.sp_kv_retract(a, None) == 3, off
