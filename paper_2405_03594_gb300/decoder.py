@@ -106,7 +106,9 @@ class Decoder:
     def sample(self, ids: torch.Tensor, new: torch.Tensor, max_new: int, sample: torch.Tensor, temperature=1.0, min_p: float = 0.0):
         """step(), then a token for each request behind its last one, drawn by `sample` (float32 [requests] in [0, 1)) from
         the probabilities at that temperature (token_probs): (next ids [requests], -1 for a request without new tokens;
-        probabilities [t, V], float32)."""
+        probabilities [t, V], float32).  temperature: a number, or one for each of the step's tokens (float32 [t], as the ids
+        lie); of one for each request, float32 [requests], those are
+        torch.repeat_interleave(temperature, new.clamp(min=0), output_size=t)."""
         probs = token_probs(self.step(ids, new, max_new), temperature, min_p)
         t, b = ids.shape[0], self.batch
         none = torch.zeros(b.requests, dtype=torch.int32, device=self.h.device)
@@ -118,7 +120,8 @@ class Decoder:
         """step(), where the last drafts[b] (int32 [requests]) of a request's new tokens are drafted ones: keeps the run of them
         that the model's probabilities accept (verify_drafts: accept float32 [t], sample float32 [requests], draft_probs [t, V]
         with row j what token j + 1 was drawn from), takes the others back out of the cache's tables, and draws the token
-        behind.  A request's first new token is the one drawn before.  Returns (accepted, rejected int32 [requests], next ids [requests])."""
+        behind.  A request's first new token is the one drawn before.  temperature: as for sample().  Returns (accepted, rejected
+        int32 [requests], next ids [requests])."""
         probs = token_probs(self.step(ids, new, max_new), temperature, min_p)
         accepted, rejected, nxt = verify_drafts(probs, ids.long(), self.batch.cu_q, drafts, accept, sample, draft_probs)
         self.batch.retract(rejected, advance=True)

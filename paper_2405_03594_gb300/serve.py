@@ -346,7 +346,7 @@ def _row_type(x: torch.Tensor, dev: int, name: str) -> int:
 def token_probs(logits: torch.Tensor, temperature=1.0, min_p: float = 0.0, out: torch.Tensor | None = None,
                 stream=None) -> torch.Tensor:
     """sp_token_probs: probabilities, float32 [T, V], of the rows of logits [T, V] (bf16 or float32, rows of unit
-    stride).  temperature: a number, or one for each row (float32 [T]); 0 or less takes the best entry.
+    stride).  temperature: a number, or one for each row (float32 [T], neither more nor fewer); 0 or less takes the best entry.
     min_p: entries of less than min_p times the best one's probability are left out.  out must not overlap logits."""
     dev = _on_current(logits.get_device(), logits, "logits")
     kind = _row_type(logits, dev, "logits")
@@ -354,6 +354,8 @@ def token_probs(logits: torch.Tensor, temperature=1.0, min_p: float = 0.0, out: 
     if v < 1:
         raise ValueError("logits: a vocabulary of one entry or more wanted")
     if isinstance(temperature, torch.Tensor):
+        if temperature.shape != (t,):  # (a longer one would be the requests', or another step's)
+            raise ValueError(f"temperature: a number, or float32 [{t}], one for each row, wanted, got {list(temperature.shape)}")
         per_row, one = _index(temperature, t, _F32, dev, "temperature"), 1.0
     else:
         per_row, one = 0, float(temperature)
