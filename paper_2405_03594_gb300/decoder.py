@@ -24,7 +24,7 @@ import torch
 
 from . import sp
 from .fp8 import Fp8Matrix
-from .serve import Batch, KvCache, token_logprobs, token_probs, verify_drafts
+from .serve import Batch, KvCache, check_drawing, token_logprobs, token_probs, verify_drafts
 
 NAMES = ("qkv", "o", "gate_up", "down")
 
@@ -108,9 +108,11 @@ class Decoder:
         the probabilities at that temperature (token_probs): (next ids [requests], -1 for a request without new tokens;
         probabilities [t, V], float32).  temperature: a number, or one for each of the step's tokens (float32 [t], as the ids
         lie); of one for each request, float32 [requests], those are
-        torch.repeat_interleave(temperature, new.clamp(min=0), output_size=t)."""
+        torch.repeat_interleave(temperature, new.clamp(min=0), output_size=t).  Arguments that cannot be are refused
+        before anything changes, as step() refuses ids."""
+        t, b = ids.numel(), self.batch
+        check_drawing(t, self.head.n, b.requests, b._gpu, sample, temperature, min_p)
         probs = token_probs(self.step(ids, new, max_new), temperature, min_p)
-        t, b = ids.shape[0], self.batch
         none = torch.zeros(b.requests, dtype=torch.int32, device=self.h.device)
         nxt = verify_drafts(probs, ids.long(), b.cu_q, none, torch.empty(t, device=self.h.device), sample)[2]
         return nxt, probs
@@ -122,6 +124,7 @@ class Decoder:
         with row j what token j + 1 was drawn from), takes the others back out of the cache's tables, and draws the token
         behind.  A request's first new token is the one drawn before.  temperature: as for sample().  Returns (accepted, rejected
         int32 [requests], next ids [requests])."""
+        check_drawing(ids.numel(), self.head.n, self.batch.requests, self.batch._gpu, sample, temperature, min_p, drafts, accept, draft_probs)
         probs = token_probs(self.step(ids, new, max_new), temperature, min_p)
         accepted, rejected, nxt = verify_drafts(probs, ids.long(), self.batch.cu_q, drafts, accept, sample, draft_probs)
         self.batch.retract(rejected, advance=True)

@@ -24,9 +24,10 @@ import struct
 import torch
 
 from . import sp
-from .sp import SpAttendArgs, SpKv4, SpKvPlanArgs, SpKvRetractArgs, SpRopeArgs, SpVerifyArgs, _check, _lib, _stream
+from .sp import SP_ERR_INVALID_ARG, SP_ERR_UNSUPPORTED, SpAttendArgs, SpKv4, SpKvPlanArgs, SpKvRetractArgs, SpRopeArgs, SpVerifyArgs, _check, _lib, _stream
 
 PLAN_PAGES, PLAN_WIDTH, PLAN_TOKENS, PLAN_INPUT = 1, 2, 4, 8  # SP_PLAN_*
+MOST_DRAWN = 1 << 22  # entries of a row that sp_verify_drafts draws from
 
 _BF16, _F32, _I32, _I64 = torch.bfloat16, torch.float32, torch.int32, torch.int64
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
@@ -343,6 +344,15 @@ def _row_type(x: torch.Tensor, dev: int, name: str) -> int:
     return 0 if dtype is _BF16 else 1
 
 
+def _row_temperatures(temperature, t: int, dev: int) -> tuple[int, float]:
+    """The address of a vector of t temperatures, or 0, and the number for all rows."""
+    if not isinstance(temperature, torch.Tensor):
+        return 0, float(temperature)
+    if temperature.shape != (t,):  # (a longer one would be the requests', or another step's)
+        raise ValueError(f"temperature: a number, or float32 [{t}], one for each row, wanted, got {list(temperature.shape)}")
+    return _index(temperature, t, _F32, dev, "temperature"), 1.0
+
+
 def token_probs(logits: torch.Tensor, temperature=1.0, min_p: float = 0.0, out: torch.Tensor | None = None,
                 stream=None) -> torch.Tensor:
     """sp_token_probs: probabilities, float32 [T, V], of the rows of logits [T, V] (bf16 or float32, rows of unit
@@ -353,12 +363,7 @@ def token_probs(logits: torch.Tensor, temperature=1.0, min_p: float = 0.0, out: 
     t, v = logits.shape
     if v < 1:
         raise ValueError("logits: a vocabulary of one entry or more wanted")
-    if isinstance(temperature, torch.Tensor):
-        if temperature.shape != (t,):  # (a longer one would be the requests', or another step's)
-            raise ValueError(f"temperature: a number, or float32 [{t}], one for each row, wanted, got {list(temperature.shape)}")
-        per_row, one = _index(temperature, t, _F32, dev, "temperature"), 1.0
-    else:
-        per_row, one = 0, float(temperature)
+    per_row, one = _row_temperatures(temperature, t, dev)
     if out is None:
         out, out_stride = torch.empty((t, v), dtype=_F32, device=logits.device), v
     elif _row_type(out, dev, "out") != 1 or out.shape != logits.shape:
@@ -369,6 +374,34 @@ def token_probs(logits: torch.Tensor, temperature=1.0, min_p: float = 0.0, out: 
                                out.data_ptr(), out_stride, _stream(stream, dev)),
            "sp_token_probs")
     return out
+
+
+def _draft_rows(draft_probs: torch.Tensor | None, t: int, v: int, dev: int) -> tuple[int, int, int]:
+    """Address, row stride and type of the drafts' probabilities [t, v]; zeros where drafts are certain."""
+    if draft_probs is None:
+        return 0, 0, 0
+    kind = _row_type(draft_probs, dev, "draft_probs")
+    if draft_probs.shape != (t, v):
+        raise ValueError(f"draft_probs: {[t, v]} wanted")
+    return draft_probs.data_ptr(), draft_probs.stride(0) if t > 1 else v, kind
+
+
+def check_drawing(t: int, v: int, requests: int, dev: int, sample: torch.Tensor, temperature, min_p: float,
+                  drafts: torch.Tensor | None = None, accept: torch.Tensor | None = None, draft_probs: torch.Tensor | None = None):
+    """Refuses the arguments that token_probs and verify_drafts would refuse for a step of t rows over v entries: what
+    changes tables before it has its logits asks first."""
+    _, one = _row_temperatures(temperature, t, dev)
+    if one != one or not 0 <= min_p <= 1:
+        _check(SP_ERR_INVALID_ARG, "sp_token_probs")
+    _index(sample, requests, _F32, dev, "sample")
+    if drafts is not None or accept is not None:
+        _index(drafts, requests, _I32, dev, "drafts")
+        _index(accept, t, _F32, dev, "accept")
+        draft, stride, _ = _draft_rows(draft_probs, t, v, dev)
+        if draft and stride < v:
+            _check(SP_ERR_INVALID_ARG, "sp_verify_drafts")
+    if v > MOST_DRAWN:
+        _check(SP_ERR_UNSUPPORTED, "sp_verify_drafts")
 
 
 def verify_drafts(probs: torch.Tensor, ids: torch.Tensor, cu_q: torch.Tensor, drafts: torch.Tensor, accept: torch.Tensor,
@@ -385,12 +418,7 @@ def verify_drafts(probs: torch.Tensor, ids: torch.Tensor, cu_q: torch.Tensor, dr
     b = cu_q.shape[0] - 1 if cu_q.dim() == 1 else -1
     if b < 0:
         raise ValueError("cu_q: int32 [requests + 1] wanted")
-    draft_kind = draft_stride = draft = 0
-    if draft_probs is not None:
-        draft_kind = _row_type(draft_probs, dev, "draft_probs")
-        if draft_probs.shape != probs.shape:
-            raise ValueError(f"draft_probs: {[t, v]} wanted")
-        draft, draft_stride = draft_probs.data_ptr(), draft_probs.stride(0) if t > 1 else v
+    draft, draft_stride, draft_kind = _draft_rows(draft_probs, t, v, dev)
     where = (_index(ids, t, _I64, dev, "ids"), _index(cu_q, b + 1, _I32, dev, "cu_q"), _index(drafts, b, _I32, dev, "drafts"),
              _index(accept, t, _F32, dev, "accept"), _index(sample, b, _F32, dev, "sample"))
     device = probs.device

@@ -24,7 +24,7 @@ STATUS = {
     0: "SP_OK", 1: "SP_ERR_INVALID_ARG", 2: "SP_ERR_UNSUPPORTED", 3: "SP_ERR_ALIGNMENT", 4: "SP_ERR_CUDA",
     5: "SP_ERR_OUT_OF_MEMORY", 6: "SP_ERR_TIMEOUT", 7: "SP_ERR_BAD_HANDLE", 8: "SP_ERR_WORKSPACE",
 }
-SP_ERR_UNSUPPORTED = 2
+SP_ERR_INVALID_ARG, SP_ERR_UNSUPPORTED = 1, 2
 # every function declared in include/sp.h, include/sp_stack.h, include/sp_serve.h and include/sp_fp8.h
 EXPORTS = ["sp_compress", "sp_decompress", "sp_workspace_size", "sp_linear", "sp_linear_ex", "sp_launch_count",
            "sp_kernel_family",
