@@ -114,7 +114,7 @@ class Decoder:
         check_drawing(t, self.head.n, b.requests, b._gpu, sample, temperature, min_p)
         probs = token_probs(self.step(ids, new, max_new), temperature, min_p)
         none = torch.zeros(b.requests, dtype=torch.int32, device=self.h.device)
-        nxt = verify_drafts(probs, ids.long(), b.cu_q, none, torch.empty(t, device=self.h.device), sample)[2]
+        nxt = verify_drafts(probs, ids.long(), b.cu_q[:b.requests + 1], none, torch.empty(t, device=self.h.device), sample)[2]
         return nxt, probs
 
     def verify(self, ids: torch.Tensor, new: torch.Tensor, max_new: int, drafts: torch.Tensor, accept: torch.Tensor,
@@ -124,10 +124,11 @@ class Decoder:
         with row j what token j + 1 was drawn from), takes the others back out of the cache's tables, and draws the token
         behind.  A request's first new token is the one drawn before.  temperature: as for sample().  Returns (accepted, rejected
         int32 [requests], next ids [requests])."""
-        check_drawing(ids.numel(), self.head.n, self.batch.requests, self.batch._gpu, sample, temperature, min_p, drafts, accept, draft_probs)
+        b = self.batch
+        check_drawing(ids.numel(), self.head.n, b.requests, b._gpu, sample, temperature, min_p, drafts, accept, draft_probs)
         probs = token_probs(self.step(ids, new, max_new), temperature, min_p)
-        accepted, rejected, nxt = verify_drafts(probs, ids.long(), self.batch.cu_q, drafts, accept, sample, draft_probs)
-        self.batch.retract(rejected, advance=True)
+        accepted, rejected, nxt = verify_drafts(probs, ids.long(), b.cu_q[:b.requests + 1], drafts, accept, sample, draft_probs)
+        b.retract(rejected, advance=True)
         return accepted, rejected, nxt
 
     def greedy(self, ids: torch.Tensor, new: torch.Tensor, max_new: int, top: int = 1):
