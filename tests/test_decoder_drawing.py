@@ -49,3 +49,13 @@ def test_a_batch_with_longer_tables(calls):
     d.batch.__dict__["cu_q"] = gpu(torch.zeros(2 * B + 5, dtype=torch.int32))
     _both(d, gpu(torch.zeros(T, dtype=torch.int64)))
     assert [a[2].shape[0] for a in seen] == [B + 1, B + 1]
+
+
+@pytest.mark.parametrize("dtype", [torch.int64, torch.int32])
+def test_ids_at_any_stride(calls, dtype):
+    """Ids that a step takes, such as a column of a table, are drawn behind as well."""
+    d, seen = calls
+    table = torch.arange(3 * T).view(T, 3).to(dtype)
+    _both(d, gpu(table)[:, 1])
+    for a in seen:
+        assert a[1].tolist() == list(range(1, 3 * T, 3))
