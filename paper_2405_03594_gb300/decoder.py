@@ -114,7 +114,8 @@ class Decoder:
         check_drawing(t, self.head.n, b.requests, b._gpu, sample, temperature, min_p)
         probs = token_probs(self.step(ids, new, max_new), temperature, min_p)
         none = torch.zeros(b.requests, dtype=torch.int32, device=self.h.device)
-        nxt = verify_drafts(probs, ids.long().contiguous(), b.cu_q[:b.requests + 1], none, torch.empty(t, device=self.h.device), sample)[2]
+        nxt = verify_drafts(probs, ids.long().contiguous(), b.cu_q[:b.requests + 1], none,
+                            torch.empty(t, dtype=torch.float32, device=self.h.device), sample)[2]
         return nxt, probs
 
     def verify(self, ids: torch.Tensor, new: torch.Tensor, max_new: int, drafts: torch.Tensor, accept: torch.Tensor,

@@ -17,7 +17,7 @@ def calls(monkeypatch):
     monkeypatch.setattr(serve, "_current_device", lambda: 0)
     monkeypatch.setattr(serve, "_stream", lambda *_: 0)
     monkeypatch.setattr(serve, "_verify", lambda *_: 0)
-    monkeypatch.setattr(decoder, "token_probs", lambda logits, *_: gpu(torch.zeros(logits.shape)))
+    monkeypatch.setattr(decoder, "token_probs", lambda logits, *_: gpu(torch.zeros(logits.shape, dtype=torch.float32)))
     seen = []
 
     def verify_drafts(*a):
@@ -59,3 +59,17 @@ def test_ids_at_any_stride(calls, dtype):
     _both(d, gpu(table)[:, 1])
     for a in seen:
         assert a[1].tolist() == list(range(1, 3 * T, 3))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float64])
+def test_under_another_default_type(calls, dtype):
+    """PyTorch's default type is the caller's own; the random numbers that nothing reads are float32 all the same."""
+    d, seen = calls
+    ids, new, w = gpu(torch.zeros(T, dtype=torch.int64)), gpu(torch.tensor([3, 2], dtype=torch.int32)), gpu(torch.zeros(B))
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(dtype)
+    try:
+        d.sample(ids, new, 3, w)
+    finally:
+        torch.set_default_dtype(before)
+    assert seen[0][4].dtype == torch.float32 and seen[0][4].shape == (T,)

@@ -64,3 +64,27 @@ def test_a_temperature_for_each_request(model):  # noqa: F811
     for r, t in enumerate((0.0, 0.0, 1.5)):
         assert torch.equal(p[r:r + 1], serve.token_probs(dec.logits[r:r + 1], t))
     assert nxt[0] == dec.logits[1].float().argmax() and nxt[1] == -1 and 0 <= nxt[2] < VOCAB
+
+
+def test_ids_at_any_stride_longer_tables_and_another_default_type(model):  # noqa: F811
+    import torch
+
+    from paper_2405_03594_gb300 import sp
+
+    a, b = _decoder(model), _decoder(model)
+    b.batch.cu_q = torch.zeros(20, dtype=torch.int32, device="cuda")
+    b.batch.cached = torch.zeros(9, dtype=torch.int32, device="cuda")
+    ids, new = _ids(40), _i32([20, 13, 7])
+    w, u = torch.full((3,), 0.4, device="cuda"), torch.full((40,), 0.002, device="cuda")
+    column = torch.stack([ids, 0 * ids, ids], 1)[:, 2]
+    assert column.stride(0) == 3
+    for call in (lambda d, i: d.sample(i, new, 20, w, 0.8)[0], lambda d, i: torch.stack([x.long() for x in d.verify(i, new, 20, _i32([4, 2, 6]), u, w, None, 0.8)])):
+        want = call(a, ids)
+        torch.set_default_dtype(torch.bfloat16)
+        try:
+            got = call(b, column)
+        finally:
+            torch.set_default_dtype(torch.float32)
+        assert torch.equal(got, want)
+    sp.check()
+    assert a.batch.cached.tolist() == b.batch.cached.tolist()[:3]
