@@ -57,7 +57,7 @@ struct PairParams {
   int32_t m_tiles;
   int64_t items;         // tiles, or their shares
   int32_t split;         // shares of a tile (of its blocks)
-  int32_t y_tma;         // rows of y start at multiples of 16 bytes
+  int32_t y_tma;         // rows of y start and end at multiples of 16 bytes
   float* part;           // sums of the shares [items][2 CTAs][NT][128]
   int* cnt;              // their arrivals [tiles][2 CTAs]
   int* status;
@@ -479,7 +479,8 @@ sp_status launch_pair(const sp_fp8_linear_args& a, const Fp8Rows& rows, void* ws
   p.items = w.tiles * w.split;
   p.part = part;
   p.cnt = static_cast<int*>(ws);
-  p.y_tma = al16(a.y) && a.y_stride % 8 == 0;
+  // (a bulk store writes whole pieces of 16 bytes: a row that ended inside one would have up to seven columns beside it written)
+  p.y_tma = al16(a.y) && a.y_stride % 8 == 0 && a.n % 8 == 0;
   if (p.y_tma) {
     const cuuint64_t dim[2] = {(cuuint64_t)a.n, (cuuint64_t)a.m}, strides[1] = {(cuuint64_t)a.y_stride * 2};
     const cuuint32_t box[2] = {(cuuint32_t)PairPlan<NT>::kOut, 32}, estride[2] = {1, 1};
