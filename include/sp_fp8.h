@@ -58,8 +58,19 @@ typedef struct sp_fp8_linear_args {
  * repeatable for given sizes and device, and the same whether x or xq is given.  SP_ERR_INVALID_ARG for a null pointer, a
  * negative size, n or k of 0, a stride that is too small, both or neither of x and xq; SP_ERR_UNSUPPORTED for sizes above
  * 2^30, strides of codes that are no multiple of 16, or more than 64 rows on a device that holds no pair of CTAs; SP_ERR_ALIGNMENT for codes, x_scale or the workspace off a
- * 16-byte boundary, or bf16 off its own size.  m == 0 returns SP_OK.  One launch, or two. */
+ * 16-byte boundary, or bf16 off its own size.  m == 0 returns SP_OK.  One launch, or two.  Of a launch that sp_check reports as
+ * SP_ERR_TIMEOUT no result is to be used; the workspace is ready for the next call. */
 sp_status sp_fp8_linear(const sp_fp8_linear_args* args, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* Failure-path test (nothing calls it in normal use).  sp_fp8_linear, with warp `warp` of CTA `cta` of the product's kernel waiting,
+ * before the one that it counts as `block` of its blocks of 128 columns, on a shared-memory barrier that nothing completes, and every
+ * wait bounded by wait_ms milliseconds.  The warp gives up and records SP_ERR_TIMEOUT, as any whose wait expires, with the copies
+ * and products before that block on their way; y is written within its bounds, with numbers that are worth nothing.
+ * The launch ends by itself, and the workspace is ready for the next call.  A cta, warp or block that the kernel does not have
+ * gives up nothing.  wait_ms in 1..10000, the others not negative (SP_ERR_INVALID_ARG otherwise); compiled for up to 16 rows, and for
+ * more than 64 where a tile has 128 rows of W (SP_ERR_UNSUPPORTED otherwise, with nothing launched), as variants of the kernels of their own. */
+sp_status sp_test_expired_fp8(const sp_fp8_linear_args* args, void* workspace_dev, size_t workspace_bytes, int32_t cta,
+                              int32_t warp, int32_t block, uint32_t wait_ms, void* stream);
 
 /* Workspace bytes of sp_fp8_linear on the current device for m rows.  Host only. */
 sp_status sp_fp8_workspace_size(int64_t m, int64_t n, int64_t k, size_t* bytes);

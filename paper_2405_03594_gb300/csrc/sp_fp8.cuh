@@ -147,6 +147,21 @@ struct Fp8Rows {
   int64_t stride, scale_stride;
 };
 
+// What sp_test_expired_fp8 makes expire: the waits of a warp of a CTA, from its block `block` on.
+struct Fp8Expire {
+  int32_t cta, warp, block;
+  uint64_t wait_ns;
+};
+
+// In the variants of sp_test_expired_fp8: whether this warp gives up before its block b.  (p: a kernel's parameters)
+template <bool kExpire, typename P>
+__device__ __forceinline__ bool gives_up(const P& p, int b, uint64_t* never) {
+  if constexpr (kExpire)
+    return b == p.expire_block && (int)blockIdx.x == p.expire_cta && (int)(threadIdx.x >> 5) == p.expire_warp && !mbar_wait(never, 0, p.timeout_ns);
+  else
+    return false;
+}
+
 // fp8_few_kernel: up to kFewTokens rows.
 constexpr int kFewTokens = 64;
 inline int few_box(int64_t m) { return m <= 16 ? 16 : m <= 32 ? 32 : 64; }  // rows of x in a tile, of map_x's box
@@ -170,8 +185,9 @@ inline bool few_fused(int64_t m, int64_t n, int64_t k, int sms) {
   const int64_t blocks = (k + kFp8Block - 1) / kFp8Block, c = few_cluster(m, n, blocks, sms);
   return m <= 8 && (m + 1) / 2 * ((blocks + c - 1) / c) <= 40;
 }
+// expire: the variant of sp_test_expired_fp8, for up to 16 rows.
 sp_status launch_fp8_few(const sp_fp8_linear_args& a, const Fp8Rows* rows, const CUtensorMap& map_w, const CUtensorMap& map_x,
-                         int sms, cudaStream_t stream);
+                         int sms, const Fp8Expire* expire, cudaStream_t stream);
 
 sp_status launch_fp8_quantize_rows(const uint16_t* x, int64_t x_stride, int64_t m, int64_t k, uint8_t* codes,
                                    int64_t stride, float* scale, int64_t scale_stride, cudaStream_t stream);

@@ -54,9 +54,12 @@ struct FewParams {
   int32_t wide;  // rows of x start at multiples of 16 bytes
   int* status;
   uint64_t timeout_ns;
+  int32_t expire_cta, expire_warp, expire_block;  // in the variants of sp_test_expired_fp8
 };
 
-template <int MT, bool FUSED>
+// kExpire: a variant for sp_test_expired_fp8, whose warp p.expire_warp of CTA p.expire_cta waits, before its block p.expire_block, for
+// what never comes, and gives up.
+template <int MT, bool FUSED, bool kExpire = false>
 __global__ void __launch_bounds__(FewPlan<MT, FUSED>::kThreads, kFewCtas)
     fp8_few_kernel(const __grid_constant__ FewParams p, const __grid_constant__ CUtensorMap tmap_w,
                    const __grid_constant__ CUtensorMap tmap_x) {
@@ -71,6 +74,7 @@ __global__ void __launch_bounds__(FewPlan<MT, FUSED>::kThreads, kFewCtas)
   uint64_t* freed = done + kMostStages;                  // and taken out
   uint64_t* drain = freed + kMostStages;                 // no product is under way
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  uint64_t* never = drain + 2;                           // (kExpire) nothing completes it
   float* scales = reinterpret_cast<float*>(smem + kCtl);  // [S][MT]
   uint8_t* ring = smem + (kCtl + P::kScales + 1023) / 1024 * 1024;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -85,6 +89,7 @@ __global__ void __launch_bounds__(FewPlan<MT, FUSED>::kThreads, kFewCtas)
       mbar_init(&freed[s], 4);
     }
     mbar_init(drain, 1);
+    if constexpr (kExpire) mbar_init(never, 1);
     fence_barrier_init();
   }
   if (warp == 5) {
@@ -112,7 +117,7 @@ __global__ void __launch_bounds__(FewPlan<MT, FUSED>::kThreads, kFewCtas)
       bool dead = false;
       int issued = 0;
       for (int b = b0; b < b1; ++b) {
-        if (!mbar_wait_short(&freed[s], ph ^ 1u, p.timeout_ns)) {
+        if (gives_up<kExpire>(p, b - b0, never) || !mbar_wait_short(&freed[s], ph ^ 1u, p.timeout_ns)) {
           dead = true;
           break;
         }
@@ -142,6 +147,7 @@ __global__ void __launch_bounds__(FewPlan<MT, FUSED>::kThreads, kFewCtas)
     uint32_t ph = 0;
     for (int b = b0; b < b1; ++b) {
       bool ok = mbar_wait_short(&w_full[s], ph, p.timeout_ns);
+      if constexpr (kExpire) ok = ok && !gives_up<kExpire>(p, b - b0, never);
       if constexpr (FUSED) ok = ok && mbar_wait_short(&x_full[s], ph, p.timeout_ns);
       if (!__all_sync(0xffffffffu, ok)) {
         if (lane == 0) set_status(p.status, kStatusTimeout);
@@ -181,7 +187,9 @@ __global__ void __launch_bounds__(FewPlan<MT, FUSED>::kThreads, kFewCtas)
     uint32_t ph = 0;
     uint4 next = ask(u);
     for (int b = b0; b < b1; ++b) {
-      if (!__all_sync(0xffffffffu, mbar_wait_short(&freed[s], ph ^ 1u, p.timeout_ns))) {
+      bool ok = mbar_wait_short(&freed[s], ph ^ 1u, p.timeout_ns);
+      if constexpr (kExpire) ok = ok && !gives_up<kExpire>(p, b - b0, never);
+      if (!__all_sync(0xffffffffu, ok)) {
         if (lane == 0) set_status(p.status, kStatusTimeout);
         break;
       }
@@ -224,6 +232,7 @@ __global__ void __launch_bounds__(FewPlan<MT, FUSED>::kThreads, kFewCtas)
     for (int b = b0; b < b1; ++b) {
       const float next = b + 1 < b1 ? __ldg(sw + b + 1) : 0.f;
       bool ok = mbar_wait_short(&done[s], ph, p.timeout_ns);
+      if constexpr (kExpire) ok = ok && !gives_up<kExpire>(p, b - b0, never);
       ok = ok && mbar_wait_short(FUSED ? &x_full[s] : &w_full[s], ph, p.timeout_ns);  // (complete: for the scales)
       if (!__all_sync(0xffffffffu, ok)) {
         if (lane == 0) set_status(p.status, kStatusTimeout);
@@ -307,24 +316,24 @@ __global__ void __launch_bounds__(FewPlan<MT, FUSED>::kThreads, kFewCtas)
   }
 }
 
-template <int MT, bool FUSED>
+template <int MT, bool FUSED, bool kExpire = false>
 sp_status launch(FewParams p, const CUtensorMap& map_w, const CUtensorMap& map_x, int sms, cudaStream_t stream) {
   using P = FewPlan<MT, FUSED>;
-  if (cudaFuncSetAttribute(fp8_few_kernel<MT, FUSED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)P::kSmem) != cudaSuccess) {
+  if (cudaFuncSetAttribute(fp8_few_kernel<MT, FUSED, kExpire>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)P::kSmem) != cudaSuccess) {
     cudaGetLastError();
     return SP_ERR_CUDA;
   }
   const int64_t tiles = (p.n + kTileN - 1) / kTileN;
   p.cluster = few_cluster(p.m, p.n, p.blocks, sms);
   if (tiles * p.cluster > INT32_MAX) return SP_ERR_UNSUPPORTED;
-  return launch_pdl(fp8_few_kernel<MT, FUSED>, dim3((unsigned)(tiles * p.cluster)), P::kThreads, P::kSmem, p.cluster, stream, p,
+  return launch_pdl(fp8_few_kernel<MT, FUSED, kExpire>, dim3((unsigned)(tiles * p.cluster)), P::kThreads, P::kSmem, p.cluster, stream, p,
                     map_w, map_x);
 }
 
 }  // namespace
 
 sp_status launch_fp8_few(const sp_fp8_linear_args& a, const Fp8Rows* rows, const CUtensorMap& map_w, const CUtensorMap& map_x,
-                         int sms, cudaStream_t stream) {
+                         int sms, const Fp8Expire* expire, cudaStream_t stream) {
   FewParams p = {};
   p.w_scale = a.w_scale;
   p.x = static_cast<const uint16_t*>(a.x);
@@ -340,6 +349,12 @@ sp_status launch_fp8_few(const sp_fp8_linear_args& a, const Fp8Rows* rows, const
   p.wide = al16(a.x) && (a.m == 1 || a.x_stride % 8 == 0);
   p.status = device_status_ptr();
   p.timeout_ns = wait_timeout_ns();
+  if (expire) {
+    p.timeout_ns = expire->wait_ns;
+    p.expire_cta = expire->cta, p.expire_warp = expire->warp, p.expire_block = expire->block;
+    if (few_box(a.m) != 16) return SP_ERR_UNSUPPORTED;
+    return rows ? launch<16, false, true>(p, map_w, map_x, sms, stream) : launch<16, true, true>(p, map_w, map_w, sms, stream);
+  }
   if (!rows) return launch<16, true>(p, map_w, map_w, sms, stream);
   return few_box(a.m) == 16   ? launch<16, false>(p, map_w, map_x, sms, stream)
          : few_box(a.m) == 32 ? launch<32, false>(p, map_w, map_x, sms, stream)

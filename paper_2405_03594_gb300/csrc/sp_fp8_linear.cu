@@ -62,6 +62,7 @@ struct PairParams {
   int* cnt;              // their arrivals [tiles][2 CTAs]
   int* status;
   uint64_t timeout_ns;
+  int32_t expire_cta, expire_warp, expire_block;  // in the variants of sp_test_expired_fp8
 };
 
 // Item i: its tile's place, and blocks [b0, b1).
@@ -76,7 +77,9 @@ __device__ __forceinline__ PairItem item_at(const PairParams& p, int64_t i) {
   return {tile % p.m_tiles, tile / p.m_tiles, (int)(part * p.blocks / p.split), (int)((part + 1) * p.blocks / p.split)};
 }
 
-template <int NT, bool SPLIT>
+// kExpire: a variant for sp_test_expired_fp8, whose warp p.expire_warp of CTA p.expire_cta waits, before its block p.expire_block, for
+// what never comes, and gives up.
+template <int NT, bool SPLIT, bool kExpire = false>
 __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
     fp8_pair_kernel(const __grid_constant__ PairParams p, const __grid_constant__ CUtensorMap tmap_w,
                     const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_y) {
@@ -114,6 +117,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
   cluster_sync_all();  // the peer's barriers are initialised
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  int count = 0;  // (kExpire) of the warp's blocks
 
   if (warp < 4) {
     registers_down<40>();
@@ -130,7 +134,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
         const PairItem it = item_at<SPLIT>(p, i);
         const int m0 = (int)(it.m_tile * kPairTokens + rank * 128), n0 = (int)(it.n_tile * NT + rank * (NT / 2));
         for (int b = it.b0; b < it.b1; ++b) {
-          if (!mbar_wait_short(&done[s], ph ^ 1u, p.timeout_ns)) {
+          if (gives_up<kExpire>(p, count++, never) || !mbar_wait_short(&done[s], ph ^ 1u, p.timeout_ns)) {
             dead = true;
             break;
           }
@@ -167,7 +171,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
         for (int b = it.b0; b < it.b1; ++b) {
           const int a = s % P::kAccs;
           bool ok = mbar_wait_short(&full[s], ph, p.timeout_ns);
-          ok = ok && mbar_wait_short(&d_empty[a], aph ^ 1u, p.timeout_ns);
+          ok = ok && mbar_wait_short(&d_empty[a], aph ^ 1u, p.timeout_ns) && !gives_up<kExpire>(p, count++, never);
           if (!__all_sync(0xffffffffu, ok)) {
             if (lane == 0) set_status(p.status, kStatusTimeout);
             dead = true;
@@ -236,6 +240,12 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
       for (int j = 0; j < C; ++j) acc[j] = 0.f;
       const int turn_at = kTwo ? (int)(kFp8Block - n0 % kFp8Block) : C;  // the first column of the second block
       auto block = [&](float sc1, float sc2) {
+        if constexpr (kExpire) {
+          if (!__all_sync(0xffffffffu, !gives_up<kExpire>(p, count++, never))) {
+            if (lane == 0) set_status(p.status, kStatusTimeout);
+            dead = true;
+          }
+        }
         if (!__all_sync(0xffffffffu, ready)) {
           // (behind a wait that has expired nothing waits, and what is read is worth nothing)
           if (!dead && !__all_sync(0xffffffffu, mbar_wait_short(&done[s], ph, p.timeout_ns))) {
@@ -428,6 +438,12 @@ PairWork pair_work(int nt, int64_t m, int64_t n, int64_t blocks, int64_t pairs) 
   return w;
 }
 
+// Rows of W in a tile: where the time is less.
+int pair_rows(int64_t m, int64_t n, int64_t k, int sms) {
+  auto clocks = [&](int nt) { return pair_work(nt, m, n, (k + kFp8Block - 1) / kFp8Block, sms / 2).clocks; };
+  return clocks(256) <= clocks(192) && clocks(256) <= clocks(128) ? 256 : clocks(192) <= clocks(128) ? 192 : 128;
+}
+
 // CTA pairs of fp8_pair_kernel that the device, which is current, holds at once; 0: none, or the lookup failed.
 template <int NT>
 int resident_pairs(int dev) {
@@ -449,10 +465,10 @@ int resident_pairs(int dev) {
   });
 }
 
-// SP_ERR_UNSUPPORTED, with nothing launched, where the device holds no pair.
+// SP_ERR_UNSUPPORTED where the device holds no pair.
 template <int NT>
 sp_status launch_pair(const sp_fp8_linear_args& a, const Fp8Rows& rows, void* ws, float* part, int sms,
-                      PFN_cuTensorMapEncodeTiled_v12000 encode, cudaStream_t stream) {
+                      PFN_cuTensorMapEncodeTiled_v12000 encode, const Fp8Expire* expire, cudaStream_t stream) {
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess) {
     cudaGetLastError();
@@ -490,7 +506,17 @@ sp_status launch_pair(const sp_fp8_linear_args& a, const Fp8Rows& rows, void* ws
   }
   p.status = device_status_ptr();
   p.timeout_ns = wait_timeout_ns();
-  return launch_pdl(w.split > 1 ? fp8_pair_kernel<NT, true> : fp8_pair_kernel<NT, false>,
+  auto kern = w.split > 1 ? fp8_pair_kernel<NT, true> : fp8_pair_kernel<NT, false>;
+  if (NT == 128 && expire) {
+    p.timeout_ns = expire->wait_ns;
+    p.expire_cta = expire->cta, p.expire_warp = expire->warp, p.expire_block = expire->block;
+    kern = w.split > 1 ? fp8_pair_kernel<128, true, true> : fp8_pair_kernel<128, false, true>;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairPlan<NT>::kSmem) != cudaSuccess) {
+      cudaGetLastError();
+      return SP_ERR_CUDA;
+    }
+  }
+  return launch_pdl(kern,
                     dim3((unsigned)(2 * std::min<int64_t>(pairs, p.items))), kPairThreads, PairPlan<NT>::kSmem, 1, stream, p, map_w, map_x, map_y);
 }
 
@@ -508,7 +534,9 @@ extern "C" sp_status sp_fp8_workspace_size(int64_t m, int64_t n, int64_t k, size
   return SP_OK;
 }
 
-extern "C" sp_status sp_fp8_linear(const sp_fp8_linear_args* a, void* ws, size_t ws_bytes, void* stream_) {
+namespace {
+
+sp_status linear(const sp_fp8_linear_args* a, void* ws, size_t ws_bytes, const Fp8Expire* expire, void* stream_) {
   if (!a || a->m < 0 || a->n < 1 || a->k < 1 || a->w_stride < a->k || !a->w || !a->w_scale || (a->x && a->xq))
     return SP_ERR_INVALID_ARG;
   if (a->m > 0 && (!a->y || a->y_stride < a->n || (!a->x && !a->xq))) return SP_ERR_INVALID_ARG;
@@ -522,13 +550,15 @@ extern "C" sp_status sp_fp8_linear(const sp_fp8_linear_args* a, void* ws, size_t
   if (a->m == 0) return SP_OK;
   const int sms = current_sms();
   if (sms == 0) return SP_ERR_CUDA;
+  const int nt = a->m <= kFewTokens ? 0 : pair_rows(a->m, a->n, a->k, sms);
+  if (expire && (a->m <= kFewTokens ? few_box(a->m) != 16 : nt != 128)) return SP_ERR_UNSUPPORTED;
   cudaStream_t stream = (cudaStream_t)stream_;
   PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
   sp_status st = tensor_map_encoder(&encode);
   if (st != SP_OK) return st;
   CUtensorMap map_w, map_x;
   if (a->m <= kFewTokens && (st = code_map(&map_w, encode, a->w, a->n, a->k, a->w_stride, kFp8Block)) != SP_OK) return st;
-  if (a->x && few_fused(a->m, a->n, a->k, sms)) return launch_fp8_few(*a, nullptr, map_w, map_w, sms, stream);
+  if (a->x && few_fused(a->m, a->n, a->k, sms)) return launch_fp8_few(*a, nullptr, map_w, map_w, sms, expire, stream);
   const Workspace w = workspace_for(a->m, a->k, sms);
   if ((a->x || a->m > kFewTokens) && (!ws || ws_bytes < w.bytes)) return SP_ERR_WORKSPACE;
   uint8_t* base = static_cast<uint8_t*>(ws);
@@ -542,14 +572,23 @@ extern "C" sp_status sp_fp8_linear(const sp_fp8_linear_args* a, void* ws, size_t
   }
   if (a->m <= kFewTokens) {
     st = code_map(&map_x, encode, rows.codes, a->m, a->k, rows.stride, few_box(a->m));
-    return st != SP_OK ? st : launch_fp8_few(*a, &rows, map_w, map_x, sms, stream);
+    return st != SP_OK ? st : launch_fp8_few(*a, &rows, map_w, map_x, sms, expire, stream);
   }
-  // rows of W in a tile: where the time is less
-  const int64_t blocks = (a->k + kFp8Block - 1) / kFp8Block;
   float* part = reinterpret_cast<float*>(base + w.part);
-  auto clocks = [&](int nt) { return pair_work(nt, a->m, a->n, blocks, sms / 2).clocks; };
-  const int nt = clocks(256) <= clocks(192) && clocks(256) <= clocks(128) ? 256 : clocks(192) <= clocks(128) ? 192 : 128;
-  return nt == 256   ? launch_pair<256>(*a, rows, ws, part, sms, encode, stream)
-         : nt == 192 ? launch_pair<192>(*a, rows, ws, part, sms, encode, stream)
-                     : launch_pair<128>(*a, rows, ws, part, sms, encode, stream);
+  return nt == 256   ? launch_pair<256>(*a, rows, ws, part, sms, encode, nullptr, stream)
+         : nt == 192 ? launch_pair<192>(*a, rows, ws, part, sms, encode, nullptr, stream)
+                     : launch_pair<128>(*a, rows, ws, part, sms, encode, expire, stream);
+}
+
+}  // namespace
+
+extern "C" sp_status sp_fp8_linear(const sp_fp8_linear_args* a, void* ws, size_t ws_bytes, void* stream) {
+  return linear(a, ws, ws_bytes, nullptr, stream);
+}
+
+extern "C" sp_status sp_test_expired_fp8(const sp_fp8_linear_args* a, void* ws, size_t ws_bytes, int32_t cta, int32_t warp,
+                                         int32_t block, uint32_t wait_ms, void* stream) {
+  if (cta < 0 || warp < 0 || block < 0 || wait_ms < 1 || wait_ms > 10000) return SP_ERR_INVALID_ARG;
+  const Fp8Expire e = {cta, warp, block, (uint64_t)wait_ms * 1000000ull};
+  return linear(a, ws, ws_bytes, &e, stream);
 }

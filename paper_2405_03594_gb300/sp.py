@@ -34,7 +34,7 @@ EXPORTS = ["sp_compress", "sp_decompress", "sp_workspace_size", "sp_linear", "sp
            "sp_chain_run", "sp_linear_epi", "sp_kv4_bytes", "sp_kv_plan", "sp_qk_norm_rope", "sp_kv4_read",
            "sp_kv4_attend", "sp_kv4_attend_workspace_size", "sp_test_expired_attend", "sp_token_logprobs",
            "sp_kv_retract", "sp_token_probs", "sp_verify_drafts", "sp_fp8_quantize_rows", "sp_fp8_quantize_blocks",
-           "sp_fp8_linear", "sp_fp8_workspace_size"]
+           "sp_fp8_linear", "sp_fp8_workspace_size", "sp_test_expired_fp8"]
 
 
 KERNELS = {0: "", 1: "linear_cc_kernel", 2: "linear_ccw_kernel", 3: "linear_tc_kernel", 4: "linear_mma_kernel",
@@ -169,6 +169,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.sp_fp8_quantize_rows.argtypes = [P, I64, I64, I64, P, I64, P, I64, P]
     lib.sp_fp8_quantize_blocks.argtypes = [P, I64, I64, I64, P, I64, P, P]
     lib.sp_fp8_linear.argtypes = [ctypes.POINTER(SpFp8LinearArgs), P, SZ, P]
+    lib.sp_test_expired_fp8.argtypes = [ctypes.POINTER(SpFp8LinearArgs), P, SZ, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                        ctypes.c_uint32, P]
     lib.sp_fp8_workspace_size.argtypes = [I64, I64, I64, ctypes.POINTER(SZ)]
     lib.sp_status_string.argtypes = [ctypes.c_int]
     lib.sp_status_string.restype = ctypes.c_char_p
