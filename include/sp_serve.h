@@ -224,7 +224,7 @@ sp_status sp_token_logprobs(const void* logits, sp_logits_dtype dtype, int64_t s
  * is one whose temperature is a NaN; T = +inf makes all entries above -inf alike.  min_p in 0..1, vocab below 2^31
  * (SP_ERR_UNSUPPORTED); rows of both that lie at the same distance from 16-byte boundaries, counted in entries, are written
  * fastest, as contiguous rows do; the stretch of memory from
- * `out`'s first entry to its last must not overlap that of the logits (SP_ERR_INVALID_ARG).  Results are bitwise repeatable for given sizes,
+ * `out`'s first entry to its last must not overlap that of the logits, nor the temperatures (SP_ERR_INVALID_ARG).  Results are bitwise repeatable for given sizes,
  * addresses and device; the order in which a row is added up, and with it the last bits, depends on the number of rows (few rows
  * have several CTAs each) and on where in 16 bytes the row begins.  One launch.  tokens == 0 returns SP_OK. */
 sp_status sp_token_probs(const void* logits, sp_logits_dtype dtype, int64_t stride, int64_t tokens, int64_t vocab,

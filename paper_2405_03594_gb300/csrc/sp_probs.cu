@@ -273,10 +273,11 @@ extern "C" sp_status sp_token_probs(const void* logits, sp_logits_dtype dtype, i
   if (reinterpret_cast<uintptr_t>(logits) % es || reinterpret_cast<uintptr_t>(out) % 4 ||
       reinterpret_cast<uintptr_t>(temperature) % 4)
     return SP_ERR_ALIGNMENT;
-  // (pieces of a row may be read again while others are written)
-  const uintptr_t in0 = reinterpret_cast<uintptr_t>(logits), out0 = reinterpret_cast<uintptr_t>(out);
-  if (in0 < out0 + 4 * ((uintptr_t)(tokens - 1) * out_stride + vocab) && out0 < in0 + es * ((uintptr_t)(tokens - 1) * stride + vocab))
-    return SP_ERR_INVALID_ARG;
+  // (pieces of a row may be read again while others are written, and a row's temperature once other rows are)
+  const uintptr_t in0 = reinterpret_cast<uintptr_t>(logits), out0 = reinterpret_cast<uintptr_t>(out), t0 = reinterpret_cast<uintptr_t>(temperature);
+  const uintptr_t out1 = out0 + 4 * ((uintptr_t)(tokens - 1) * out_stride + vocab);
+  if (in0 < out1 && out0 < in0 + es * ((uintptr_t)(tokens - 1) * stride + vocab)) return SP_ERR_INVALID_ARG;
+  if (temperature && t0 < out1 && out0 < t0 + 4 * (uintptr_t)tokens) return SP_ERR_INVALID_ARG;
   const int sms = current_sms();
   if (sms == 0) return SP_ERR_CUDA;
   const int64_t pieces = (vocab * es + 15) / 16;

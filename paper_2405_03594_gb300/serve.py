@@ -357,7 +357,7 @@ def token_probs(logits: torch.Tensor, temperature=1.0, min_p: float = 0.0, out: 
                 stream=None) -> torch.Tensor:
     """sp_token_probs: probabilities, float32 [T, V], of the rows of logits [T, V] (bf16 or float32, rows of unit
     stride).  temperature: a number, or one for each row (float32 [T], neither more nor fewer); 0 or less takes the best entry.
-    min_p: entries of less than min_p times the best one's probability are left out.  out must not overlap logits.  The last
+    min_p: entries of less than min_p times the best one's probability are left out.  out must not overlap logits or temperature.  The last
     bits of a row depend on how many rows the call has: those of a row alone and among others may differ."""
     dev = _on_current(logits.get_device(), logits, "logits")
     kind = _row_type(logits, dev, "logits")

@@ -28,3 +28,18 @@ def test_a_row_alone_and_among_others(v, dtype):
             # (entries are left out by their own logit and the best one, which no order changes)
             assert torch.equal(some == 0, among[r:r + n] == 0)
     sp.check()
+
+
+def test_temperatures_beside_the_results():
+    """Right before the first entry and right behind the last one is no overlap."""
+    from paper_2405_03594_gb300 import serve, sp
+
+    x = torch.randn((3, 100), generator=torch.Generator(device="cuda").manual_seed(0), device="cuda")
+    one = torch.full((3 + 300 + 3,), 0.5, device="cuda")
+    want = serve.token_probs(x, 0.5)
+    for t in (one[:3], one[303:]):
+        assert torch.equal(serve.token_probs(x, t, out=one[3:303].view(3, 100)), want)
+        assert (t == 0.5).all()
+    with pytest.raises(sp.SpError, match="INVALID_ARG"):
+        serve.token_probs(x, one[302:305], out=one[3:303].view(3, 100))
+    sp.check()
