@@ -55,7 +55,8 @@ typedef struct sp_fp8_linear_args {
 /* y = x . W^T.  x is quantised on the way (into the workspace, or on chip where there are few rows).  `workspace` as for
  * sp_linear: sp_fp8_workspace_size bytes, its first SP_WORKSPACE_ZERO_BYTES zero before its first use, calls that share it
  * ordered on one stream; one buffer can serve every call of the library that takes one.  Results are bitwise
- * repeatable for given sizes and device, and the same whether x or xq is given.  SP_ERR_INVALID_ARG for a null pointer, a
+ * repeatable for given sizes and device, and the same whether x or xq is given.  y must not overlap x, xq or their scales; what lies
+ * beside its rows is left as it is.  SP_ERR_INVALID_ARG for a null pointer, a
  * negative size, n or k of 0, a stride that is too small, both or neither of x and xq; SP_ERR_UNSUPPORTED for sizes above
  * 2^30, strides of codes that are no multiple of 16, or more than 64 rows on a device that holds no pair of CTAs; SP_ERR_ALIGNMENT for codes, x_scale or the workspace off a
  * 16-byte boundary, or bf16 off its own size.  m == 0 returns SP_OK.  One launch, or two.  Of a launch that sp_check reports as

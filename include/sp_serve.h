@@ -261,7 +261,7 @@ typedef struct sp_verify_args {
  * depends on nothing but the inputs.  Probabilities need not add up to 1.  A row without any weight gives -1; a
  * drafted token outside the vocabulary is refused; of a request whose rows and drafts do not belong together nothing is
  * kept (0, 0, -1): all three are recorded for sp_check.  A request without rows gets (0, 0, -1).  vocab up to 2^22 (SP_ERR_UNSUPPORTED); an
- * address off its entries' own size gives SP_ERR_ALIGNMENT.  One launch.
+ * address off its entries' own size gives SP_ERR_ALIGNMENT.  What is written must not overlap what is read.  One launch.
  * requests == 0 returns SP_OK. */
 sp_status sp_verify_drafts(const sp_verify_args* args, void* stream);
 

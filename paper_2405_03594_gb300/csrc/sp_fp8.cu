@@ -2,8 +2,10 @@
 //
 // A row's block is held by 16 lanes, eight entries each, a warp taking two neighbouring blocks; its largest
 // magnitude goes around by shuffles, so that x is read once and its codes and scale are written once.  A weight's
-// block of 128 x 128 is held by a CTA's registers in the same way.  Measured: 4096 x 4096 (50 MB) 12 us, 4.2 TB/s, of
-// 0.75 of the issue slots before four pairs of blocks went to a warp (17 us); 16 x 4096 4 us, which is latency.
+// block of 128 x 128 is held by a CTA's registers in the same way.  Measured: rows of 4096 x 4096 (50 MB) 11 us, 4.5 TB/s (17 us, of
+// 0.75 of the issue slots, before four pairs of blocks went to a warp; half of them are taken now, and a warp has one batch of loads in its
+// life, so that the rest is their way); 16 x 4096 1.3 us among others, 4 alone, which is latency.  A weight of 4096 x 4096
+// 11.7 us, of 22016 x 4096 57 us (4.7 TB/s): a CTA's loads, its maximum and its stores follow one another, four CTAs to an SM.
 #include <type_traits>
 
 #include "sp_fp8.cuh"

@@ -115,8 +115,8 @@ __device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
 __device__ __forceinline__ void fma_behind(float& c, uint32_t a, float s) {
   asm volatile("fma.rn.f32 %0, %1, %2, %0;" : "+f"(c) : "f"(__uint_as_float(a)), "f"(s));
 }
-// The same for two numbers at once. Where a thread's registers are nearly all taken the pairs cost moves: 256 columns of a tile
-// take 300 us of 4096 x 22016 x 4096 one by one and 370 in pairs, 128 columns 397 and 356.
+// The same for two numbers at once. Where a thread's registers are nearly all taken the pairs cost moves: with 256 columns a tile
+// 4096 x 22016 x 4096 takes 301 us one by one and 306 in pairs (4096 x 19456 x 8192: 468 and 528), with 128 columns 401 and 367.
 __device__ __forceinline__ void fma2_behind(float& c0, float& c1, uint32_t a0, uint32_t a1, float s) {
   asm volatile(
       "{\n\t.reg .b64 c, a, s;\n\t"

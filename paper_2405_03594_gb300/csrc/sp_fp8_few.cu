@@ -2,7 +2,7 @@
 //
 // Bound by reading W once. A tile is 128 rows of W (the lanes of tensor memory) by MT tokens (its columns), so that
 // W is the tensor cores' first operand and few tokens waste no time there. The blocks of a tile's rows are shared by the
-// CTAs of a cluster, as many as fill the machine; each holds up to ninety kilobytes of W in flight, two of them on an SM, and
+// CTAs of a cluster, as many as fill the machine; each holds 80 kilobytes of W in flight (64 with tiles of 64 tokens), two of them on an SM, and
 // their sums meet through the cluster's shared memory, in order. Nothing goes through global memory but
 // W, x and y:
 //   producer    W's tiles by TMA into a ring, asked into L2 before the launch before this one has ended; of quantised x its

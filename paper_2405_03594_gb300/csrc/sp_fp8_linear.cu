@@ -8,7 +8,8 @@
 // fp8_pair_kernel: pairs of SMs (cta_group::2), a tile of 256 tokens (the lanes of tensor memory, 128 in each CTA) by NT rows of
 // W. A thread's scale of a block is then one number, and a sum costs one FMA. What a block costs, 4096 x 22016 x 4096 with NT = 256,
 // in clocks of the SM (a block's products alone: 512): copies 590, copies and products 680, copies and the epilogue 720,
-// all together 890, in tiles that cost 2400 more: 300 us, 2.46 PFLOP/s. The products and the epilogue meet at tensor memory,
+// all together 890, in tiles that cost 3500 more (16 waves of tiles of 16, 32, 64 blocks: 138, 248, 468 us at 2070 MHz): 300 us, 2.46 PFLOP/s,
+// of which 15 are the nineteenth wave of 8 tiles. The products and the epilogue meet at tensor memory,
 // which both read, and the epilogue's eight warps hold as many sums as their registers take, so that they work on one block at a time.
 // One commit a block, which frees the copies' stage and hands over the sums: with one for each it is 311 us. The scales of four
 // blocks are under way in registers of their own, and rows go out through shared memory: 396 us at first, which waited for
@@ -420,7 +421,7 @@ sp_status code_map(CUtensorMap* map, PFN_cuTensorMapEncodeTiled_v12000 encode, c
 // and some 3500 around a tile. Where tiles are fewer than the pairs they are shared by the blocks of their columns, at 4000
 // and some for each share, if that is less. Measured, us, with shares / without: 128 x 4096 x 11008 (NT = 128, two) 26.5 / 38.3; tiles left
 // by whole waves in a launch of shares behind them: 512 x 12288 x 4096 52 / 38, so those are not shared. The three widths, 128 / 192 / 256, us:
-// 100 x 3000 x 4096 15.3 / 19.6 / 21.8, 512 x 12288 x 4096 40.2 / 35.2 / 37.3, 4096 x 22016 x 4096 368 / 366 / 299.
+// 100 x 3000 x 4096 15.1 / 19.3 / 21.4, 512 x 12288 x 4096 39.5 / 34.8 / 36.8, 4096 x 22016 x 4096 367 / 364 / 301.
 struct PairWork {
   int64_t tiles;
   int split;
@@ -465,7 +466,8 @@ int resident_pairs(int dev) {
   });
 }
 
-// SP_ERR_UNSUPPORTED where the device holds no pair.
+// SP_ERR_UNSUPPORTED where the device holds no pair (x has been quantised into the workspace by then).  Registers: the epilogue's
+// sums leave few; with shared tiles of 256 columns 164 bytes of a thread's others are kept in memory, with the rest 28 or 48.
 template <int NT>
 sp_status launch_pair(const sp_fp8_linear_args& a, const Fp8Rows& rows, void* ws, float* part, int sms,
                       PFN_cuTensorMapEncodeTiled_v12000 encode, const Fp8Expire* expire, cudaStream_t stream) {
